@@ -54,7 +54,7 @@ typedef enum {
   PARD_ERR_RANGE = -7        /* the call ran, but an activation exceeded fp16's range (see below) */
 } pard_status;
 
-enum { PARD_F32 = 0, PARD_BF16 = 1 };
+enum { PARD_F32 = 0, PARD_BF16 = 1, PARD_F16 = 2 };
 enum { PARD_TARGET = 0, PARD_DRAFT = 1 };
 /* Drafting of the fused loop: PARD's one parallel pass over the pending tokens
  * and K-1 mask tokens (Sec. 3.1, eq. 7), or vanilla speculative decoding's K
@@ -344,6 +344,190 @@ pard_status pard_cod_build_noalloc(const int32_t *tokens, const int64_t *tok_off
                                    const int64_t *out_offsets, int32_t *out_ids, int32_t *out_labels,
                                    int32_t *out_pos, int32_t *out_section, int32_t *out_column,
                                    int32_t *out_len, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Mask-token training on the packed rows of pard_cod_build (Sec. 3.2, eq. 8).
+ *
+ * Next to matrix products and RMSNorm, a training step of the draft takes the
+ * rotation of queries and keys (packed rows repeat positions), attention over
+ * the packed rows, and the loss.  These calls work on the caller's device
+ * buffers.  Except pard_cod_plan_build they only enqueue work on hip_stream
+ * (NULL: the default stream), return at once and can be captured into a HIP
+ * graph; the current device must be the stream's.  They allocate nothing: a
+ * workspace (256-byte aligned) is scratch of one call, needs no clearing, and
+ * may be used again by a later call on the same stream.  Two calls that may
+ * run at the same time (two streams, two graphs) need workspaces of their own.
+ * Status codes as everywhere; there is no context, so no message.
+ * ------------------------------------------------------------------------ */
+
+/* A [rows][heads][head_dim] tensor: strides in elements (positive; heads do
+ * not overlap), the elements of a head contiguous. */
+typedef struct {
+  void *data;
+  int64_t row_stride, head_stride;
+} pard_heads;
+
+/* Rotary tables.  Frequency i < rot_dim / 2 is w = theta^(-2i / rot_dim),
+ * scaled for long contexts:
+ *   PARD_ROPE_PLAIN   unchanged
+ *   PARD_ROPE_LINEAR  w / factor
+ *   PARD_ROPE_LLAMA3  as the rope_* fields of pard_model_spec (low, high: turns
+ *                     of the original context)
+ *   PARD_ROPE_YARN    w (1 - ramp) + ramp w / factor, ramp rising from 0 to 1
+ *                     between the dims floor(dim(high)) and ceil(dim(low)) (cut
+ *                     to [0, rot_dim - 1]), dim(t) = rot_dim ln(original_max_pos
+ *                     / (2 pi t)) / (2 ln theta); cosines and sines are
+ *                     multiplied by 0.1 ln(factor) + 1
+ * pard_rope_table writes (cos, sin)(pos * w_i), computed in float64, as float
+ * pairs [n_pos][rot_dim / 2].  Errors: ARG (rot_dim not even or outside [2,
+ * 1024], n_pos outside [1, 2^24], theta <= 1, unknown scaling; factor < 1,
+ * and for LLAMA3 / YARN not 0 < low < high or original_max_pos < 1; table null
+ * or not 16-byte aligned), DEVICE.  pard_rope_table_bytes: its size (0 if
+ * invalid). */
+enum { PARD_ROPE_PLAIN = 0, PARD_ROPE_LINEAR = 1, PARD_ROPE_LLAMA3 = 2, PARD_ROPE_YARN = 3 };
+typedef struct {
+  int32_t rot_dim, scaling;
+  float theta, factor, low, high;
+  int32_t original_max_pos;
+} pard_rope_spec;
+size_t pard_rope_table_bytes(const pard_rope_spec *spec, int32_t n_pos);
+pard_status pard_rope_table(const pard_rope_spec *spec, int32_t n_pos, float *table, void *hip_stream);
+
+/* Rotation of queries and keys in one pass, after an optional RMSNorm of every
+ * head.  For a head x at position p = positions[row]:
+ *   n = x                                     (q_gain and k_gain null)
+ *   n = gain * x / sqrt(mean(x^2) + eps)      (gains: float[head_dim])
+ *   y = n with the pairs (a, b) = (n[i], n[i + rot_dim / 2]) (PARD_ROPE_HALF)
+ *       or (n[2i], n[2i + 1]) (PARD_ROPE_INTERLEAVED), i < rot_dim / 2, turned
+ *       to (a cos - b sin, b cos + a sin); dims from rot_dim on are n.
+ * Everything is computed in float32 and rounded once to dtype (PARD_F32,
+ * PARD_BF16 or PARD_F16).  A row whose position is outside [0, n_pos) gets
+ * NaN.  Outputs may be the inputs themselves (same data and strides), but may
+ * not overlap them otherwise.  n_k = 0: no keys (k, k_out, k_gain unused).
+ * Vectorised where data and strides are multiples of 16 bytes, head_dim and
+ * rot_dim of 16 and head_dim <= 512; slower otherwise.
+ * Errors: ARG (null pointer, rows < 0, n_q < 1, n_k < 0, head_dim outside [2,
+ * 1024], rot_dim not even or outside [2, head_dim], n_pos outside [1, 2^24],
+ * unknown layout, one gain without the other, negative or non-finite eps,
+ * strides < 1 or below an overlap), UNSUPPORTED (dtype; rows * (n_q + n_k)
+ * above 2^31 - 1), DEVICE. */
+enum { PARD_ROPE_HALF = 0, PARD_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  int64_t rows;
+  int32_t n_q, n_k, head_dim, dtype;
+  int32_t rot_dim, layout, n_pos;
+  float eps;
+  const int32_t *positions;        /* device, [rows] */
+  const float *table;              /* device, pard_rope_table of n_pos positions */
+  const float *q_gain, *k_gain;    /* device, [head_dim]; both or neither */
+} pard_rope_args;
+pard_status pard_qk_rope(const pard_rope_args *args, const pard_heads *q, const pard_heads *k,
+                         const pard_heads *q_out, const pard_heads *k_out, void *hip_stream);
+
+/* Gradient of pard_qk_rope: from dy (q_dy, k_dy) to dx (q_dx, k_dx).  With
+ * gains, q and k are the forward call's inputs and the gains' gradients are
+ * written to q_dgain and k_dgain (float[head_dim], sums over rows and heads,
+ * deterministic); without, q, k, q_dgain and k_dgain are not used and may be
+ * null.  dx may be dy itself.  The workspace is needed with gains only.
+ * Errors: as pard_qk_rope; NOMEM (workspace too small). */
+size_t pard_qk_rope_workspace_bytes(const pard_rope_args *args);
+pard_status pard_qk_rope_grad(const pard_rope_args *args, const pard_heads *q_dy, const pard_heads *k_dy,
+                              const pard_heads *q, const pard_heads *k, const pard_heads *q_dx,
+                              const pard_heads *k_dx, float *q_dgain, float *k_dgain, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/* Plan of a batch of packed samples for pard_cod_attn, built once per batch
+ * and used by every layer's calls.  section, column, out_offsets and out_len
+ * are pard_cod_build's (out_offsets on the host, the others on the device);
+ * any rows in its form will do: in each sample's region the rows of subtask 1
+ * (columns 0, 1, 2, ..), then those of each later subtask k <= 64 by ascending
+ * column, each with column - k + 1 in subtask 1's columns; at most 8192
+ * columns.  A sample of length 0 is empty.  Rows of a region past its sample's
+ * length are padding; rows outside the regions belong to no sample.
+ * plan_data (device, 256-byte aligned, pard_cod_plan_bytes(rows, n_samples)
+ * bytes with rows = out_offsets[n_samples]) must live as long as *plan, which
+ * refers to it.  The call waits for its result, so it cannot be captured.
+ * Errors: ARG (null pointer, misaligned plan_data, n_samples < 1, offsets
+ * negative or descending, rows not in the form above: then *plan is not set),
+ * UNSUPPORTED (2^31 rows or more), NOMEM (plan_bytes too small), DEVICE. */
+typedef struct {
+  int64_t rows;                    /* out_offsets[n_samples] */
+  int32_t n_samples, n_tiles;
+  const void *data;
+} pard_cod_plan;
+size_t pard_cod_plan_bytes(int64_t rows, int32_t n_samples);
+pard_status pard_cod_plan_build(const int32_t *section, const int32_t *column, const int64_t *out_offsets,
+                                const int32_t *out_len, int32_t n_samples, void *plan_data, size_t plan_bytes,
+                                void *hip_stream, pard_cod_plan *plan);
+
+/* Attention over packed rows (the context of eq. 8, see pard_cod_build): row
+ * (k, j) attends to the real tokens t_0 .. t_{j-k+1} of its sample and to the
+ * rows (k', j - k + k'), 2 <= k' <= k, that are there.
+ *   out = softmax(scale * q K^T) V,  lse = log sum exp(scale * q K^T)
+ * q, out: [plan rows][n_heads][head_dim]; k, v: [plan rows][n_kv_heads]
+ * [head_dim], query head h reads key head h / (n_heads / n_kv_heads); lse:
+ * [n_heads][plan rows], float, may be null.  Padding rows of a region get out
+ * = 0 and lse = -inf; rows outside the regions are left as they are; neither's
+ * inputs are used, whatever they hold.  (A NaN or an infinity in a sample's
+ * own rows may reach any row of that sample.)  Scores, softmax and sums are
+ * float32; probabilities are rounded to dtype for the product with V.
+ * Results are deterministic.  No output may overlap an input.
+ * Errors: ARG (null pointer, a plan that was not built, head counts < 1,
+ * n_heads not a multiple of n_kv_heads, scale not finite, data not 16-byte
+ * aligned, strides not multiples of 8 elements or below head_dim), UNSUPPORTED
+ * (head_dim not 64 or 128, dtype not PARD_BF16 or PARD_F16), DEVICE. */
+typedef struct {
+  const pard_cod_plan *plan;
+  int32_t n_heads, n_kv_heads, head_dim, dtype;
+  float scale;
+} pard_cod_attn_args;
+pard_status pard_cod_attn(const pard_cod_attn_args *args, const pard_heads *q, const pard_heads *k,
+                          const pard_heads *v, const pard_heads *out, float *lse, void *hip_stream);
+
+/* Gradient of pard_cod_attn: out and lse are the forward call's outputs.
+ * Padding rows of dq, dk and dv get 0, rows outside the regions are left as
+ * they are.  Probabilities and score gradients are rounded to dtype for the
+ * products; sums over a key head's query heads are float32.  Deterministic.
+ * Errors: as pard_cod_attn; NOMEM (workspace too small). */
+size_t pard_cod_attn_workspace_bytes(const pard_cod_attn_args *args);
+pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads *d_out, const pard_heads *q,
+                               const pard_heads *k, const pard_heads *v, const pard_heads *out,
+                               const float *lse, const pard_heads *dq, const pard_heads *dk,
+                               const pard_heads *dv, void *workspace, size_t workspace_bytes,
+                               void *hip_stream);
+
+/* Mask-token loss (eq. 8: the cross entropy of each subtask averaged over its
+ * rows) and its gradient.  Row r counts if labels[r] >= 0 and section[r] is in
+ * [1, n_sections] (section may be null with n_sections = 1: every row is in
+ * subtask 1).  With CE = log sum exp(logits) - logits[label]:
+ *   loss[k] = mean of CE over subtask k's counted rows (0 if there are none)
+ *   loss[0] = sum_k weights[k - 1] loss[k]            (weights: host, floats)
+ *           = mean of CE over all counted rows        (weights null)
+ *   row_loss[r] = CE, 0 for rows that do not count (may be null)
+ *   d_logits = grad_scale * d loss[0] / d logits (may be null: loss only; may
+ *              be logits itself); rows that do not count get 0
+ * A label of vocab or more makes its row's loss and gradient NaN.  Sums are
+ * float32, means over rows float64.  logits, d_logits: dtype (PARD_F32,
+ * PARD_BF16, PARD_F16), [rows][vocab] with row strides in elements; loss:
+ * device, float[1 + n_sections].  Deterministic.
+ * Errors: ARG (null pointer, rows < 0, vocab < 1, n_sections outside [1, 64],
+ * strides below vocab, non-finite grad_scale or weights), UNSUPPORTED (dtype,
+ * 2^31 rows or more), NOMEM (workspace too small), DEVICE. */
+typedef struct {
+  int64_t rows;
+  int32_t vocab, dtype, n_sections;
+  float grad_scale;
+  const void *logits;
+  int64_t logits_stride;
+  const int32_t *labels, *section;   /* device, [rows] */
+  const float *weights;              /* host, [n_sections], or null */
+  void *d_logits;
+  int64_t d_stride;
+  float *loss, *row_loss;            /* device */
+} pard_cod_loss_args;
+size_t pard_cod_loss_workspace_bytes(const pard_cod_loss_args *args);
+pard_status pard_cod_loss(const pard_cod_loss_args *args, void *workspace, size_t workspace_bytes,
+                          void *hip_stream);
 
 /* Message of the last error on this context (never NULL; "" if none). */
 const char *pard_last_error(const pard_ctx *ctx);

@@ -24,9 +24,11 @@ lib = C.CDLL(LIB_PATH)
 
 PARD_OK, PARD_ERR_ARG, PARD_ERR_STATE, PARD_ERR_CAPACITY = 0, -1, -2, -3
 PARD_ERR_NOMEM, PARD_ERR_DEVICE, PARD_ERR_UNSUPPORTED, PARD_ERR_RANGE = -4, -5, -6, -7
-PARD_F32, PARD_BF16 = 0, 1
+PARD_F32, PARD_BF16, PARD_F16 = 0, 1, 2
 PARD_TARGET, PARD_DRAFT = 0, 1
 PARD_MODE_PARALLEL, PARD_MODE_VANILLA = 0, 1
+PARD_ROPE_PLAIN, PARD_ROPE_LINEAR, PARD_ROPE_LLAMA3, PARD_ROPE_YARN = range(4)
+PARD_ROPE_HALF, PARD_ROPE_INTERLEAVED = 0, 1
 OP_EMBED, OP_QKV, OP_ATTN, OP_O, OP_GATEUP, OP_DOWN, OP_LM, OP_TAIL = range(8)
 
 
@@ -47,7 +49,40 @@ class pard_stats(C.Structure):
                 ("accept_hist", C.c_int64 * 33)]
 
 
+class pard_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class pard_rope_spec(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_float), ("factor", C.c_float),
+                ("low", C.c_float), ("high", C.c_float), ("original_max_pos", C.c_int32)]
+
+
+class pard_rope_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n_q", C.c_int32), ("n_k", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("n_pos", C.c_int32),
+                ("eps", C.c_float), ("positions", C.c_void_p), ("table", C.c_void_p), ("q_gain", C.c_void_p),
+                ("k_gain", C.c_void_p)]
+
+
+class pard_cod_plan(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n_samples", C.c_int32), ("n_tiles", C.c_int32), ("data", C.c_void_p)]
+
+
+class pard_cod_attn_args(C.Structure):
+    _fields_ = [("plan", C.POINTER(pard_cod_plan)), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class pard_cod_loss_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int32), ("dtype", C.c_int32), ("n_sections", C.c_int32),
+                ("grad_scale", C.c_float), ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+                ("labels", C.c_void_p), ("section", C.c_void_p), ("weights", C.POINTER(C.c_float)),
+                ("d_logits", C.c_void_p), ("d_stride", C.c_int64), ("loss", C.c_void_p), ("row_loss", C.c_void_p)]
+
+
 _I32P = C.POINTER(C.c_int32)
+_HEADSP = C.POINTER(pard_heads)
 _SPECP = C.POINTER(pard_model_spec)
 _CTX = C.c_void_p
 
@@ -76,6 +111,21 @@ _sig = {
     "pard_cod_build_noalloc": (C.c_int, [C.c_void_p, C.POINTER(C.c_int64), C.c_int32, C.c_int32, C.c_double,
                                          C.c_double, C.c_int32, C.c_uint64, C.POINTER(C.c_int64), C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "pard_rope_table_bytes": (C.c_size_t, [C.POINTER(pard_rope_spec), C.c_int32]),
+    "pard_rope_table": (C.c_int, [C.POINTER(pard_rope_spec), C.c_int32, C.c_void_p, C.c_void_p]),
+    "pard_qk_rope": (C.c_int, [C.POINTER(pard_rope_args), *[_HEADSP] * 4, C.c_void_p]),
+    "pard_qk_rope_workspace_bytes": (C.c_size_t, [C.POINTER(pard_rope_args)]),
+    "pard_qk_rope_grad": (C.c_int, [C.POINTER(pard_rope_args), *[_HEADSP] * 6, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_size_t, C.c_void_p]),
+    "pard_cod_plan_bytes": (C.c_size_t, [C.c_int64, C.c_int32]),
+    "pard_cod_plan_build": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int32,
+                                      C.c_void_p, C.c_size_t, C.c_void_p, C.POINTER(pard_cod_plan)]),
+    "pard_cod_attn": (C.c_int, [C.POINTER(pard_cod_attn_args), *[_HEADSP] * 4, C.c_void_p, C.c_void_p]),
+    "pard_cod_attn_workspace_bytes": (C.c_size_t, [C.POINTER(pard_cod_attn_args)]),
+    "pard_cod_attn_grad": (C.c_int, [C.POINTER(pard_cod_attn_args), *[_HEADSP] * 5, C.c_void_p, *[_HEADSP] * 3,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]),
+    "pard_cod_loss_workspace_bytes": (C.c_size_t, [C.POINTER(pard_cod_loss_args)]),
+    "pard_cod_loss": (C.c_int, [C.POINTER(pard_cod_loss_args), C.c_void_p, C.c_size_t, C.c_void_p]),
     "pard_read_logits": (C.c_int, [_CTX, C.c_int32, C.c_int32, C.POINTER(C.c_float), C.c_int32,
                                    C.c_int32]),
     "pard_read_weight": (C.c_int, [_CTX, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
@@ -213,6 +263,299 @@ def cod_build_noalloc(tokens, tok_offsets: Sequence[int], k: int, r: float, r_mi
     if rc != PARD_OK:
         raise PardError(rc, "pard_cod_build_noalloc failed")
     return out_offs, out, out_len
+
+
+# ---- mask-token training: rotary positions, packed attention, the loss -----------
+
+def _bad(what: str):
+    raise PardError(PARD_ERR_ARG, what)
+
+
+_DTYPES = {}
+
+
+def _dtype(t, what: str) -> int:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: PARD_F32, torch.bfloat16: PARD_BF16, torch.float16: PARD_F16})
+    if t.dtype not in _DTYPES:
+        raise PardError(PARD_ERR_UNSUPPORTED, f"{what}: dtype {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _heads(t, what: str, like=None, shape=None) -> pard_heads:
+    """A [rows, heads, head_dim] device tensor whose heads are contiguous."""
+    if t.dim() != 3 or not t.is_cuda:
+        _bad(f"{what}: a [rows, heads, head_dim] device tensor is wanted, got {tuple(t.shape)} on {t.device}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        _bad(f"{what}: the elements of a head must be contiguous")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _bad(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _bad(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return pard_heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _vector(t, what: str, n: int, dtype, device) -> int:
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != (n,) or not t.is_contiguous():
+        _bad(f"{what}: a contiguous {dtype} tensor of {n} on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class _On:
+    """Runs a call on `stream` (a torch stream; None: the device's current one)
+    with that device current: outputs and workspaces made inside belong to the
+    stream, and `used` tensors stay alive until it is done with them."""
+
+    def __init__(self, device, stream, *used):
+        import torch
+        self.cuda = torch.cuda
+        now = torch.cuda.current_stream(device)
+        self.stream = now if stream is None else stream
+        self.handle = C.c_void_p(self.stream.cuda_stream)
+        self.ctx = None
+        if self.stream != now or torch.cuda.current_device() != self.stream.device_index:
+            if self.stream.device_index != now.device_index:
+                _bad("the stream belongs to another device than the tensors")
+            self.ctx = torch.cuda.stream(self.stream)
+        self.used = used if self.stream != now else ()
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        for t in self.used:
+            if t is not None:
+                t.record_stream(self.stream)
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _workspace(n_bytes: int, device):
+    import torch
+    return torch.empty(max(n_bytes, 1), dtype=torch.uint8, device=device)   # (the allocator aligns to 512 bytes)
+
+
+def _done(rc: int, what: str) -> None:
+    if rc != PARD_OK:
+        raise PardError(rc, f"{what} failed")
+
+
+_ROPE_SCALINGS = {None: PARD_ROPE_PLAIN, "linear": PARD_ROPE_LINEAR, "llama3": PARD_ROPE_LLAMA3, "yarn": PARD_ROPE_YARN}
+_ROPE_LAYOUTS = {"half": PARD_ROPE_HALF, "interleaved": PARD_ROPE_INTERLEAVED}
+
+
+def rope_table(n_pos: int, rot_dim: int, theta: float, scaling: Optional[str] = None, factor: float = 1.0,
+               low: float = 1.0, high: float = 4.0, original_max_pos: int = 8192, device="cuda", stream=None):
+    """(cos, sin) table [n_pos, rot_dim / 2, 2] of qk_rope (pard_rope_table);
+    scaling None, "linear", "llama3" or "yarn"."""
+    import torch
+    if scaling not in _ROPE_SCALINGS:
+        _bad(f"rope_table: unknown scaling {scaling!r}")
+    spec = pard_rope_spec(rot_dim, _ROPE_SCALINGS[scaling], theta, factor, low, high, original_max_pos)
+    if lib.pard_rope_table_bytes(C.byref(spec), n_pos) == 0:
+        _bad("rope_table: bad sizes or scaling parameters")
+    device = torch.device(device)
+    if device.index is None:
+        device = torch.device(device.type, torch.cuda.current_device())
+    with _On(device, stream) as on:
+        table = torch.empty(n_pos, rot_dim // 2, 2, dtype=torch.float32, device=device)
+        _done(lib.pard_rope_table(C.byref(spec), n_pos, C.c_void_p(table.data_ptr()), on.handle), "pard_rope_table")
+    return table
+
+
+def _rope_args(q, k, positions, table, layout, q_gain, k_gain, eps) -> pard_rope_args:
+    import torch
+    if layout not in _ROPE_LAYOUTS:
+        _bad(f"qk_rope: unknown layout {layout!r}")
+    rows, n_q, hd = q.shape
+    if (table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or table.device != q.device
+            or not table.is_contiguous()):
+        _bad("qk_rope: table: a contiguous float32 [n_pos, rot_dim / 2, 2] tensor on the queries' device is wanted")
+    gains = [None if g is None else _vector(g, "gain", hd, torch.float32, q.device) for g in (q_gain, k_gain)]
+    if k is not None and (q_gain is None) != (k_gain is None):
+        _bad("qk_rope: both gains or neither")
+    return pard_rope_args(rows, n_q, 0 if k is None else k.shape[1], hd, _dtype(q, "qk_rope"), 2 * table.shape[1],
+                          _ROPE_LAYOUTS[layout], table.shape[0], eps,
+                          _vector(positions, "positions", rows, torch.int32, q.device), table.data_ptr(), *gains)
+
+
+def qk_rope(q, k, positions, table, layout: str = "half", q_gain=None, k_gain=None, eps: float = 1e-6, q_out=None,
+            k_out=None, stream=None):
+    """Rotary positions of queries and keys [rows, heads, head_dim], with gains
+    after an RMSNorm of every head (pard_qk_rope).  k may be None.  Returns
+    (q_out, k_out), new tensors unless given; they may be q and k themselves."""
+    import torch
+    hq = _heads(q, "q")
+    hk = None if k is None else _heads(k, "k", q, (q.shape[0], k.shape[1], q.shape[2]))
+    args = _rope_args(q, k, positions, table, layout, q_gain, k_gain, eps)
+    with _On(q.device, stream, q, k, positions, table, q_gain, k_gain, q_out, k_out) as on:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k_out is None and k is not None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        oq = _heads(q_out, "q_out", q, q.shape)
+        ok = None if k is None else _heads(k_out, "k_out", k, k.shape)
+        _done(lib.pard_qk_rope(args, hq, hk, oq, ok, on.handle), "pard_qk_rope")
+    return q_out, None if k is None else k_out
+
+
+def qk_rope_grad(q_dy, k_dy, positions, table, layout: str = "half", q=None, k=None, q_gain=None, k_gain=None,
+                 eps: float = 1e-6, q_dx=None, k_dx=None, stream=None):
+    """Gradient of qk_rope (pard_qk_rope_grad).  With gains, q and k are the
+    forward call's inputs.  Returns (q_dx, k_dx, q_dgain, k_dgain), the last two
+    None without gains; q_dx and k_dx may be q_dy and k_dy themselves."""
+    import torch
+    hdq = _heads(q_dy, "q_dy")
+    hdk = None if k_dy is None else _heads(k_dy, "k_dy", q_dy, (q_dy.shape[0], k_dy.shape[1], q_dy.shape[2]))
+    args = _rope_args(q_dy, k_dy, positions, table, layout, q_gain, k_gain, eps)
+    hq = hk = None
+    if q_gain is not None:
+        if q is None or (k_dy is not None and k is None):
+            _bad("qk_rope_grad: the gradient of the norm needs the forward call's inputs")
+        hq = _heads(q, "q", q_dy, q_dy.shape)
+        hk = None if k_dy is None else _heads(k, "k", k_dy, k_dy.shape)
+    with _On(q_dy.device, stream, q_dy, k_dy, positions, table, q, k, q_gain, k_gain, q_dx, k_dx) as on:
+        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+        q_dx = new(q_dy) if q_dx is None else q_dx
+        k_dx = new(k_dy) if k_dx is None and k_dy is not None else k_dx
+        oq = _heads(q_dx, "q_dx", q_dy, q_dy.shape)
+        ok = None if k_dy is None else _heads(k_dx, "k_dx", k_dy, k_dy.shape)
+        q_dg = None if q_gain is None else new(q_gain)
+        k_dg = None if q_gain is None or k_dy is None else new(k_gain)
+        n_ws = lib.pard_qk_rope_workspace_bytes(args) if q_gain is not None else 0
+        ws = _workspace(n_ws, q_dy.device) if n_ws else None
+        _done(lib.pard_qk_rope_grad(args, hdq, hdk, hq, hk, oq, ok, q_dg.data_ptr() if q_dg is not None else None,
+                                    k_dg.data_ptr() if k_dg is not None else None,
+                                    ws.data_ptr() if n_ws else None, n_ws, on.handle), "pard_qk_rope_grad")
+    return q_dx, None if k_dy is None else k_dx, q_dg, k_dg
+
+
+class CodPlan:
+    """Plan of a batch of packed samples (pard_cod_plan): built once per batch,
+    used by every layer's cod_attn and cod_attn_grad."""
+
+    def __init__(self, plan: pard_cod_plan, data):
+        self.plan, self.data = plan, data
+        self.rows, self.device = plan.rows, data.device
+
+
+def cod_plan(section, column, out_offsets: Sequence[int], out_len, stream=None) -> CodPlan:
+    """Plan for attention over packed rows (pard_cod_plan_build).  section,
+    column, out_len: int32 device tensors as cod_build returns them,
+    out_offsets: the samples' regions (host, n_samples + 1)."""
+    import torch
+    offs = np.ascontiguousarray(np.asarray(out_offsets, np.int64))
+    n = len(offs) - 1
+    if offs.ndim != 1 or n < 1 or (np.diff(offs) < 0).any() or offs[0] < 0:
+        _bad("cod_plan: out_offsets must be ascending bounds of at least one sample")
+    rows = int(offs[-1])
+    dev = out_len.device
+    for name, t in (("section", section), ("column", column)):
+        if t.dtype != torch.int32 or t.device != dev or t.dim() != 1 or len(t) < rows or not t.is_contiguous():
+            _bad(f"cod_plan: {name}: a contiguous int32 tensor of at least {rows} on {dev} is wanted")
+    _vector(out_len, "out_len", n, torch.int32, dev)
+    n_bytes = lib.pard_cod_plan_bytes(rows, n)
+    if n_bytes == 0:
+        raise PardError(PARD_ERR_UNSUPPORTED, "cod_plan: too many rows")
+    plan = pard_cod_plan()
+    with _On(dev, stream, section, column, out_len) as on:
+        data = _workspace(n_bytes, dev)
+        _done(lib.pard_cod_plan_build(section.data_ptr(), column.data_ptr(), offs.ctypes.data_as(C.POINTER(C.c_int64)),
+                                      out_len.data_ptr(), n, data.data_ptr(), n_bytes, on.handle, plan),
+              "pard_cod_plan_build")
+    return CodPlan(plan, data)
+
+
+def _attn_args(q, k, v, plan: CodPlan, scale):
+    rows, n_q, hd = q.shape
+    if plan.device != q.device:
+        _bad(f"cod_attn: the plan is on {plan.device}, the tensors on {q.device}")
+    if rows < plan.rows:
+        _bad(f"cod_attn: {rows} rows, the plan has {plan.rows}")
+    shape = (rows, k.shape[1] if k.dim() == 3 else 0, hd)
+    hs = _heads(q, "q"), _heads(k, "k", q, shape), _heads(v, "v", q, shape)
+    scale = hd ** -0.5 if scale is None else float(scale)
+    return pard_cod_attn_args(C.pointer(plan.plan), n_q, shape[1], hd, _dtype(q, "cod_attn"), scale), hs
+
+
+def cod_attn(q, k, v, plan: CodPlan, scale: Optional[float] = None, out=None, stream=None):
+    """Attention over packed rows (pard_cod_attn): q [rows, heads, head_dim], k
+    and v [rows, kv heads, head_dim]; scale: head_dim ** -0.5 unless given.
+    Returns (out, lse), lse [heads, plan rows] in float32.  Rows that belong to
+    no sample's region are left as they are (out given) or hold nothing (new)."""
+    import torch
+    args, (hq, hk, hv) = _attn_args(q, k, v, plan, scale)
+    with _On(q.device, stream, q, k, v, plan.data, out) as on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ho = _heads(out, "out", q, q.shape)
+        lse = torch.empty(q.shape[1], plan.rows, dtype=torch.float32, device=q.device)
+        _done(lib.pard_cod_attn(args, hq, hk, hv, ho, lse.data_ptr(), on.handle), "pard_cod_attn")
+    return out, lse
+
+
+def cod_attn_grad(d_out, q, k, v, out, lse, plan: CodPlan, scale: Optional[float] = None, dq=None, dk=None, dv=None,
+                  stream=None):
+    """Gradient of cod_attn (pard_cod_attn_grad); out and lse are the forward
+    call's.  Returns (dq, dk, dv), new tensors unless given."""
+    import torch
+    args, (hq, hk, hv) = _attn_args(q, k, v, plan, scale)
+    hdo, ho = _heads(d_out, "d_out", q, q.shape), _heads(out, "out", q, q.shape)
+    if (lse.dtype != torch.float32 or lse.device != q.device or tuple(lse.shape) != (q.shape[1], plan.rows)
+            or not lse.is_contiguous()):
+        _bad(f"cod_attn_grad: lse: the forward call's ({q.shape[1]}, {plan.rows}) tensor is wanted")
+    with _On(q.device, stream, d_out, q, k, v, out, lse, plan.data, dq, dk, dv) as on:
+        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+        dq, dk, dv = (new(t) if d is None else d for d, t in ((dq, q), (dk, k), (dv, v)))
+        outs = [_heads(d, n, t, t.shape) for d, n, t in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v))]
+        n_ws = lib.pard_cod_attn_workspace_bytes(args)
+        ws = _workspace(n_ws, q.device)
+        _done(lib.pard_cod_attn_grad(args, hdo, hq, hk, hv, ho, lse.data_ptr(), *outs, ws.data_ptr(), n_ws, on.handle),
+              "pard_cod_attn_grad")
+    return dq, dk, dv
+
+
+def cod_loss(logits, labels, section, n_sections: int, weights: Optional[Sequence[float]] = None, grad: bool = True,
+             grad_scale: float = 1.0, d_logits=None, stream=None):
+    """Mask-token loss of logits [rows, vocab] and its gradient (pard_cod_loss).
+    labels, section: int32 [rows] (cod_build's; section None: one subtask);
+    weights: of the subtasks' means, None: the mean over all counted rows.
+    Returns (loss [], subtask means [n_sections], row losses [rows], d_logits or
+    None); d_logits may be logits itself."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _bad("cod_loss: logits: a [rows, vocab] device tensor with contiguous rows is wanted")
+    rows, vocab = logits.shape
+    dev = logits.device
+    w = None
+    if weights is not None:
+        if len(weights) != n_sections:
+            _bad(f"cod_loss: {len(weights)} weights for {n_sections} subtasks")
+        w = (C.c_float * max(n_sections, 1))(*[float(x) for x in weights])
+    p_labels = _vector(labels, "labels", rows, torch.int32, dev)
+    p_section = None if section is None else _vector(section, "section", rows, torch.int32, dev)
+    if not 1 <= n_sections <= 64:
+        _bad("cod_loss: n_sections outside [1, 64]")
+    with _On(dev, stream, logits, labels, section, d_logits) as on:
+        if grad and d_logits is None:
+            d_logits = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
+        if not grad:
+            d_logits = None
+        elif (d_logits.dtype != logits.dtype or d_logits.device != dev or d_logits.shape != logits.shape
+              or (vocab > 1 and d_logits.stride(1) != 1)):
+            _bad("cod_loss: d_logits: a tensor like logits is wanted")
+        loss = torch.empty(1 + n_sections, dtype=torch.float32, device=dev)
+        row_loss = torch.empty(rows, dtype=torch.float32, device=dev)
+        args = pard_cod_loss_args(rows, vocab, _dtype(logits, "cod_loss"), n_sections, grad_scale, logits.data_ptr(),
+                                  logits.stride(0), p_labels, p_section, w, None if d_logits is None else d_logits.data_ptr(),
+                                  0 if d_logits is None else d_logits.stride(0), loss.data_ptr(), row_loss.data_ptr())
+        n_ws = lib.pard_cod_loss_workspace_bytes(args)
+        ws = _workspace(n_ws, dev)
+        _done(lib.pard_cod_loss(args, ws.data_ptr(), n_ws, on.handle), "pard_cod_loss")
+    return loss[0], loss[1:], row_loss, d_logits
 
 
 class Engine:
