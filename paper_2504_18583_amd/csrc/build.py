@@ -28,9 +28,9 @@ STEP_EXE = os.path.join(PKG, "step_counters")
 MFMA_EXE = os.path.join(PKG, "mfma_peak")
 
 SOURCES = ["engine.hip", "gemm.hip", "gemm_rows.hip", "attention.hip", "attn_prefill.hip", "device_init.hip", "cod.hip",
-           "rope.hip", "cod_plan.hip", "cod_attn.hip", "cod_loss.hip", "train.hip",
+           "rope.hip", "cod_plan.hip", "cod_attn.hip", "cod_attn_grad.hip", "cod_loss.hip", "train.hip",
            "gemm_counters.hip", "layer_counters.hip", "step_counters.hip", "mfma_peak.hip"]
-LIB_SOURCES = SOURCES[:12]
+LIB_SOURCES = SOURCES[:13]
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,167 +1,259 @@
-// Attention over packed COD rows, forward and gradient.
-#include "train.h"
+// Attention over packed COD rows on gfx950 MFMA.
+//
+// In the plan's order a row attends to the real tokens 0 .. c (one run of rows
+// in memory) and to the mask rows of its chain before it.  A workgroup of four
+// wavefronts owns 64 NQ (row, head) pairs of one key head, in order; a
+// wavefront 16 NQ of them.
+//   * First the wavefront's own chains: at most 16 NQ / group + K - 1 keys, by
+//     their places in the order, 32 at a time; K straight into operand
+//     registers, V through the wavefront's quarter of an LDS buffer.
+//   * Then all four walk the real tokens in stages of 64 keys through two LDS
+//     buffers (LDS-DMA, the next stage in flight during the current one).  Only
+//     stages around the wavefront's own tokens compare keys with rows.
+// A tile is S^T = K Q^T, online softmax in base 2, O^T += V^T P^T, with the
+// running maximum raised only when a score passes it by 2^kLazy.
+#include "cod_attn_tile.h"
 
 namespace pard {
 namespace {
 
-__device__ __forceinline__ float wave_sum(float x) {
+using namespace cod;
+
+constexpr int kStageKeys = 64;
+constexpr float kLazy = 8.f;
+
+// Softmax of NB blocks of 16 keys: scores s become packed probabilities pf,
+// running maximum m (base 2), sum l and output o follow.  Hidden scores are
+// -infinity; m starts finite, so that a row without keys keeps l = 0.
+template <int NQ, int NB, int DB, class M>
+__device__ __forceinline__ void softmax_step(const f32x4 (&s)[NQ][NB], float (&m)[NQ], float (&l)[NQ], f32x4 (&o)[NQ][DB],
+                                             u32x4 (&pf)[NQ][NB / 2], float scale2) {
+  bool raise = false;
+  float mx[NQ];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
-  return x;
-}
-__device__ __forceinline__ float wave_max(float x) {
+  for (int t = 0; t < NQ; ++t) {
+    float v = fmaxf(s[t][0][0], s[t][0][1]);
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
-  return x;
-}
-
-template <class E>
-__device__ __forceinline__ const typename E::T* at(const Heads& h, int64_t row, int head) {
-  return reinterpret_cast<const typename E::T*>(h.data) + row * h.rs + head * h.hs;
-}
-template <class E>
-__device__ __forceinline__ typename E::T* at_out(const Heads& h, int64_t row, int head) {
-  return reinterpret_cast<typename E::T*>(h.data) + row * h.rs + head * h.hs;
-}
-
-template <int HD, class E>
-__device__ __forceinline__ float dot(const typename E::T* a, const typename E::T* b) {
-  float s = 0.f;
-  for (int d = 0; d < HD; ++d) s += E::load(a[d]) * E::load(b[d]);
-  return s;
-}
-
-// Calls f(row) for this lane's share of the rows that order entry m (at
-// position p) attends to.
-template <class F>
-__device__ __forceinline__ void keys_of(const CodPlanView& v, int off, int4 m, int p, F&& f) {
-  const int lane = threadIdx.x;
-  for (int t = lane; t < m.y; t += 64) f(t);
-  for (int b = m.z + lane; b <= p && b < m.w; b += 64) f(v.order[off + b].x);
-}
-
-// One wavefront per (order position of a tile, query head): a lane's keys 64
-// apart, its own maximum, sum and output, joined at the end.
-template <int HD, class E>
-__global__ __launch_bounds__(64) void k_fwd(const CodAttnArgs a) {
-  const int2 tile = a.plan.tiles[blockIdx.x / kCodTile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int p = tile.y * kCodTile + blockIdx.x % kCodTile, h = blockIdx.y;
-  if (p >= s.cap) return;
-  const int4 m = a.plan.order[s.off + p];
-  const int64_t row = s.off + m.x;
-  const auto* q = at<E>(a.q, row, h);
-  const int kvh = h / a.group;
-  float mx = -INFINITY, l = 0.f, acc[HD];
-  for (int d = 0; d < HD; ++d) acc[d] = 0.f;
-  keys_of(a.plan, s.off, m, p, [&](int key) {
-    const float sc = a.scale * dot<HD, E>(q, at<E>(a.k, s.off + key, kvh));
-    const auto* v = at<E>(a.v, s.off + key, kvh);
-    const float n = fmaxf(mx, sc), c = expf(mx - n), w = expf(sc - n);
-    mx = n;
-    l = l * c + w;
-    for (int d = 0; d < HD; ++d) acc[d] = acc[d] * c + w * E::load(v[d]);
-  });
-  const float top = wave_max(mx);
-  const float c = top == -INFINITY ? 0.f : expf(mx - top);
-  l = wave_sum(l * c);
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  for (int d = 0; d < HD; ++d) {
-    const float o = wave_sum(acc[d] * c) * inv;
-    if (threadIdx.x == 0) at_out<E>(a.out, row, h)[d] = E::store(o);
+    for (int i = 2; i < 4 * NB; i += 2) v = fmaxf(fmaxf(v, s[t][i / 4][i % 4]), s[t][i / 4][i % 4 + 1]);
+    mx[t] = v * scale2;
+    raise |= mx[t] > m[t] + kLazy;
   }
-  if (threadIdx.x == 0 && a.lse) a.lse[h * a.rows + row] = l > 0.f ? top + logf(l) : -INFINITY;
-}
-
-template <int HD, class E>
-__global__ __launch_bounds__(64) void k_dq(const CodAttnArgs a) {
-  const int2 tile = a.plan.tiles[blockIdx.x / kCodTile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int p = tile.y * kCodTile + blockIdx.x % kCodTile, h = blockIdx.y;
-  if (p >= s.cap) return;
-  const int4 m = a.plan.order[s.off + p];
-  const int64_t row = s.off + m.x;
-  const int kvh = h / a.group;
-  float acc[HD];
-  for (int d = 0; d < HD; ++d) acc[d] = 0.f;
-  if (p < s.len) {
-    const auto* q = at<E>(a.q, row, h);
-    const auto* go = at<E>(a.d_out, row, h);
-    const float delta = dot<HD, E>(go, at<E>(a.out, row, h)), lse = a.lse[h * a.rows + row];
-    if (threadIdx.x == 0) a.delta[h * a.rows + row] = delta;
-    keys_of(a.plan, s.off, m, p, [&](int key) {
-      const auto* k = at<E>(a.k, s.off + key, kvh);
-      const float w = expf(a.scale * dot<HD, E>(q, k) - lse);
-      const float ds = w * (dot<HD, E>(go, at<E>(a.v, s.off + key, kvh)) - delta) * a.scale;
-      for (int d = 0; d < HD; ++d) acc[d] += ds * E::load(k[d]);
-    });
-  }
-  for (int d = 0; d < HD; ++d) {
-    const float o = wave_sum(acc[d]);
-    if (threadIdx.x == 0) at_out<E>(a.dq, row, h)[d] = E::store(o);
-  }
-}
-
-// One wavefront per (order position, key head): its key's queries are the
-// later positions (real token) or those of its chain (mask row).
-template <int HD, class E>
-__global__ __launch_bounds__(64) void k_dkv(const CodAttnArgs a) {
-  const int2 tile = a.plan.tiles[blockIdx.x / kCodTile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int p = tile.y * kCodTile + blockIdx.x % kCodTile, kvh = blockIdx.y;
-  if (p >= s.cap) return;
-  const int4 m = a.plan.order[s.off + p];
-  const int64_t row = s.off + m.x;
-  float dk[HD], dv[HD];
-  for (int d = 0; d < HD; ++d) dk[d] = dv[d] = 0.f;
-  if (p < s.len) {
-    const auto* k = at<E>(a.k, row, kvh);
-    const auto* v = at<E>(a.v, row, kvh);
-    const int end = m.x < s.n_real ? s.len : m.w;
-    for (int h = kvh * a.group; h < (kvh + 1) * a.group; ++h)
-      for (int i = p + threadIdx.x; i < end; i += 64) {
-        const int64_t qr = s.off + a.plan.order[s.off + i].x;
-        const auto* q = at<E>(a.q, qr, h);
-        const auto* go = at<E>(a.d_out, qr, h);
-        const float w = expf(a.scale * dot<HD, E>(q, k) - a.lse[h * a.rows + qr]);
-        const float ds = w * (dot<HD, E>(go, v) - a.delta[h * a.rows + qr]) * a.scale;
-        for (int d = 0; d < HD; ++d) {
-          dv[d] += w * E::load(go[d]);
-          dk[d] += ds * E::load(q[d]);
-        }
-      }
-  }
-  for (int d = 0; d < HD; ++d) {
-    const float x = wave_sum(dk[d]), y = wave_sum(dv[d]);
-    if (threadIdx.x == 0) {
-      at_out<E>(a.dk, row, kvh)[d] = E::store(x);
-      at_out<E>(a.dv, row, kvh)[d] = E::store(y);
+  if (__any(raise)) {                                // uniform
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      const float mr = max4g(mx[t]);
+      const float m_new = mr > m[t] + kLazy ? mr : m[t];
+      const float corr = __builtin_amdgcn_exp2f(m[t] - m_new);
+      m[t] = m_new;
+      l[t] *= corr;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[t][db] *= corr;
     }
   }
+#pragma unroll
+  for (int t = 0; t < NQ; ++t)
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][kb][i], scale2, -m[t]));
+        l[t] += p[i];
+      }
+      pf[t][kb >> 1][(kb & 1) * 2] = M::pack(p[0], p[1]);
+      pf[t][kb >> 1][(kb & 1) * 2 + 1] = M::pack(p[2], p[3]);
+    }
 }
 
-template <int HD, class E>
-hipError_t launch_fwd(const CodAttnArgs& a, hipStream_t st) {
-  k_fwd<HD, E><<<dim3(a.n_tiles * kCodTile, a.n_heads), 64, 0, st>>>(a);
-  return hipGetLastError();
+template <int HD, int NQ, class M>
+__global__ __launch_bounds__(256, 2) void k_cod_attn(const CodAttnArgs a) {
+  constexpr int QW = 16 * NQ;                        // pairs per wavefront
+  constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
+  // a stage: four blocks of K, four of V; two arrays of their own (the
+  // compiler's waits before an LDS read cover the loads into that array only)
+  __shared__ __attribute__((aligned(16))) u32x4 b0[8 * BU], b1[8 * BU];
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = a.group, per_tile = kCodTile / (64 * NQ) * group;   // workgroups of a tile and key head
+  const int kvh = blockIdx.x % a.n_kv, rest = blockIdx.x / a.n_kv;
+  const int2 tile = a.plan.tiles[rest / per_tile];
+  const CodSampleInfo s = a.plan.samples[tile.x];
+  const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.y * kCodTile;
+  if (p0 + pair0 / group >= s.cap) return;           // uniform: the whole block leaves
+  const int4* const order = a.plan.order + s.off;
+  const int last = s.len - 1;
+
+  // this lane's pairs (those past the sample repeat its last row and are not stored)
+  int row[NQ], pos[NQ], seen[NQ], chain[NQ];         // place, place as read, real tokens seen, first mask row seen
+  u32x4 q[NQ][KS];
+  float m[NQ], l[NQ];
+  f32x4 o[NQ][DB];
+  const uint32_t sign = scale_sign(a.scale);
+  int n_st = 0;
+  if (last >= p0 + pair0 / group) {                  // uniform: the block has rows
+    n_st = (order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y + kStageKeys - 1) / kStageKeys;
+  }
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
+    row[t] = p0 + pair / group;
+    pos[t] = min(row[t], last);
+    m[t] = -1e30f;
+    l[t] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (n_st == 0) continue;                         // uniform
+    const int4 e = order[pos[t]];
+    seen[t] = e.y;
+    chain[t] = e.z;
+    const char* src = at(a.q, s.off + e.x, head) + g4 * 16;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      q[t][ks] = *reinterpret_cast<const u32x4*>(src + ks * 64);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[t][ks][i] ^= sign;
+    }
+  }
+  if (n_st > 0) {                                    // uniform
+    const float scale2 = base2_scale(a.scale);
+    // this wavefront's 16 keys of every stage (past the real tokens: the last one)
+    const int64_t k_step = 2 * a.k.rs, v_step = 2 * a.v.rs;
+    const char* const k0 = at(a.k, s.off, kvh) + block_byte(lane);
+    const char* const v0 = at(a.v, s.off, kvh) + block_byte(lane);
+    auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
+      const int key = min(st * kStageKeys + wave * 16 + block_row(lane), s.n_real - 1);
+      load_block<HD>(k0 + key * k_step, buf + wave * BU);
+      load_block<HD>(v0 + key * v_step, buf + (4 + wave) * BU);
+    };
+    load(b0, 0);
+
+    const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
+    const int first_seen = __builtin_amdgcn_readfirstlane(seen[0]);          // of this wavefront's pairs
+    const int last_seen = p0 + (pair0 + wave * QW) / group > last ? 0 : order[w_last].y;
+    // the wavefront's chains
+    const int chain0 = __builtin_amdgcn_readfirstlane(chain[0]);
+    u32x4* const mine = b1 + wave * 2 * BU;
+    for (int c0 = chain0; c0 <= w_last && last_seen > 0; c0 += 32) {         // uniform
+#pragma unroll
+      for (int hb = 0; hb < 2; ++hb) {
+        const int kp = min(c0 + hb * 16 + block_row(lane), last);
+        load_block<HD>(v0 + order[kp].x * v_step, mine + hb * BU);
+      }
+      f32x4 sc[NQ][2];
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const char* src = at(a.k, s.off + order[min(c0 + kb * 16 + c16, last)].x, kvh) + g4 * 16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(src + ks * 64);
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NQ; ++t)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int kp = c0 + kb * 16 + g4 * 4 + i;
+            if (kp < chain[t] || kp > pos[t]) sc[t][kb][i] = -INFINITY;
+          }
+      u32x4 pf[NQ][1];
+      softmax_step<NQ, 2, DB, M>(sc, m, l, o, pf, scale2);
+      wait_all();
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 vf = cols_frag<HD>(mine, db, lane);
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) o[t][db] = M::mma(vf, pf[t][0], o[t][db]);
+      }
+      wait_all();                                    // (its reads are done before the next loads)
+    }
+
+    auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
+      wait_and_meet();
+      if (st + 1 < n_st) load(nxt, st + 1);          // uniform
+      __builtin_amdgcn_sched_barrier(0);
+      const int key0 = st * kStageKeys;
+      if (key0 >= last_seen) return;                 // uniform: past this wavefront's rows
+      f32x4 sc[NQ][4];
+#pragma unroll
+      for (int t = 0; t < NQ; ++t)
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) sc[t][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kf = rows_frag(cur + kb * BU, ks, lane);
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
+        }
+      if (key0 + kStageKeys > first_seen) {          // uniform: around this wavefront's own tokens
+#pragma unroll
+        for (int t = 0; t < NQ; ++t)
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (key0 + kb * 16 + g4 * 4 + i >= seen[t]) sc[t][kb][i] = -INFINITY;
+      }
+      u32x4 pf[NQ][2];
+      softmax_step<NQ, 4, DB, M>(sc, m, l, o, pf, scale2);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const u32x4 vf = cols_frag<HD>(cur + (4 + 2 * tt) * BU, db, lane);
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) o[t][db] = M::mma(vf, pf[t][tt], o[t][db]);
+        }
+    };
+    int st = 0;
+    for (; st + 2 <= n_st; st += 2) {
+      stage(st, b0, b1);
+      stage(st + 1, b1, b0);
+    }
+    if (st < n_st) stage(st, b0, b1);
+  }
+
+  // lane (c16, g4) holds elements 16 db + 4 g4 .. + 3 of pair 16 t + c16
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const float sum = sum4g(l[t]);
+    if (row[t] >= s.cap) continue;
+    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
+    const bool real = row[t] <= last;
+    const int64_t r = s.off + order[row[t]].x;
+    const float inv = real ? 1.0f / sum : 0.f;
+    char* const dst = at(a.out, r, head) + g4 * 8;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const f32x4 v = real ? o[t][db] * inv : f32x4{0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<u32x2*>(dst + db * 32) = u32x2{M::pack(v[0], v[1]), M::pack(v[2], v[3])};
+    }
+    if (a.lse && g4 == 0)
+      a.lse[head * a.rows + r] = real ? (m[t] + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
 }
-template <int HD, class E>
-hipError_t launch_grad(const CodAttnArgs& a, hipStream_t st) {
-  k_dq<HD, E><<<dim3(a.n_tiles * kCodTile, a.n_heads), 64, 0, st>>>(a);
-  k_dkv<HD, E><<<dim3(a.n_tiles * kCodTile, a.n_kv), 64, 0, st>>>(a);
+
+template <int HD, class M>
+hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
+  constexpr int NQ = HD == 128 ? 2 : 1;
+  const int64_t blocks = (int64_t)a.n_tiles * (kCodTile / (64 * NQ)) * a.group * a.n_kv;
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  k_cod_attn<HD, NQ, M><<<(unsigned)blocks, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_cod_attn(int head_dim, int dtype, const CodAttnArgs& a, hipStream_t st) {
-  if (head_dim == 64) return dtype == PARD_BF16 ? launch_fwd<64, ElemBF16>(a, st) : launch_fwd<64, ElemF16>(a, st);
-  return dtype == PARD_BF16 ? launch_fwd<128, ElemBF16>(a, st) : launch_fwd<128, ElemF16>(a, st);
-}
-
-hipError_t launch_cod_attn_grad(int head_dim, int dtype, const CodAttnArgs& a, hipStream_t st) {
-  if (head_dim == 64) return dtype == PARD_BF16 ? launch_grad<64, ElemBF16>(a, st) : launch_grad<64, ElemF16>(a, st);
-  return dtype == PARD_BF16 ? launch_grad<128, ElemBF16>(a, st) : launch_grad<128, ElemF16>(a, st);
+  if (head_dim == 64) return dtype == PARD_BF16 ? launch_hd<64, MmaBF16>(a, st) : launch_hd<64, MmaF16>(a, st);
+  return dtype == PARD_BF16 ? launch_hd<128, MmaBF16>(a, st) : launch_hd<128, MmaF16>(a, st);
 }
 
 }  // namespace pard
