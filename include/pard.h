@@ -449,7 +449,7 @@ pard_status pard_qk_rope_grad(const pard_rope_args *args, const pard_heads *q_dy
  * refers to it.  The call waits for its result, so it cannot be captured.
  * Errors: ARG (null pointer, misaligned plan_data, n_samples < 1, offsets
  * negative or descending, rows not in the form above: then *plan is not set),
- * UNSUPPORTED (2^31 rows or more), NOMEM (plan_bytes too small), DEVICE. */
+ * UNSUPPORTED (2^31 rows or more, a region above 2^19), NOMEM (plan_bytes too small), DEVICE. */
 typedef struct {
   int64_t rows;                    /* out_offsets[n_samples] */
   int32_t n_samples, n_tiles;
@@ -475,7 +475,8 @@ pard_status pard_cod_plan_build(const int32_t *section, const int32_t *column, c
  * Errors: ARG (null pointer, a plan that was not built, head counts < 1,
  * n_heads not a multiple of n_kv_heads, scale not finite, data not 16-byte
  * aligned, strides not multiples of 8 elements or below head_dim), UNSUPPORTED
- * (head_dim not 64 or 128, dtype not PARD_BF16 or PARD_F16), DEVICE. */
+ * (head_dim not 64 or 128, dtype not PARD_BF16 or PARD_F16, n_heads above
+ * 65535 or 1024 n_kv_heads), DEVICE. */
 typedef struct {
   const pard_cod_plan *plan;
   int32_t n_heads, n_kv_heads, head_dim, dtype;

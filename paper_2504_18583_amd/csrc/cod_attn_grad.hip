@@ -1,119 +1,452 @@
-// Gradient of attention over packed COD rows.
-#include "train.h"
+// Gradient of attention over packed COD rows on gfx950 MFMA: with P = exp(scale
+// Q K^T - lse) over the pairs of rows that see each other,
+//   dV = P^T dO,  dS = P (dO V^T - delta),  delta = rowsum(dO O),
+//   dQ = scale dS K,  dK = scale dS^T Q.
+//
+// Two launches, no atomics, so that every sum has one order:
+//   k_cod_dq  as the forward kernel: a workgroup owns 64 NQ (row, head) pairs of
+//     a key head and walks their keys.  It also leaves lse, delta, the real
+//     tokens seen and the place of every pair, in pair order, for the other.
+//   k_cod_dkv  a workgroup owns 64 NK real tokens of a key head (K and V in
+//     operand registers) and walks the pairs that see them, all heads of the
+//     group, in stages of 64 through LDS.  Mask rows are seen by the rows of
+//     their chain alone: workgroups behind those take 64 places of the order,
+//     16 a wavefront, each with the few pairs from its first place to its last
+//     chain's end.
+#include "cod_attn_tile.h"
+
+#include <algorithm>
 
 namespace pard {
 namespace {
 
-__device__ __forceinline__ float wave_sum(float x) {
+using namespace cod;
+
+constexpr int kStage = 64;                           // keys (dq) or pairs (dkv) of a stage
+
+// Statistics of 64 pairs of one key head: base-2 log-sum (+infinity past the
+// sample: probability 0), delta, real tokens seen, place in the order.
+struct PairStats {
+  float lse2[64], delta[64];
+  int seen[64], pos[64];
+};
+static_assert(sizeof(PairStats) == 1024, "one LDS-DMA load");
+
+// First block of 64 pairs of a sample (every sample has blocks of its own).
+__device__ __forceinline__ int64_t stats_base(const CodAttnArgs& a, int64_t off, int sample) {
+  return off * a.group / 64 + sample;
+}
+__host__ __device__ inline int64_t stats_blocks(int64_t rows, int group, int n_samples) {
+  return rows * group / 64 + n_samples + 1;          // of one key head
+}
+
+template <int HD, int NQ, class M>
+__global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
+  constexpr int QW = 16 * NQ;                        // pairs per wavefront
+  constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
+  __shared__ __attribute__((aligned(16))) u32x4 b0[8 * BU], b1[8 * BU];
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = a.group, per_tile = kCodTile / (64 * NQ) * group;
+  const int kvh = blockIdx.x % a.n_kv, rest = blockIdx.x / a.n_kv;
+  const int2 tile = a.plan.tiles[rest / per_tile];
+  const CodSampleInfo s = a.plan.samples[tile.x];
+  const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.y * kCodTile;
+  if (p0 + pair0 / group >= s.cap) return;           // uniform
+  const int4* const order = a.plan.order + s.off;
+  const int last = s.len - 1;
+  const int n_st =
+      last >= p0 + pair0 / group
+          ? (order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y + kStage - 1) / kStage : 0;
+
+  int row[NQ], pos[NQ], seen[NQ], chain[NQ];
+  float lse2[NQ], delta[NQ];
+  u32x4 q[NQ][KS], go[NQ][KS];
+  f32x4 dq[NQ][DB];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
-  return x;
-}
-
-template <class E>
-__device__ __forceinline__ const typename E::T* at(const Heads& h, int64_t row, int head) {
-  return reinterpret_cast<const typename E::T*>(h.data) + row * h.rs + head * h.hs;
-}
-template <class E>
-__device__ __forceinline__ typename E::T* at_out(const Heads& h, int64_t row, int head) {
-  return reinterpret_cast<typename E::T*>(h.data) + row * h.rs + head * h.hs;
-}
-
-template <int HD, class E>
-__device__ __forceinline__ float dot(const typename E::T* a, const typename E::T* b) {
-  float s = 0.f;
-  for (int d = 0; d < HD; ++d) s += E::load(a[d]) * E::load(b[d]);
-  return s;
-}
-
-// Calls f(row) for this lane's share of the rows that order entry m (at
-// position p) attends to.
-template <class F>
-__device__ __forceinline__ void keys_of(const CodPlanView& v, int off, int4 m, int p, F&& f) {
-  const int lane = threadIdx.x;
-  for (int t = lane; t < m.y; t += 64) f(t);
-  for (int b = m.z + lane; b <= p && b < m.w; b += 64) f(v.order[off + b].x);
-}
-
-template <int HD, class E>
-__global__ __launch_bounds__(64) void k_dq(const CodAttnArgs a) {
-  const int2 tile = a.plan.tiles[blockIdx.x / kCodTile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int p = tile.y * kCodTile + blockIdx.x % kCodTile, h = blockIdx.y;
-  if (p >= s.cap) return;
-  const int4 m = a.plan.order[s.off + p];
-  const int64_t row = s.off + m.x;
-  const int kvh = h / a.group;
-  float acc[HD];
-  for (int d = 0; d < HD; ++d) acc[d] = 0.f;
-  if (p < s.len) {
-    const auto* q = at<E>(a.q, row, h);
-    const auto* go = at<E>(a.d_out, row, h);
-    const float delta = dot<HD, E>(go, at<E>(a.out, row, h)), lse = a.lse[h * a.rows + row];
-    if (threadIdx.x == 0) a.delta[h * a.rows + row] = delta;
-    keys_of(a.plan, s.off, m, p, [&](int key) {
-      const auto* k = at<E>(a.k, s.off + key, kvh);
-      const float w = expf(a.scale * dot<HD, E>(q, k) - lse);
-      const float ds = w * (dot<HD, E>(go, at<E>(a.v, s.off + key, kvh)) - delta) * a.scale;
-      for (int d = 0; d < HD; ++d) acc[d] += ds * E::load(k[d]);
-    });
+  for (int t = 0; t < NQ; ++t) {
+    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
+    row[t] = p0 + pair / group;
+    pos[t] = min(row[t], last);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) dq[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (n_st == 0) continue;                         // uniform
+    const int4 e = order[pos[t]];
+    const int64_t r = s.off + e.x;
+    seen[t] = e.y;
+    chain[t] = e.z;
+    lse2[t] = a.lse[head * a.rows + r] * kLog2e;
+    const char* const qs = at(a.q, r, head) + g4 * 16;
+    const char* const gs = at(a.d_out, r, head) + g4 * 16;
+    const char* const os = at(a.out, r, head) + g4 * 16;
+    float sum = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      q[t][ks] = *reinterpret_cast<const u32x4*>(qs + ks * 64);
+      go[t][ks] = *reinterpret_cast<const u32x4*>(gs + ks * 64);
+      const u32x4 ov = *reinterpret_cast<const u32x4*>(os + ks * 64);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 x = M::unpack(go[t][ks][i]), y = M::unpack(ov[i]);
+        sum = fmaf(x[0], y[0], sum);
+        sum = fmaf(x[1], y[1], sum);
+      }
+    }
+    delta[t] = sum4g(sum);
+    const int64_t in_sample = (int64_t)p0 * group + pair;
+    if (g4 == 0 && (in_sample & ~63) < (int64_t)s.len * group) {
+      const bool real = row[t] <= last;
+      PairStats& st = reinterpret_cast<PairStats*>(a.stats)[kvh * a.stats_blocks + stats_base(a, s.off, tile.x) + in_sample / 64];
+      const int i = (int)(in_sample & 63);
+      st.lse2[i] = real ? lse2[t] : INFINITY;
+      st.delta[i] = delta[t];
+      st.seen[i] = seen[t];
+      st.pos[i] = pos[t];
+    }
   }
-  for (int d = 0; d < HD; ++d) {
-    const float o = wave_sum(acc[d]);
-    if (threadIdx.x == 0) at_out<E>(a.dq, row, h)[d] = E::store(o);
-  }
-}
+  if (n_st > 0) {                                    // uniform
+    const float scale2 = a.scale * kLog2e;
+    const int64_t k_step = 2 * a.k.rs, v_step = 2 * a.v.rs;
+    const char* const k0 = at(a.k, s.off, kvh);
+    const char* const v0 = at(a.v, s.off, kvh);
+    auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
+      const int key = min(st * kStage + wave * 16 + block_row(lane), s.n_real - 1);
+      load_block<HD>(k0 + key * k_step + block_byte(lane), buf + wave * BU);
+      load_block<HD>(v0 + key * v_step + block_byte(lane), buf + (4 + wave) * BU);
+    };
+    load(b0, 0);
+    const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
+    const int first_seen = __builtin_amdgcn_readfirstlane(seen[0]);
+    const int last_seen = p0 + (pair0 + wave * QW) / group > last ? 0 : order[w_last].y;
 
-// One wavefront per (order position, key head): its key's queries are the
-// later positions (real token) or those of its chain (mask row).
-template <int HD, class E>
-__global__ __launch_bounds__(64) void k_dkv(const CodAttnArgs a) {
-  const int2 tile = a.plan.tiles[blockIdx.x / kCodTile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int p = tile.y * kCodTile + blockIdx.x % kCodTile, kvh = blockIdx.y;
-  if (p >= s.cap) return;
-  const int4 m = a.plan.order[s.off + p];
-  const int64_t row = s.off + m.x;
-  float dk[HD], dv[HD];
-  for (int d = 0; d < HD; ++d) dk[d] = dv[d] = 0.f;
-  if (p < s.len) {
-    const auto* k = at<E>(a.k, row, kvh);
-    const auto* v = at<E>(a.v, row, kvh);
-    const int end = m.x < s.n_real ? s.len : m.w;
-    for (int h = kvh * a.group; h < (kvh + 1) * a.group; ++h)
-      for (int i = p + threadIdx.x; i < end; i += 64) {
-        const int64_t qr = s.off + a.plan.order[s.off + i].x;
-        const auto* q = at<E>(a.q, qr, h);
-        const auto* go = at<E>(a.d_out, qr, h);
-        const float w = expf(a.scale * dot<HD, E>(q, k) - a.lse[h * a.rows + qr]);
-        const float ds = w * (dot<HD, E>(go, v) - a.delta[h * a.rows + qr]) * a.scale;
-        for (int d = 0; d < HD; ++d) {
-          dv[d] += w * E::load(go[d]);
-          dk[d] += ds * E::load(q[d]);
+    // dQ += dS K over 32 keys: their scores and dO V^T products are in sc and
+    // dp, K in two LDS blocks; hidden(t, kb, i): key kb * 16 + 4 g4 + i
+    auto add = [&](f32x4 (&sc)[NQ][2], f32x4 (&dp)[NQ][2], const u32x4* kblocks, bool masked, auto hidden)
+                   __attribute__((always_inline)) {
+      u32x4 ds[NQ];
+#pragma unroll
+      for (int t = 0; t < NQ; ++t)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          float x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[t][kb][i], scale2, -lse2[t]));
+          if (masked) {                              // uniform
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = hidden(t, kb, i) ? 0.f : x[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] *= dp[t][kb][i] - delta[t];
+          ds[t][kb * 2] = M::pack(x[0], x[1]);
+          ds[t][kb * 2 + 1] = M::pack(x[2], x[3]);
+        }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 kf = cols_frag<HD>(kblocks, db, lane);
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) dq[t][db] = M::mma(kf, ds[t], dq[t][db]);
+      }
+    };
+
+    // the wavefront's chains
+    const int chain0 = __builtin_amdgcn_readfirstlane(chain[0]);
+    u32x4* const mine = b1 + wave * 2 * BU;
+    for (int c0 = chain0; c0 <= w_last && last_seen > 0; c0 += 32) {   // uniform
+#pragma unroll
+      for (int hb = 0; hb < 2; ++hb)
+        load_block<HD>(k0 + order[min(c0 + hb * 16 + block_row(lane), last)].x * k_step + block_byte(lane), mine + hb * BU);
+      f32x4 sc[NQ][2], dp[NQ][2];
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = dp[t][0] = dp[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const char* const src = v0 + order[min(c0 + kb * 16 + c16, last)].x * v_step + g4 * 16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 vf = *reinterpret_cast<const u32x4*>(src + ks * 64);
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) dp[t][kb] = M::mma(vf, go[t][ks], dp[t][kb]);
         }
       }
+      wait_all();
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kf = rows_frag(mine + kb * BU, ks, lane);
+#pragma unroll
+          for (int t = 0; t < NQ; ++t) sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
+        }
+      add(sc, dp, mine, true, [&](int t, int kb, int i) {
+        const int kp = c0 + kb * 16 + g4 * 4 + i;
+        return kp < chain[t] || kp > pos[t];
+      });
+      wait_all();                                    // (its reads are done before the next loads)
+    }
+
+    auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
+      wait_and_meet();
+      if (st + 1 < n_st) load(nxt, st + 1);          // uniform
+      __builtin_amdgcn_sched_barrier(0);
+      const int key0 = st * kStage;
+      if (key0 >= last_seen) return;                 // uniform
+      const bool masked = key0 + kStage > first_seen;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        f32x4 sc[NQ][2], dp[NQ][2];
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = dp[t][0] = dp[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const u32x4 kf = rows_frag(cur + (2 * hh + kb) * BU, ks, lane);
+            const u32x4 vf = rows_frag(cur + (4 + 2 * hh + kb) * BU, ks, lane);
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+              sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
+              dp[t][kb] = M::mma(vf, go[t][ks], dp[t][kb]);
+            }
+          }
+        add(sc, dp, cur + 2 * hh * BU, masked,
+            [&](int t, int kb, int i) { return key0 + hh * 32 + kb * 16 + g4 * 4 + i >= seen[t]; });
+      }
+    };
+    int st = 0;
+    for (; st + 2 <= n_st; st += 2) {
+      stage(st, b0, b1);
+      stage(st + 1, b1, b0);
+    }
+    if (st < n_st) stage(st, b0, b1);
   }
-  for (int d = 0; d < HD; ++d) {
-    const float x = wave_sum(dk[d]), y = wave_sum(dv[d]);
-    if (threadIdx.x == 0) {
-      at_out<E>(a.dk, row, kvh)[d] = E::store(x);
-      at_out<E>(a.dv, row, kvh)[d] = E::store(y);
+
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    if (row[t] >= s.cap) continue;
+    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
+    char* const dst = at(a.dq, s.off + order[row[t]].x, head) + g4 * 8;
+    const bool real = row[t] <= last;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const f32x4 v = real ? dq[t][db] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<u32x2*>(dst + db * 32) = u32x2{M::pack(v[0], v[1]), M::pack(v[2], v[3])};
     }
   }
 }
 
-template <int HD, class E>
-hipError_t launch_grad(const CodAttnArgs& a, hipStream_t st) {
-  k_dq<HD, E><<<dim3(a.n_tiles * kCodTile, a.n_heads), 64, 0, st>>>(a);
-  k_dkv<HD, E><<<dim3(a.n_tiles * kCodTile, a.n_kv), 64, 0, st>>>(a);
+// dK and dV of NK blocks of 16 keys (operands kf, vf) over 32 pairs in two LDS
+// blocks each of Q and dO, statistics st from pair 32 h on.
+template <int HD, int NK, class M, class H>
+__device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const PairStats& st, int h,
+                                         const u32x4 (&kf)[NK][HD / 32], const u32x4 (&vf)[NK][HD / 32],
+                                         f32x4 (&dk)[NK][HD / 16], f32x4 (&dv)[NK][HD / 16], float scale2, int lane,
+                                         bool masked, H&& hidden) {
+  constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
+  const int g4 = lane >> 4;
+  u32x4 p[NK], ds[NK];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    f32x4 sc[NK], dp[NK];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) sc[k] = dp[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4 qf = rows_frag(qb + b * BU, ks, lane), gf = rows_frag(gb + b * BU, ks, lane);
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        sc[k] = M::mma(qf, kf[k][ks], sc[k]);
+        dp[k] = M::mma(gf, vf[k][ks], dp[k]);
+      }
+    }
+    const int i0 = h * 32 + b * 16 + g4 * 4;         // this lane's four pairs
+    const f32x4 lse2 = *reinterpret_cast<const f32x4*>(st.lse2 + i0), delta = *reinterpret_cast<const f32x4*>(st.delta + i0);
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      float x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[k][i], scale2, -lse2[i]));
+      if (masked) {                                  // uniform
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = hidden(k, i0 + i) ? 0.f : x[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = x[i] * (dp[k][i] - delta[i]);
+      p[k][b * 2] = M::pack(x[0], x[1]);
+      p[k][b * 2 + 1] = M::pack(x[2], x[3]);
+      ds[k][b * 2] = M::pack(y[0], y[1]);
+      ds[k][b * 2 + 1] = M::pack(y[2], y[3]);
+    }
+  }
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    const u32x4 gc = cols_frag<HD>(gb, db, lane), qc = cols_frag<HD>(qb, db, lane);
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      dv[k][db] = M::mma(gc, p[k], dv[k][db]);
+      dk[k][db] = M::mma(qc, ds[k], dk[k][db]);
+    }
+  }
+}
+
+// A lane's 4 elements of every 16 of one row of dK and dV.
+template <int HD, class M>
+__device__ __forceinline__ void store_dkv(const CodAttnArgs& a, int64_t row, int kvh, const f32x4 (&dk)[HD / 16],
+                                          const f32x4 (&dv)[HD / 16], int g4) {
+  char* const ks = at(a.dk, row, kvh) + g4 * 8;
+  char* const vs = at(a.dv, row, kvh) + g4 * 8;
+#pragma unroll
+  for (int db = 0; db < HD / 16; ++db) {
+    const f32x4 x = dk[db] * a.scale, y = dv[db];
+    *reinterpret_cast<u32x2*>(ks + db * 32) = u32x2{M::pack(x[0], x[1]), M::pack(x[2], x[3])};
+    *reinterpret_cast<u32x2*>(vs + db * 32) = u32x2{M::pack(y[0], y[1]), M::pack(y[2], y[3])};
+  }
+}
+
+template <int HD, int NK, class M>
+__global__ __launch_bounds__(256, 2) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
+  constexpr int KW = 16 * NK;                        // keys per wavefront
+  constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
+  // a stage: four blocks of Q, four of dO, the pairs' statistics
+  __shared__ __attribute__((aligned(16))) u32x4 b0[8 * BU + 64], b1[8 * BU + 64];
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = a.group;
+  const float scale2 = a.scale * kLog2e;
+  const bool real = blockIdx.x < real_blocks;        // uniform
+  const unsigned id = real ? blockIdx.x : blockIdx.x - real_blocks;
+  const int keys = real ? 4 * KW : 64, per_tile = kCodTile / keys;
+  const int kvh = id % a.n_kv, rest = id / a.n_kv;
+  // (early real tokens are seen by the most rows: the list from its end)
+  const int2 tile = a.plan.tiles[real ? a.n_tiles - 1 - rest / per_tile : rest / per_tile];
+  const CodSampleInfo s = a.plan.samples[tile.x];
+  const int4* const order = a.plan.order + s.off;
+  const int last = s.len - 1, n_pairs = s.len * group;
+  const int t0 = tile.y * kCodTile + (rest % per_tile) * keys;
+  const PairStats* const stats = reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.x);
+  // a lane's row of 16 pairs from `pair` on, in the order (past the sample: its last row)
+  auto place = [&](int pair) { return min((pair + block_row(lane)) / group, last); };
+  auto load_pairs = [&](int pair, int packed, u32x4* qb, u32x4* gb) __attribute__((always_inline)) {
+    const int head = kvh * group + (pair + block_row(lane)) % group;
+    load_block<HD>(at(a.q, s.off + packed, head) + block_byte(lane), qb);
+    load_block<HD>(at(a.d_out, s.off + packed, head) + block_byte(lane), gb);
+  };
+  if (real) {
+    if (t0 >= s.n_real) return;                      // uniform
+    u32x4 kf[NK][KS], vf[NK][KS];
+    f32x4 dk[NK][DB], dv[NK][DB];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const int key = min(t0 + wave * KW + k * 16 + c16, s.n_real - 1);
+      const char* const ks_ = at(a.k, s.off + key, kvh) + g4 * 16;
+      const char* const vs_ = at(a.v, s.off + key, kvh) + g4 * 16;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        kf[k][ks] = *reinterpret_cast<const u32x4*>(ks_ + ks * 64);
+        vf[k][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) dk[k][db] = dv[k][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int st0 = a.plan.first[s.off + t0] * group / kStage, st1 = (n_pairs + kStage - 1) / kStage;
+    const int w0 = t0 + wave * KW;                   // this wavefront's first key
+    int packed = order[place(st0 * kStage + wave * 16)].x;   // of the next stage to load
+    auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
+      load_pairs(st * kStage + wave * 16, packed, buf + wave * BU, buf + (4 + wave) * BU);
+      if (wave == 0)
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st) + lane * 16),
+            (__attribute__((address_space(3))) void*)(buf + 8 * BU), 16, 0, 0);
+      packed = order[place((st + 1) * kStage + wave * 16)].x;
+    };
+    load(b0, st0);
+    auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
+      wait_and_meet();
+      if (st + 1 < st1) load(nxt, st + 1);           // uniform
+      __builtin_amdgcn_sched_barrier(0);
+      const PairStats& ps = *reinterpret_cast<const PairStats*>(cur + 8 * BU);
+      const int lo = __builtin_amdgcn_readfirstlane(ps.seen[0]), hi = __builtin_amdgcn_readfirstlane(ps.seen[63]);
+      if (hi <= w0) return;                          // uniform: no pair sees this wavefront's keys
+      const bool masked = lo < w0 + KW;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (4 + 2 * h) * BU, ps, h, kf, vf, dk, dv, scale2, lane, masked,
+                            [&](int k, int i) { return ps.seen[i] <= w0 + k * 16 + c16; });
+    };
+    int st = st0;
+    for (; st + 2 <= st1; st += 2) {
+      stage(st, b0, b1);
+      stage(st + 1, b1, b0);
+    }
+    if (st < st1) stage(st, b0, b1);
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const int key = w0 + k * 16 + c16;
+      if (key < s.n_real) store_dkv<HD, M>(a, s.off + key, kvh, dk[k], dv[k], g4);
+    }
+    return;
+  }
+
+  // mask rows (and padding): this wavefront's 16 places
+  const int w0 = t0 + wave * 16, mine = w0 + c16;
+  if (w0 >= s.cap) return;                           // (no barrier below)
+  const int4 e = order[min(mine, s.cap - 1)];
+  const bool branch = mine <= last && e.x >= s.n_real;
+  u32x4 kf[1][KS], vf[1][KS];
+  f32x4 dk[1][DB], dv[1][DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dk[0][db] = dv[0][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (w0 <= last) {                                  // uniform
+    const int4 el = order[min(mine, last)];
+    const char* const ks_ = at(a.k, s.off + el.x, kvh) + g4 * 16;
+    const char* const vs_ = at(a.v, s.off + el.x, kvh) + g4 * 16;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[0][ks] = *reinterpret_cast<const u32x4*>(ks_ + ks * 64);
+      vf[0][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
+    }
+    const int end = order[min(w0 + 15, last)].w * group;
+    u32x4* const qb = (wave & 2 ? b1 : b0) + (wave & 1) * 4 * BU;
+    for (int c0 = w0 * group / 32 * 32; c0 < end; c0 += 32) {   // uniform
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        load_pairs(c0 + b * 16, order[place(c0 + b * 16)].x, qb + b * BU, qb + (2 + b) * BU);
+      wait_all();
+      const PairStats& st = stats[c0 / 64];
+      dkv_step<HD, 1, M>(qb, qb + 2 * BU, st, (c0 / 32) & 1, kf, vf, dk, dv, scale2, lane, true,
+                         [&](int, int i) { return !branch || st.pos[i] < mine || st.pos[i] >= e.w; });
+      wait_all();                                    // (its reads are done before the next loads)
+    }
+  }
+  if (mine > last) {                                 // (whatever the sample's rows hold)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) dk[0][db] = dv[0][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (mine < s.cap && (branch || mine > last)) store_dkv<HD, M>(a, s.off + e.x, kvh, dk[0], dv[0], g4);
+}
+
+template <int HD, class M>
+hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
+  constexpr int NQ = HD == 128 ? 2 : 1, NK = HD == 128 ? 1 : 2;
+  const int64_t heads = (int64_t)a.n_tiles * a.n_kv;
+  const int64_t dq = heads * (kCodTile / (64 * NQ)) * a.group;
+  const int64_t real = heads * (kCodTile / (64 * NK)), all = real + heads * (kCodTile / 64);
+  if (dq > 0x7fffffff || all > 0x7fffffff) return hipErrorInvalidValue;
+  k_cod_dq<HD, NQ, M><<<(unsigned)dq, 256, 0, st>>>(a);
+  k_cod_dkv<HD, NK, M><<<(unsigned)all, 256, 0, st>>>(a, (unsigned)real);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cod_attn_grad(int head_dim, int dtype, const CodAttnArgs& a, hipStream_t st) {
-  if (head_dim == 64) return dtype == PARD_BF16 ? launch_grad<64, ElemBF16>(a, st) : launch_grad<64, ElemF16>(a, st);
-  return dtype == PARD_BF16 ? launch_grad<128, ElemBF16>(a, st) : launch_grad<128, ElemF16>(a, st);
+size_t cod_attn_grad_workspace(int64_t rows, int n_samples, int n_kv, int group) {
+  return sizeof(PairStats) * (size_t)stats_blocks(rows, group, n_samples) * n_kv;
+}
+
+hipError_t launch_cod_attn_grad(int head_dim, int dtype, const CodAttnArgs& args, hipStream_t st) {
+  CodAttnArgs a = args;
+  a.stats_blocks = stats_blocks(a.rows, a.group, a.n_samples);
+  if (head_dim == 64) return dtype == PARD_BF16 ? launch_hd<64, MmaBF16>(a, st) : launch_hd<64, MmaF16>(a, st);
+  return dtype == PARD_BF16 ? launch_hd<128, MmaBF16>(a, st) : launch_hd<128, MmaF16>(a, st);
 }
 
 }  // namespace pard

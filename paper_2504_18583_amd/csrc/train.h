@@ -78,14 +78,16 @@ hipError_t launch_cod_plan(const int32_t* section, const int32_t* column, const 
 
 struct CodAttnArgs {
   CodPlanView plan;
-  int n_tiles, n_heads, n_kv, group;
-  int64_t rows;                            // of lse and delta
+  int n_tiles, n_samples, n_heads, n_kv, group;
+  int64_t rows;                            // of lse
   float scale;
   Heads q, k, v, out;
   float* lse;                              // forward: written (may be null); gradient: read
   Heads d_out, dq, dk, dv;
-  float* delta;                            // gradient: row sums of d_out * out, [n_heads][rows]
+  void* stats;                             // gradient: the pairs' statistics (workspace)
+  int64_t stats_blocks;                    // blocks of 64 pairs of a key head
 };
+size_t cod_attn_grad_workspace(int64_t rows, int n_samples, int n_kv, int group);
 hipError_t launch_cod_attn(int head_dim, int dtype, const CodAttnArgs& a, hipStream_t st);
 hipError_t launch_cod_attn_grad(int head_dim, int dtype, const CodAttnArgs& a, hipStream_t st);
 

@@ -79,8 +79,8 @@ pard_status attn_check(const pard_cod_attn_args* a) {
     return PARD_ERR_ARG;
   if ((a->head_dim != 64 && a->head_dim != 128) || (a->dtype != PARD_BF16 && a->dtype != PARD_F16))
     return PARD_ERR_UNSUPPORTED;
-  // (grid: tiles, heads)
-  return a->n_heads > 65535 ? PARD_ERR_UNSUPPORTED : PARD_OK;
+  // (pairs of a sample and key head are numbered in 32 bits)
+  return a->n_heads > 65535 || a->n_heads / a->n_kv_heads > 1024 ? PARD_ERR_UNSUPPORTED : PARD_OK;
 }
 
 // The kernels read and write 16 bytes of a head at a time.
@@ -93,6 +93,7 @@ CodAttnArgs attn_args(const pard_cod_attn_args* a) {
   CodAttnArgs r{};
   cod_plan_layout(a->plan->rows, a->plan->n_samples, const_cast<void*>(a->plan->data), &r.plan);
   r.n_tiles = a->plan->n_tiles;
+  r.n_samples = a->plan->n_samples;
   r.n_heads = a->n_heads;
   r.n_kv = a->n_kv_heads;
   r.group = a->n_heads / a->n_kv_heads;
@@ -241,7 +242,8 @@ pard_status pard_cod_attn(const pard_cod_attn_args* args, const pard_heads* q, c
 
 size_t pard_cod_attn_workspace_bytes(const pard_cod_attn_args* args) {
   if (attn_check(args) != PARD_OK) return 0;
-  return align256(sizeof(float) * (size_t)args->n_heads * args->plan->rows);
+  return cod_attn_grad_workspace(args->plan->rows, args->plan->n_samples, args->n_kv_heads,
+                                 args->n_heads / args->n_kv_heads);
 }
 
 pard_status pard_cod_attn_grad(const pard_cod_attn_args* args, const pard_heads* d_out, const pard_heads* q,
@@ -268,7 +270,7 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args* args, const pard_heads*
   r.dq = view(dq);
   r.dk = view(dk);
   r.dv = view(dv);
-  r.delta = static_cast<float*>(workspace);
+  r.stats = workspace;
   return status_of(launch_cod_attn_grad(args->head_dim, args->dtype, r, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
