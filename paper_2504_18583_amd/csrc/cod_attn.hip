@@ -66,7 +66,7 @@ __device__ __forceinline__ void softmax_step(const f32x4 (&s)[NQ][NB], float (&m
 }
 
 template <int HD, int NQ, class M>
-__global__ __launch_bounds__(256, 2) void k_cod_attn(const CodAttnArgs a) {
+__global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAttnArgs a) {
   constexpr int QW = 16 * NQ;                        // pairs per wavefront
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
   // a stage: four blocks of K, four of V; two arrays of their own (the
@@ -76,90 +76,102 @@ __global__ __launch_bounds__(256, 2) void k_cod_attn(const CodAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = a.group, per_tile = kCodTile / (64 * NQ) * group;   // workgroups of a tile and key head
   const int kvh = blockIdx.x % a.n_kv, rest = blockIdx.x / a.n_kv;
-  const int2 tile = a.plan.tiles[rest / per_tile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.y * kCodTile;
+  const CodTileInfo tile = a.plan.tiles[rest / per_tile];
+  const CodSampleInfo s = tile.s;
+  const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.tile * kCodTile;
   if (p0 + pair0 / group >= s.cap) return;           // uniform: the whole block leaves
   const int4* const order = a.plan.order + s.off;
   const int last = s.len - 1;
 
-  // this lane's pairs (those past the sample repeat its last row and are not stored)
-  int row[NQ], pos[NQ], seen[NQ], chain[NQ];         // place, place as read, real tokens seen, first mask row seen
+  // The places of this lane's pairs (those past the sample repeat its last row
+  // and are not stored) and of the keys before them are read at once, then the
+  // rows they name: two round trips to memory before the first product.
+  const int w_row0 = p0 + (pair0 + wave * QW) / group;             // of this wavefront's pairs
+  const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
+  const int chain0 = max(w_row0 - s.reach, 0);
+  int row[NQ];                                       // this pair's place
+  int4 e[NQ];                                        // packed row, real tokens seen, first mask row seen (and chain's end)
   u32x4 q[NQ][KS];
   float m[NQ], l[NQ];
   f32x4 o[NQ][DB];
-  const uint32_t sign = scale_sign(a.scale);
-  int n_st = 0;
-  if (last >= p0 + pair0 / group) {                  // uniform: the block has rows
-    n_st = (order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y + kStageKeys - 1) / kStageKeys;
-  }
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
-    row[t] = p0 + pair / group;
-    pos[t] = min(row[t], last);
+    row[t] = p0 + (pair0 + wave * QW + t * 16 + c16) / group;
     m[t] = -1e30f;
     l[t] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (n_st == 0) continue;                         // uniform
-    const int4 e = order[pos[t]];
-    seen[t] = e.y;
-    chain[t] = e.z;
-    const char* src = at(a.q, s.off + e.x, head) + g4 * 16;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      q[t][ks] = *reinterpret_cast<const u32x4*>(src + ks * 64);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) q[t][ks][i] ^= sign;
-    }
   }
-  if (n_st > 0) {                                    // uniform
-    const float scale2 = base2_scale(a.scale);
-    // this wavefront's 16 keys of every stage (past the real tokens: the last one)
+  if (last >= p0 + pair0 / group) {                  // uniform: the block has rows
     const int64_t k_step = 2 * a.k.rs, v_step = 2 * a.v.rs;
-    const char* const k0 = at(a.k, s.off, kvh) + block_byte(lane);
-    const char* const v0 = at(a.v, s.off, kvh) + block_byte(lane);
+    const char* const k0 = at(a.k, s.off, kvh);
+    const char* const v0 = at(a.v, s.off, kvh);
+    // this wavefront's 16 keys of every stage (past the real tokens: the last one)
     auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
       const int key = min(st * kStageKeys + wave * 16 + block_row(lane), s.n_real - 1);
-      load_block<HD>(k0 + key * k_step, buf + wave * BU);
-      load_block<HD>(v0 + key * v_step, buf + (4 + wave) * BU);
+      load_block<HD>(k0 + key * k_step + block_byte(lane), buf + wave * BU);
+      load_block<HD>(v0 + key * v_step + block_byte(lane), buf + (4 + wave) * BU);
     };
-    load(b0, 0);
-
-    const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
-    const int first_seen = __builtin_amdgcn_readfirstlane(seen[0]);          // of this wavefront's pairs
-    const int last_seen = p0 + (pair0 + wave * QW) / group > last ? 0 : order[w_last].y;
-    // the wavefront's chains
-    const int chain0 = __builtin_amdgcn_readfirstlane(chain[0]);
-    u32x4* const mine = b1 + wave * 2 * BU;
-    for (int c0 = chain0; c0 <= w_last && last_seen > 0; c0 += 32) {         // uniform
+    const int st_seen = order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y;
+    const int last_seen = w_row0 > last ? 0 : order[w_last].y;
+    int k_row[2], v_row[2];                          // 32 keys from c0 on
+    auto chain_rows = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int hb = 0; hb < 2; ++hb) {
-        const int kp = min(c0 + hb * 16 + block_row(lane), last);
-        load_block<HD>(v0 + order[kp].x * v_step, mine + hb * BU);
+      for (int b = 0; b < 2; ++b) {
+        k_row[b] = order[min(c0 + b * 16 + c16, last)].x;
+        v_row[b] = order[min(c0 + b * 16 + block_row(lane), last)].x;
       }
+    };
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) e[t] = order[min(row[t], last)];
+    chain_rows(chain0);
+    load(b0, 0);
+    const uint32_t sign = scale_sign(a.scale);
+    const float scale2 = base2_scale(a.scale);
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      const int head = kvh * group + (pair0 + wave * QW + t * 16 + c16) % group;
+      const char* src = at(a.q, s.off + e[t].x, head) + g4 * 16;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) q[t][ks] = *reinterpret_cast<const u32x4*>(src + ks * 64);
+    }
+    // the wavefront's chains
+    u32x4* const mine = b1 + wave * 2 * BU;
+    u32x4 kf[2][KS];
+    auto load_chain = [&](int next) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const u32x4*>(k0 + k_row[b] * k_step + g4 * 16 + ks * 64);
+        load_block<HD>(v0 + v_row[b] * v_step + block_byte(lane), mine + b * BU);
+      }
+      if (next <= w_last) chain_rows(next);          // uniform
+    };
+    if (s.reach > 0) load_chain(chain0 + 32);        // uniform
+#pragma unroll
+    for (int t = 0; t < NQ; ++t)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[t][ks][i] ^= sign;
+    for (int c0 = chain0; c0 <= w_last && s.reach > 0; c0 += 32) {           // uniform
       f32x4 sc[NQ][2];
 #pragma unroll
       for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const char* src = at(a.k, s.off + order[min(c0 + kb * 16 + c16, last)].x, kvh) + g4 * 16;
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(src + ks * 64);
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-          for (int t = 0; t < NQ; ++t) sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
-        }
-      }
+          for (int t = 0; t < NQ; ++t) sc[t][b] = M::mma(kf[b][ks], q[t][ks], sc[t][b]);
 #pragma unroll
       for (int t = 0; t < NQ; ++t)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int kp = c0 + kb * 16 + g4 * 4 + i;
-            if (kp < chain[t] || kp > pos[t]) sc[t][kb][i] = -INFINITY;
+            const int kp = c0 + b * 16 + g4 * 4 + i;
+            if (kp < e[t].z || kp > min(row[t], last)) sc[t][b][i] = -INFINITY;
           }
       u32x4 pf[NQ][1];
       softmax_step<NQ, 2, DB, M>(sc, m, l, o, pf, scale2);
@@ -171,8 +183,11 @@ __global__ __launch_bounds__(256, 2) void k_cod_attn(const CodAttnArgs a) {
         for (int t = 0; t < NQ; ++t) o[t][db] = M::mma(vf, pf[t][0], o[t][db]);
       }
       wait_all();                                    // (its reads are done before the next loads)
+      if (c0 + 32 <= w_last) load_chain(c0 + 64);    // uniform
     }
 
+    const int first_seen = __builtin_amdgcn_readfirstlane(e[0].y);           // of this wavefront's pairs
+    const int n_st = (st_seen + kStageKeys - 1) / kStageKeys;
     auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
       wait_and_meet();
       if (st + 1 < n_st) load(nxt, st + 1);          // uniform
@@ -199,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void k_cod_attn(const CodAttnArgs a) {
           for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (key0 + kb * 16 + g4 * 4 + i >= seen[t]) sc[t][kb][i] = -INFINITY;
+              if (key0 + kb * 16 + g4 * 4 + i >= e[t].y) sc[t][kb][i] = -INFINITY;
       }
       u32x4 pf[NQ][2];
       softmax_step<NQ, 4, DB, M>(sc, m, l, o, pf, scale2);
@@ -242,7 +257,7 @@ __global__ __launch_bounds__(256, 2) void k_cod_attn(const CodAttnArgs a) {
 
 template <int HD, class M>
 hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
-  constexpr int NQ = HD == 128 ? 2 : 1;
+  constexpr int NQ = 2;
   const int64_t blocks = (int64_t)a.n_tiles * (kCodTile / (64 * NQ)) * a.group * a.n_kv;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
   k_cod_attn<HD, NQ, M><<<(unsigned)blocks, 256, 0, st>>>(a);

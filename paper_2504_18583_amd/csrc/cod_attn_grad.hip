@@ -49,62 +49,28 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = a.group, per_tile = kCodTile / (64 * NQ) * group;
   const int kvh = blockIdx.x % a.n_kv, rest = blockIdx.x / a.n_kv;
-  const int2 tile = a.plan.tiles[rest / per_tile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
-  const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.y * kCodTile;
+  const CodTileInfo tile = a.plan.tiles[rest / per_tile];
+  const CodSampleInfo s = tile.s;
+  const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.tile * kCodTile;
   if (p0 + pair0 / group >= s.cap) return;           // uniform
   const int4* const order = a.plan.order + s.off;
   const int last = s.len - 1;
-  const int n_st =
-      last >= p0 + pair0 / group
-          ? (order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y + kStage - 1) / kStage : 0;
-
-  int row[NQ], pos[NQ], seen[NQ], chain[NQ];
+  // (as in the forward kernel: the places of all rows read first, then the rows)
+  const int w_row0 = p0 + (pair0 + wave * QW) / group;             // of this wavefront's pairs
+  const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
+  const int chain0 = max(w_row0 - s.reach, 0);
+  int row[NQ];                                       // this pair's place
+  int4 e[NQ];                                        // packed row, real tokens seen, first mask row seen (and chain's end)
   float lse2[NQ], delta[NQ];
   u32x4 q[NQ][KS], go[NQ][KS];
   f32x4 dq[NQ][DB];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
-    row[t] = p0 + pair / group;
-    pos[t] = min(row[t], last);
+    row[t] = p0 + (pair0 + wave * QW + t * 16 + c16) / group;
 #pragma unroll
     for (int db = 0; db < DB; ++db) dq[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (n_st == 0) continue;                         // uniform
-    const int4 e = order[pos[t]];
-    const int64_t r = s.off + e.x;
-    seen[t] = e.y;
-    chain[t] = e.z;
-    lse2[t] = a.lse[head * a.rows + r] * kLog2e;
-    const char* const qs = at(a.q, r, head) + g4 * 16;
-    const char* const gs = at(a.d_out, r, head) + g4 * 16;
-    const char* const os = at(a.out, r, head) + g4 * 16;
-    float sum = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      q[t][ks] = *reinterpret_cast<const u32x4*>(qs + ks * 64);
-      go[t][ks] = *reinterpret_cast<const u32x4*>(gs + ks * 64);
-      const u32x4 ov = *reinterpret_cast<const u32x4*>(os + ks * 64);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x2 x = M::unpack(go[t][ks][i]), y = M::unpack(ov[i]);
-        sum = fmaf(x[0], y[0], sum);
-        sum = fmaf(x[1], y[1], sum);
-      }
-    }
-    delta[t] = sum4g(sum);
-    const int64_t in_sample = (int64_t)p0 * group + pair;
-    if (g4 == 0 && (in_sample & ~63) < (int64_t)s.len * group) {
-      const bool real = row[t] <= last;
-      PairStats& st = reinterpret_cast<PairStats*>(a.stats)[kvh * a.stats_blocks + stats_base(a, s.off, tile.x) + in_sample / 64];
-      const int i = (int)(in_sample & 63);
-      st.lse2[i] = real ? lse2[t] : INFINITY;
-      st.delta[i] = delta[t];
-      st.seen[i] = seen[t];
-      st.pos[i] = pos[t];
-    }
   }
-  if (n_st > 0) {                                    // uniform
+  if (last >= p0 + pair0 / group) {                  // uniform: the block has rows
     const float scale2 = a.scale * kLog2e;
     const int64_t k_step = 2 * a.k.rs, v_step = 2 * a.v.rs;
     const char* const k0 = at(a.k, s.off, kvh);
@@ -114,10 +80,64 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
       load_block<HD>(k0 + key * k_step + block_byte(lane), buf + wave * BU);
       load_block<HD>(v0 + key * v_step + block_byte(lane), buf + (4 + wave) * BU);
     };
+    const int st_seen = order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y;
+    const int last_seen = w_row0 > last ? 0 : order[w_last].y;
+    int k_row[2], v_row[2];                          // 32 keys from c0 on
+    auto chain_rows = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        v_row[b] = order[min(c0 + b * 16 + c16, last)].x;
+        k_row[b] = order[min(c0 + b * 16 + block_row(lane), last)].x;
+      }
+    };
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) e[t] = order[min(row[t], last)];
+    chain_rows(chain0);
     load(b0, 0);
-    const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
-    const int first_seen = __builtin_amdgcn_readfirstlane(seen[0]);
-    const int last_seen = p0 + (pair0 + wave * QW) / group > last ? 0 : order[w_last].y;
+    u32x4* const mine = b1 + wave * 2 * BU;
+    u32x4 vf[2][KS];
+    auto load_chain = [&](int next) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) vf[b][ks] = *reinterpret_cast<const u32x4*>(v0 + v_row[b] * v_step + g4 * 16 + ks * 64);
+        load_block<HD>(k0 + k_row[b] * k_step + block_byte(lane), mine + b * BU);
+      }
+      if (next <= w_last) chain_rows(next);          // uniform
+    };
+    if (s.reach > 0) load_chain(chain0 + 32);        // uniform
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
+      const int64_t r = s.off + e[t].x;
+      const char* const qs = at(a.q, r, head) + g4 * 16;
+      const char* const gs = at(a.d_out, r, head) + g4 * 16;
+      const char* const os = at(a.out, r, head) + g4 * 16;
+      lse2[t] = a.lse[head * a.rows + r] * kLog2e;
+      float sum = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        q[t][ks] = *reinterpret_cast<const u32x4*>(qs + ks * 64);
+        go[t][ks] = *reinterpret_cast<const u32x4*>(gs + ks * 64);
+        const u32x4 ov = *reinterpret_cast<const u32x4*>(os + ks * 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x2 x = M::unpack(go[t][ks][i]), y = M::unpack(ov[i]);
+          sum = fmaf(x[0], y[0], sum);
+          sum = fmaf(x[1], y[1], sum);
+        }
+      }
+      delta[t] = sum4g(sum);
+      const int64_t in_sample = (int64_t)p0 * group + pair;
+      if (g4 == 0 && (in_sample & ~63) < (int64_t)s.len * group) {
+        PairStats& st = reinterpret_cast<PairStats*>(a.stats)[kvh * a.stats_blocks + stats_base(a, s.off, tile.sample) + in_sample / 64];
+        const int i = (int)(in_sample & 63);
+        st.lse2[i] = row[t] <= last ? lse2[t] : INFINITY;
+        st.delta[i] = delta[t];
+        st.seen[i] = e[t].y;
+        st.pos[i] = min(row[t], last);
+      }
+    }
 
     // dQ += dS K over 32 keys: their scores and dO V^T products are in sc and
     // dp, K in two LDS blocks; hidden(t, kb, i): key kb * 16 + 4 g4 + i
@@ -149,25 +169,16 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
     };
 
     // the wavefront's chains
-    const int chain0 = __builtin_amdgcn_readfirstlane(chain[0]);
-    u32x4* const mine = b1 + wave * 2 * BU;
-    for (int c0 = chain0; c0 <= w_last && last_seen > 0; c0 += 32) {   // uniform
-#pragma unroll
-      for (int hb = 0; hb < 2; ++hb)
-        load_block<HD>(k0 + order[min(c0 + hb * 16 + block_row(lane), last)].x * k_step + block_byte(lane), mine + hb * BU);
+    for (int c0 = chain0; c0 <= w_last && s.reach > 0; c0 += 32) {           // uniform
       f32x4 sc[NQ][2], dp[NQ][2];
 #pragma unroll
       for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = dp[t][0] = dp[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const char* const src = v0 + order[min(c0 + kb * 16 + c16, last)].x * v_step + g4 * 16;
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 vf = *reinterpret_cast<const u32x4*>(src + ks * 64);
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-          for (int t = 0; t < NQ; ++t) dp[t][kb] = M::mma(vf, go[t][ks], dp[t][kb]);
-        }
-      }
+          for (int t = 0; t < NQ; ++t) dp[t][kb] = M::mma(vf[kb][ks], go[t][ks], dp[t][kb]);
       wait_all();
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -179,11 +190,14 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
         }
       add(sc, dp, mine, true, [&](int t, int kb, int i) {
         const int kp = c0 + kb * 16 + g4 * 4 + i;
-        return kp < chain[t] || kp > pos[t];
+        return kp < e[t].z || kp > min(row[t], last);
       });
       wait_all();                                    // (its reads are done before the next loads)
+      if (c0 + 32 <= w_last) load_chain(c0 + 64);    // uniform
     }
 
+    const int first_seen = __builtin_amdgcn_readfirstlane(e[0].y);           // of this wavefront's pairs
+    const int n_st = (st_seen + kStage - 1) / kStage;
     auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
       wait_and_meet();
       if (st + 1 < n_st) load(nxt, st + 1);          // uniform
@@ -209,7 +223,7 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
             }
           }
         add(sc, dp, cur + 2 * hh * BU, masked,
-            [&](int t, int kb, int i) { return key0 + hh * 32 + kb * 16 + g4 * 4 + i >= seen[t]; });
+            [&](int t, int kb, int i) { return key0 + hh * 32 + kb * 16 + g4 * 4 + i >= e[t].y; });
       }
     };
     int st = 0;
@@ -317,12 +331,12 @@ __global__ __launch_bounds__(256, 2) void k_cod_dkv(const CodAttnArgs a, unsigne
   const int keys = real ? 4 * KW : 64, per_tile = kCodTile / keys;
   const int kvh = id % a.n_kv, rest = id / a.n_kv;
   // (early real tokens are seen by the most rows: the list from its end)
-  const int2 tile = a.plan.tiles[real ? a.n_tiles - 1 - rest / per_tile : rest / per_tile];
-  const CodSampleInfo s = a.plan.samples[tile.x];
+  const CodTileInfo tile = a.plan.tiles[real ? a.n_tiles - 1 - rest / per_tile : rest / per_tile];
+  const CodSampleInfo s = tile.s;
   const int4* const order = a.plan.order + s.off;
   const int last = s.len - 1, n_pairs = s.len * group;
-  const int t0 = tile.y * kCodTile + (rest % per_tile) * keys;
-  const PairStats* const stats = reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.x);
+  const int t0 = tile.tile * kCodTile + (rest % per_tile) * keys;
+  const PairStats* const stats = reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.sample);
   // a lane's row of 16 pairs from `pair` on, in the order (past the sample: its last row)
   auto place = [&](int pair) { return min((pair + block_row(lane)) / group, last); };
   auto load_pairs = [&](int pair, int packed, u32x4* qb, u32x4* gb) __attribute__((always_inline)) {
@@ -426,7 +440,7 @@ __global__ __launch_bounds__(256, 2) void k_cod_dkv(const CodAttnArgs a, unsigne
 
 template <int HD, class M>
 hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
-  constexpr int NQ = HD == 128 ? 2 : 1, NK = HD == 128 ? 1 : 2;
+  constexpr int NQ = 2, NK = HD == 128 ? 1 : 2;
   const int64_t heads = (int64_t)a.n_tiles * a.n_kv;
   const int64_t dq = heads * (kCodTile / (64 * NQ)) * a.group;
   const int64_t real = heads * (kCodTile / (64 * NK)), all = real + heads * (kCodTile / 64);

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_cod_plan(const int32_t* sectio
     v.order[(size_t)off + p] = int4{r, c + 1, start_s[c] + (int)(m & 1), start_s[c] + __popcll(m)};
     if (k == 1 && r == c) v.first[(size_t)off + c] = start_s[c];
   }
-  if (tid == 0) v.samples[s] = CodSampleInfo{off, len, n_real, cap};
+  if (tid == 0) v.samples[s] = CodSampleInfo{off, len, n_real, cap, len > 0 ? min(max(sec[len - 1], 1), kCodMaxSections) - 1 : 0};
   if (bad) *v.bad = 1;
 }
 
@@ -128,7 +128,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_cod_tiles(int n_samples, int n
   }
   for (int s = tid >> 6; s < n_samples; s += kPlanThreads / 64) {
     const int n = tiles_of(s);
-    for (int l = lane; l < n; l += 64) v.tiles[atomicAdd(&level_s[l], 1)] = int2{s, l};
+    const CodSampleInfo info = v.samples[s];
+    for (int l = lane; l < n; l += 64) v.tiles[atomicAdd(&level_s[l], 1)] = CodTileInfo{info, s, l, 0};
   }
 }
 
@@ -145,14 +146,14 @@ size_t cod_plan_layout(int64_t rows, int n_samples, void* data, CodPlanView* v) 
   char* const order = take((size_t)rows * sizeof(int4));
   char* const first = take((size_t)rows * sizeof(int));
   char* const samples = take((size_t)n_samples * sizeof(CodSampleInfo));
-  char* const tiles = take(((size_t)rows / kCodTile + n_samples) * sizeof(int2));
+  char* const tiles = take(((size_t)rows / kCodTile + n_samples) * sizeof(CodTileInfo));
   char* const offsets = take(((size_t)n_samples + 1) * sizeof(int64_t));
   char* const bad = take(sizeof(int));
   if (v) {
     v->order = reinterpret_cast<int4*>(order);
     v->first = reinterpret_cast<int*>(first);
     v->samples = reinterpret_cast<CodSampleInfo*>(samples);
-    v->tiles = reinterpret_cast<int2*>(tiles);
+    v->tiles = reinterpret_cast<CodTileInfo*>(tiles);
     v->offsets = reinterpret_cast<int64_t*>(offsets);
     v->bad = reinterpret_cast<int*>(bad);
   }

@@ -60,6 +60,11 @@ constexpr int kCodTile = 128;              // order positions of a tile
 constexpr int kCodMaxSections = 64;
 struct CodSampleInfo {
   int off, len, n_real, cap;               // region start, rows, subtask 1's rows, region size
+  int reach;                               // rows of a chain before its last at most (largest subtask - 1)
+};
+struct CodTileInfo {
+  CodSampleInfo s;
+  int sample, tile, pad;
 };
 struct CodPlanView {
   // [off + position]: packed row in the region, real tokens it sees, position
@@ -68,7 +73,7 @@ struct CodPlanView {
   int4* order;
   int* first;                              // [off + real token]: its position
   CodSampleInfo* samples;
-  int2* tiles;                             // (sample, tile), later tiles first
+  CodTileInfo* tiles;                      // later tiles first
   int64_t* offsets;                        // the caller's out_offsets
   int* bad;                                // nonzero: rows not in the documented form
 };
