@@ -474,7 +474,7 @@ pard_status pard_cod_plan_build(const int32_t *section, const int32_t *column, c
  * Results are deterministic.  No output may overlap an input.
  * Errors: ARG (null pointer, a plan that was not built, head counts < 1,
  * n_heads not a multiple of n_kv_heads, scale not finite, data not 16-byte
- * aligned, strides not multiples of 8 elements or below head_dim), UNSUPPORTED
+ * aligned, strides not multiples of 8 elements or above 2^31 - 1), UNSUPPORTED
  * (head_dim not 64 or 128, dtype not PARD_BF16 or PARD_F16, n_heads above
  * 65535 or 1024 n_kv_heads), DEVICE. */
 typedef struct {

@@ -89,28 +89,30 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAtt
   const int w_row0 = p0 + (pair0 + wave * QW) / group;             // of this wavefront's pairs
   const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
   const int chain0 = max(w_row0 - s.reach, 0);
-  int row[NQ];                                       // this pair's place
-  int4 e[NQ];                                        // packed row, real tokens seen, first mask row seen (and chain's end)
+  int row[NQ], head[NQ];                             // this pair's place and query head
+  int4 e[NQ] = {};                                   // packed row, real tokens seen, first mask row seen (and chain's end)
   u32x4 q[NQ][KS];
   float m[NQ], l[NQ];
   f32x4 o[NQ][DB];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    row[t] = p0 + (pair0 + wave * QW + t * 16 + c16) / group;
+    const int pair = pair0 + wave * QW + t * 16 + c16, r = quotient(pair, a.by_group);
+    row[t] = p0 + r;
+    head[t] = kvh * group + remainder(pair, r, a.by_group);
     m[t] = -1e30f;
     l[t] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (last >= p0 + pair0 / group) {                  // uniform: the block has rows
-    const int64_t k_step = 2 * a.k.rs, v_step = 2 * a.v.rs;
+    const uint64_t k_step = a.k.rs, v_step = a.v.rs;
     const char* const k0 = at(a.k, s.off, kvh);
     const char* const v0 = at(a.v, s.off, kvh);
     // this wavefront's 16 keys of every stage (past the real tokens: the last one)
     auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
       const int key = min(st * kStageKeys + wave * 16 + block_row(lane), s.n_real - 1);
-      load_block<HD>(k0 + key * k_step + block_byte(lane), buf + wave * BU);
-      load_block<HD>(v0 + key * v_step + block_byte(lane), buf + (4 + wave) * BU);
+      load_block<HD>(k0 + (uint32_t)key * k_step + block_byte(lane), buf + wave * BU);
+      load_block<HD>(v0 + (uint32_t)key * v_step + block_byte(lane), buf + (4 + wave) * BU);
     };
     const int st_seen = order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y;
     const int last_seen = w_row0 > last ? 0 : order[w_last].y;
@@ -130,8 +132,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAtt
     const float scale2 = base2_scale(a.scale);
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-      const int head = kvh * group + (pair0 + wave * QW + t * 16 + c16) % group;
-      const char* src = at(a.q, s.off + e[t].x, head) + g4 * 16;
+      const char* src = at(a.q, s.off + e[t].x, head[t]) + g4 * 16;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) q[t][ks] = *reinterpret_cast<const u32x4*>(src + ks * 64);
     }
@@ -142,8 +143,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAtt
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const u32x4*>(k0 + k_row[b] * k_step + g4 * 16 + ks * 64);
-        load_block<HD>(v0 + v_row[b] * v_step + block_byte(lane), mine + b * BU);
+        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = *reinterpret_cast<const u32x4*>(k0 + (uint32_t)k_row[b] * k_step + g4 * 16 + ks * 64);
+        load_block<HD>(v0 + (uint32_t)v_row[b] * v_step + block_byte(lane), mine + b * BU);
       }
       if (next <= w_last) chain_rows(next);          // uniform
     };
@@ -154,6 +155,9 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAtt
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[t][ks][i] ^= sign;
+    uint32_t own[NQ];                                // mask rows of its chain that a row sees, itself included
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) own[t] = min(row[t], last) - e[t].z + 1;
     for (int c0 = chain0; c0 <= w_last && s.reach > 0; c0 += 32) {           // uniform
       f32x4 sc[NQ][2];
 #pragma unroll
@@ -170,8 +174,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAtt
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int kp = c0 + b * 16 + g4 * 4 + i;
-            if (kp < e[t].z || kp > min(row[t], last)) sc[t][b][i] = -INFINITY;
+            if ((uint32_t)(c0 + b * 16 + g4 * 4 + i - e[t].z) >= own[t]) sc[t][b][i] = -INFINITY;
           }
       u32x4 pf[NQ][1];
       softmax_step<NQ, 2, DB, M>(sc, m, l, o, pf, scale2);
@@ -240,18 +243,17 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAtt
   for (int t = 0; t < NQ; ++t) {
     const float sum = sum4g(l[t]);
     if (row[t] >= s.cap) continue;
-    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
     const bool real = row[t] <= last;
-    const int64_t r = s.off + order[row[t]].x;
-    const float inv = real ? 1.0f / sum : 0.f;
-    char* const dst = at(a.out, r, head) + g4 * 8;
+    const uint32_t r = s.off + (real ? e[t].x : order[row[t]].x);
+    const float inv = __builtin_amdgcn_rcpf(sum);    // (1 ulp of float32, before the rounding to 16 bits)
+    char* const dst = at(a.out, r, head[t]) + g4 * 8;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const f32x4 v = real ? o[t][db] * inv : f32x4{0.f, 0.f, 0.f, 0.f};
       *reinterpret_cast<u32x2*>(dst + db * 32) = u32x2{M::pack(v[0], v[1]), M::pack(v[2], v[3])};
     }
     if (a.lse && g4 == 0)
-      a.lse[head * a.rows + r] = real ? (m[t] + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+      a.lse[head[t] * a.rows + r] = real ? (m[t] + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
   }
 }
 

@@ -7,12 +7,11 @@
 //   k_cod_dq  as the forward kernel: a workgroup owns 64 NQ (row, head) pairs of
 //     a key head and walks their keys.  It also leaves lse, delta, the real
 //     tokens seen and the place of every pair, in pair order, for the other.
-//   k_cod_dkv  a workgroup owns 64 NK real tokens of a key head (K and V in
-//     operand registers) and walks the pairs that see them, all heads of the
-//     group, in stages of 64 through LDS.  Mask rows are seen by the rows of
-//     their chain alone: workgroups behind those take 64 places of the order,
-//     16 a wavefront, each with the few pairs from its first place to its last
-//     chain's end.
+//   k_cod_dkv  a workgroup owns 128 real tokens of a key head (K and V in operand
+//     registers) and walks the pairs that see them, all heads of the group, in
+//     stages through LDS.  Mask rows are seen by the rows of
+//     their chain alone: workgroups behind those own 128 places of the order and
+//     walk the pairs from the first place to the last chain's end.
 #include "cod_attn_tile.h"
 
 #include <algorithm>
@@ -22,22 +21,22 @@ namespace {
 
 using namespace cod;
 
-constexpr int kStage = 64;                           // keys (dq) or pairs (dkv) of a stage
+constexpr int kStage = 64;                           // keys of a stage (dq)
 
 // Statistics of 64 pairs of one key head: base-2 log-sum (+infinity past the
-// sample: probability 0), delta, real tokens seen, place in the order.
+// sample: probability 0), -delta, real tokens seen, place in the order.
 struct PairStats {
-  float lse2[64], delta[64];
+  float lse2[64], ndelta[64];
   int seen[64], pos[64];
 };
-static_assert(sizeof(PairStats) == 1024, "one LDS-DMA load");
 
 // First block of 64 pairs of a sample (every sample has blocks of its own).
 __device__ __forceinline__ int64_t stats_base(const CodAttnArgs& a, int64_t off, int sample) {
   return off * a.group / 64 + sample;
 }
+// Blocks of one key head; a stage may read one past its sample's.
 __host__ __device__ inline int64_t stats_blocks(int64_t rows, int group, int n_samples) {
-  return rows * group / 64 + n_samples + 1;          // of one key head
+  return rows * group / 64 + n_samples + 2;
 }
 
 template <int HD, int NQ, class M>
@@ -59,26 +58,28 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   const int w_row0 = p0 + (pair0 + wave * QW) / group;             // of this wavefront's pairs
   const int w_last = min(p0 + (pair0 + (wave + 1) * QW - 1) / group, last);
   const int chain0 = max(w_row0 - s.reach, 0);
-  int row[NQ];                                       // this pair's place
-  int4 e[NQ];                                        // packed row, real tokens seen, first mask row seen (and chain's end)
+  int row[NQ], head[NQ];                             // this pair's place and query head
+  int4 e[NQ] = {};                                   // packed row, real tokens seen, first mask row seen (and chain's end)
   float lse2[NQ], delta[NQ];
   u32x4 q[NQ][KS], go[NQ][KS];
   f32x4 dq[NQ][DB];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    row[t] = p0 + (pair0 + wave * QW + t * 16 + c16) / group;
+    const int pair = pair0 + wave * QW + t * 16 + c16, r = quotient(pair, a.by_group);
+    row[t] = p0 + r;
+    head[t] = kvh * group + remainder(pair, r, a.by_group);
 #pragma unroll
     for (int db = 0; db < DB; ++db) dq[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (last >= p0 + pair0 / group) {                  // uniform: the block has rows
     const float scale2 = a.scale * kLog2e;
-    const int64_t k_step = 2 * a.k.rs, v_step = 2 * a.v.rs;
+    const uint64_t k_step = a.k.rs, v_step = a.v.rs;
     const char* const k0 = at(a.k, s.off, kvh);
     const char* const v0 = at(a.v, s.off, kvh);
     auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
       const int key = min(st * kStage + wave * 16 + block_row(lane), s.n_real - 1);
-      load_block<HD>(k0 + key * k_step + block_byte(lane), buf + wave * BU);
-      load_block<HD>(v0 + key * v_step + block_byte(lane), buf + (4 + wave) * BU);
+      load_block<HD>(k0 + (uint32_t)key * k_step + block_byte(lane), buf + wave * BU);
+      load_block<HD>(v0 + (uint32_t)key * v_step + block_byte(lane), buf + (4 + wave) * BU);
     };
     const int st_seen = order[min(p0 + (pair0 + 64 * NQ - 1) / group, last)].y;
     const int last_seen = w_row0 > last ? 0 : order[w_last].y;
@@ -100,20 +101,19 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) vf[b][ks] = *reinterpret_cast<const u32x4*>(v0 + v_row[b] * v_step + g4 * 16 + ks * 64);
-        load_block<HD>(k0 + k_row[b] * k_step + block_byte(lane), mine + b * BU);
+        for (int ks = 0; ks < KS; ++ks) vf[b][ks] = *reinterpret_cast<const u32x4*>(v0 + (uint32_t)v_row[b] * v_step + g4 * 16 + ks * 64);
+        load_block<HD>(k0 + (uint32_t)k_row[b] * k_step + block_byte(lane), mine + b * BU);
       }
       if (next <= w_last) chain_rows(next);          // uniform
     };
     if (s.reach > 0) load_chain(chain0 + 32);        // uniform
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-      const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
-      const int64_t r = s.off + e[t].x;
-      const char* const qs = at(a.q, r, head) + g4 * 16;
-      const char* const gs = at(a.d_out, r, head) + g4 * 16;
-      const char* const os = at(a.out, r, head) + g4 * 16;
-      lse2[t] = a.lse[head * a.rows + r] * kLog2e;
+      const uint32_t r = s.off + e[t].x;
+      const char* const qs = at(a.q, r, head[t]) + g4 * 16;
+      const char* const gs = at(a.d_out, r, head[t]) + g4 * 16;
+      const char* const os = at(a.out, r, head[t]) + g4 * 16;
+      lse2[t] = a.lse[head[t] * a.rows + r] * kLog2e;
       float sum = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -128,12 +128,12 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
         }
       }
       delta[t] = sum4g(sum);
-      const int64_t in_sample = (int64_t)p0 * group + pair;
-      if (g4 == 0 && (in_sample & ~63) < (int64_t)s.len * group) {
+      const int in_sample = p0 * group + pair0 + wave * QW + t * 16 + c16;   // (below 2^30)
+      if (g4 == 0 && (in_sample & ~63) < s.len * group) {
         PairStats& st = reinterpret_cast<PairStats*>(a.stats)[kvh * a.stats_blocks + stats_base(a, s.off, tile.sample) + in_sample / 64];
-        const int i = (int)(in_sample & 63);
+        const int i = in_sample & 63;
         st.lse2[i] = row[t] <= last ? lse2[t] : INFINITY;
-        st.delta[i] = delta[t];
+        st.ndelta[i] = -delta[t];
         st.seen[i] = e[t].y;
         st.pos[i] = min(row[t], last);
       }
@@ -169,6 +169,9 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
     };
 
     // the wavefront's chains
+    uint32_t own[NQ];                                // mask rows of its chain that a row sees, itself included
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) own[t] = min(row[t], last) - e[t].z + 1;
     for (int c0 = chain0; c0 <= w_last && s.reach > 0; c0 += 32) {           // uniform
       f32x4 sc[NQ][2], dp[NQ][2];
 #pragma unroll
@@ -189,8 +192,7 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
           for (int t = 0; t < NQ; ++t) sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
         }
       add(sc, dp, mine, true, [&](int t, int kb, int i) {
-        const int kp = c0 + kb * 16 + g4 * 4 + i;
-        return kp < e[t].z || kp > min(row[t], last);
+        return (uint32_t)(c0 + kb * 16 + g4 * 4 + i - e[t].z) >= own[t];
       });
       wait_all();                                    // (its reads are done before the next loads)
       if (c0 + 32 <= w_last) load_chain(c0 + 64);    // uniform
@@ -237,9 +239,8 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
     if (row[t] >= s.cap) continue;
-    const int pair = pair0 + wave * QW + t * 16 + c16, head = kvh * group + pair % group;
-    char* const dst = at(a.dq, s.off + order[row[t]].x, head) + g4 * 8;
     const bool real = row[t] <= last;
+    char* const dst = at(a.dq, s.off + (real ? e[t].x : order[row[t]].x), head[t]) + g4 * 8;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const f32x4 v = real ? dq[t][db] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -248,47 +249,55 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   }
 }
 
-// dK and dV of NK blocks of 16 keys (operands kf, vf) over 32 pairs in two LDS
-// blocks each of Q and dO, statistics st from pair 32 h on.
-template <int HD, int NK, class M, class H>
-__device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const PairStats& st, int h,
-                                         const u32x4 (&kf)[NK][HD / 32], const u32x4 (&vf)[NK][HD / 32],
-                                         f32x4 (&dk)[NK][HD / 16], f32x4 (&dv)[NK][HD / 16], float scale2, int lane,
-                                         bool masked, H&& hidden) {
+// dK and dV of NK blocks of 16 keys (operands kf and vf(k, ks)) over 32 pairs in
+// two LDS blocks each of Q and dO, the pairs i0 .. of statistics st; if masked,
+// key block k of this lane is hidden from the pairs for whose `by` entry (st.seen
+// or st.pos) hidden(k, entry) holds.  dO V^T starts from -delta.
+template <int HD, int NK, class M, class V, class H>
+__device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const PairStats& st, int i0,
+                                         const u32x4 (&kf)[NK][HD / 32], V&& vf, f32x4 (&dk)[NK][HD / 16],
+                                         f32x4 (&dv)[NK][HD / 16], float scale2, int lane, bool masked, const int* by,
+                                         H&& hidden) {
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
   const int g4 = lane >> 4;
   u32x4 p[NK], ds[NK];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
+    const int i = i0 + b * 16 + g4 * 4;              // this lane's four pairs
+    const f32x4 lse2 = *reinterpret_cast<const f32x4*>(st.lse2 + i);
     f32x4 sc[NK], dp[NK];
 #pragma unroll
-    for (int k = 0; k < NK; ++k) sc[k] = dp[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < NK; ++k) {
+      sc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      dp[k] = *reinterpret_cast<const f32x4*>(st.ndelta + i);
+    }
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const u32x4 qf = rows_frag(qb + b * BU, ks, lane), gf = rows_frag(gb + b * BU, ks, lane);
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
         sc[k] = M::mma(qf, kf[k][ks], sc[k]);
-        dp[k] = M::mma(gf, vf[k][ks], dp[k]);
+        dp[k] = M::mma(gf, vf(k, ks), dp[k]);
       }
     }
-    const int i0 = h * 32 + b * 16 + g4 * 4;         // this lane's four pairs
-    const f32x4 lse2 = *reinterpret_cast<const f32x4*>(st.lse2 + i0), delta = *reinterpret_cast<const f32x4*>(st.delta + i0);
+    float x[NK][4];
+#pragma unroll
+    for (int k = 0; k < NK; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[k][j] = __builtin_amdgcn_exp2f(fmaf(sc[k][j], scale2, -lse2[j]));
+    if (masked) {                                    // uniform
+      const i32x4 entry = *reinterpret_cast<const i32x4*>(by + i);
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[k][j] = hidden(k, entry[j]) ? 0.f : x[k][j];
+    }
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
-      float x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[k][i], scale2, -lse2[i]));
-      if (masked) {                                  // uniform
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = hidden(k, i0 + i) ? 0.f : x[i];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = x[i] * (dp[k][i] - delta[i]);
-      p[k][b * 2] = M::pack(x[0], x[1]);
-      p[k][b * 2 + 1] = M::pack(x[2], x[3]);
-      ds[k][b * 2] = M::pack(y[0], y[1]);
-      ds[k][b * 2 + 1] = M::pack(y[2], y[3]);
+      p[k][b * 2] = M::pack(x[k][0], x[k][1]);
+      p[k][b * 2 + 1] = M::pack(x[k][2], x[k][3]);
+      ds[k][b * 2] = M::pack(x[k][0] * dp[k][0], x[k][1] * dp[k][1]);
+      ds[k][b * 2 + 1] = M::pack(x[k][2] * dp[k][2], x[k][3] * dp[k][3]);
     }
   }
 #pragma unroll
@@ -304,7 +313,7 @@ __device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const
 
 // A lane's 4 elements of every 16 of one row of dK and dV.
 template <int HD, class M>
-__device__ __forceinline__ void store_dkv(const CodAttnArgs& a, int64_t row, int kvh, const f32x4 (&dk)[HD / 16],
+__device__ __forceinline__ void store_dkv(const CodAttnArgs& a, uint32_t row, int kvh, const f32x4 (&dk)[HD / 16],
                                           const f32x4 (&dv)[HD / 16], int g4) {
   char* const ks = at(a.dk, row, kvh) + g4 * 8;
   char* const vs = at(a.dv, row, kvh) + g4 * 8;
@@ -316,120 +325,182 @@ __device__ __forceinline__ void store_dkv(const CodAttnArgs& a, int64_t row, int
   }
 }
 
-template <int HD, int NK, class M>
-__global__ __launch_bounds__(256, 2) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
-  constexpr int KW = 16 * NK;                        // keys per wavefront
+// Eight wavefronts.  Real tokens: wavefront w has keys 32 (w % 4) .. of the
+// workgroup's 128 and half w / 4 of every stage's pairs; the halves are added at
+// the end.  Mask rows: wavefront w has 16 of 128 places and all pairs.  The pairs
+// are walked from the last to the first, so that the tiles of a sample, which all
+// end with its last pair, read the same stages at the same time.
+template <int HD, class M>
+__global__ __launch_bounds__(512, 2) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
+  constexpr int NK = 2, KW = 16 * NK;                // keys per wavefront
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
-  // a stage: four blocks of Q, four of dO, the pairs' statistics
-  __shared__ __attribute__((aligned(16))) u32x4 b0[8 * BU + 64], b1[8 * BU + 64];
+  // a stage: SP pairs, their blocks of Q and of dO (32 KiB in all) and statistics;
+  // a ring of three stages, in arrays of their own
+  constexpr int SP = HD == 64 ? 128 : 64, SB = SP / 16, SU = 2 * SB * BU + SP;
+  // at head_dim 128 the real tokens' V stays in LDS (in registers it would leave too few)
+  constexpr bool VL = HD == 128;
+  __shared__ __attribute__((aligned(16))) u32x4 b0[SU], b1[SU], b2[SU], v_s[VL ? 8 * BU : 1];
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = a.group;
   const float scale2 = a.scale * kLog2e;
   const bool real = blockIdx.x < real_blocks;        // uniform
   const unsigned id = real ? blockIdx.x : blockIdx.x - real_blocks;
-  const int keys = real ? 4 * KW : 64, per_tile = kCodTile / keys;
-  const int kvh = id % a.n_kv, rest = id / a.n_kv;
-  // (early real tokens are seen by the most rows: the list from its end)
-  const CodTileInfo tile = a.plan.tiles[real ? a.n_tiles - 1 - rest / per_tile : rest / per_tile];
+  const int kvh = id % a.n_kv;
+  const CodTileInfo tile = a.plan.by_sample[id / a.n_kv];
   const CodSampleInfo s = tile.s;
   const int4* const order = a.plan.order + s.off;
-  const int last = s.len - 1, n_pairs = s.len * group;
-  const int t0 = tile.tile * kCodTile + (rest % per_tile) * keys;
-  const PairStats* const stats = reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.sample);
-  // a lane's row of 16 pairs from `pair` on, in the order (past the sample: its last row)
-  auto place = [&](int pair) { return min((pair + block_row(lane)) / group, last); };
-  auto load_pairs = [&](int pair, int packed, u32x4* qb, u32x4* gb) __attribute__((always_inline)) {
-    const int head = kvh * group + (pair + block_row(lane)) % group;
-    load_block<HD>(at(a.q, s.off + packed, head) + block_byte(lane), qb);
-    load_block<HD>(at(a.d_out, s.off + packed, head) + block_byte(lane), gb);
+  const int last = s.len - 1, n_pairs = s.len * group, t0 = tile.tile * kCodTile;
+  if (t0 >= (real ? s.n_real : s.cap)) return;       // uniform
+  const PairStats* const stats =
+      reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.sample);
+
+  // Stages: a wavefront loads 16 pairs (past the sample: its last row) of Q and of
+  // dO (HD 64), or wavefronts 0 .. 3 of Q and 4 .. 7 of dO, and part of the
+  // statistics.  Data is loaded two stages ahead, the packed rows that it is at
+  // four: a wavefront's loads go out in one fixed order, packed rows before data,
+  // so that the wait for a stage's data covers the rows of the stage two on and
+  // leaves the newer loads in flight.  Stages past the first repeat it.
+  const int part = wave % SB, in_stage = part * 16 + block_row(lane);
+  auto fence = [&]() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+  auto stages = [&](int st0, int st1, auto step) __attribute__((always_inline)) {
+    constexpr int ND = (SB == 8 ? 2 : 1) * (HD / 32) + 1;   // data loads of a stage and wavefront
+    int packed[3];
+    auto find = [&](int slot, int st) __attribute__((always_inline)) {
+      packed[slot] = order[min(quotient(max(st, st0) * SP + in_stage, a.by_group), last)].x;
+      fence();
+    };
+    auto load = [&](u32x4* buf, int slot, int at_stage) __attribute__((always_inline)) {
+      const int st = max(at_stage, st0), x = st * SP + in_stage;
+      const uint32_t head = kvh * group + remainder(x, quotient(x, a.by_group), a.by_group), r = s.off + packed[slot];
+      if (SB == 8 || wave < 4) load_block<HD>(at(a.q, r, head) + block_byte(lane), buf + part * BU);
+      if (SB == 8 || wave >= 4) load_block<HD>(at(a.d_out, r, head) + block_byte(lane), buf + (SB + part) * BU);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st * (SP / 64)) + part * 256 + lane * 4),
+          (__attribute__((address_space(3))) void*)(buf + 2 * SB * BU + part * 16), 4, 0, 0);
+      fence();
+    };
+    find(0, st1 - 1);
+    find(1, st1 - 2);
+    find(2, st1 - 3);
+    load(b0, 0, st1 - 1);
+    find(0, st1 - 4);
+    load(b1, 1, st1 - 2);
+    // stage st (ring phase ph): its buffer cur; the one of the stage before it
+    // (read before the last barrier) takes the stage two on
+    auto one = [&](int st, int ph, const u32x4* cur, u32x4* dst) __attribute__((always_inline)) {
+      fence();
+      __builtin_amdgcn_s_waitcnt(vm_wait(ND + 1));
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      fence();
+      find((ph + 1) % 3, st - 4);
+      load(dst, (ph + 2) % 3, st - 2);
+      if (st >= st0) step(st, cur, reinterpret_cast<const PairStats*>(cur + 2 * SB * BU));   // uniform
+    };
+    for (int st = st1 - 1; st >= st0; st -= 3) {
+      one(st, 0, b0, b2);
+      one(st - 1, 1, b1, b0);
+      one(st - 2, 2, b2, b1);
+    }
+    wait_all();                                      // (the loads still in flight, before LDS is used again)
   };
+
   if (real) {
-    if (t0 >= s.n_real) return;                      // uniform
-    u32x4 kf[NK][KS], vf[NK][KS];
+    const int kw = wave & 3, half = wave >> 2;       // this wavefront's keys and pairs
+    const int w0 = t0 + kw * KW;
+    u32x4 kf[NK][KS], vr[VL ? 1 : NK][VL ? 1 : KS];
     f32x4 dk[NK][DB], dv[NK][DB];
+    if (VL) load_block<HD>(at(a.v, s.off + min(t0 + wave * 16 + block_row(lane), s.n_real - 1), kvh) + block_byte(lane),
+                           v_s + (VL ? wave * BU : 0));
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
-      const int key = min(t0 + wave * KW + k * 16 + c16, s.n_real - 1);
-      const char* const ks_ = at(a.k, s.off + key, kvh) + g4 * 16;
-      const char* const vs_ = at(a.v, s.off + key, kvh) + g4 * 16;
+      const uint32_t key = s.off + min(w0 + k * 16 + c16, s.n_real - 1);
+      const char* const ks_ = at(a.k, key, kvh) + g4 * 16;
+      const char* const vs_ = at(a.v, key, kvh) + g4 * 16;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         kf[k][ks] = *reinterpret_cast<const u32x4*>(ks_ + ks * 64);
-        vf[k][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
+        if (!VL) vr[VL ? 0 : k][VL ? 0 : ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) dk[k][db] = dv[k][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int st0 = a.plan.first[s.off + t0] * group / kStage, st1 = (n_pairs + kStage - 1) / kStage;
-    const int w0 = t0 + wave * KW;                   // this wavefront's first key
-    int packed = order[place(st0 * kStage + wave * 16)].x;   // of the next stage to load
-    auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
-      load_pairs(st * kStage + wave * 16, packed, buf + wave * BU, buf + (4 + wave) * BU);
-      if (wave == 0)
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st) + lane * 16),
-            (__attribute__((address_space(3))) void*)(buf + 8 * BU), 16, 0, 0);
-      packed = order[place((st + 1) * kStage + wave * 16)].x;
+    const auto vf = [&](int k, int ks) __attribute__((always_inline)) {
+      return VL ? rows_frag(v_s + (2 * kw + k) * BU, ks, lane) : vr[VL ? 0 : k][VL ? 0 : ks];
     };
-    load(b0, st0);
-    auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
-      wait_and_meet();
-      if (st + 1 < st1) load(nxt, st + 1);           // uniform
-      __builtin_amdgcn_sched_barrier(0);
-      const PairStats& ps = *reinterpret_cast<const PairStats*>(cur + 8 * BU);
-      const int lo = __builtin_amdgcn_readfirstlane(ps.seen[0]), hi = __builtin_amdgcn_readfirstlane(ps.seen[63]);
-      if (hi <= w0) return;                          // uniform: no pair sees this wavefront's keys
-      const bool masked = lo < w0 + KW;
+    // pairs from which on this wavefront's first and last key are seen
+    const int* const first = a.plan.first + s.off;
+    const int from = first[min(w0, s.n_real - 1)] * group, free = first[min(w0 + KW, s.n_real) - 1] * group;
+    stages(first[t0] * group / SP, (n_pairs + SP - 1) / SP,
+           [&](int st, const u32x4* cur, const PairStats* ps) __attribute__((always_inline)) {
+#pragma unroll 1
+             for (int h = half * (SP / 64); h < (half + 1) * (SP / 64); ++h) {
+               const int c0 = st * SP + h * 32;
+               if (c0 + 32 <= from || c0 >= n_pairs) continue;   // uniform: no pair that sees this wavefront's keys
+               const PairStats& stat = ps[h / 2];
+               // (before `free` some pair does not see some key)
+               dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (SB + 2 * h) * BU, stat, h % 2 * 32, kf, vf, dk, dv, scale2, lane,
+                                   c0 < free, stat.seen, [&](int k, int seen) { return seen <= w0 + k * 16 + c16; });
+             }
+           });
+    // the second half's sums through LDS: dK, then dV (a wavefront's in half a buffer)
+    static_assert(2 * NK * DB * 64 <= SU, "two slots in a buffer");
+    f32x4* const slot = reinterpret_cast<f32x4*>(kw & 2 ? b1 : b0) + (kw & 1) * NK * DB * 64 + lane;
+    auto add_halves = [&](f32x4 (&x)[NK][DB]) __attribute__((always_inline)) {
+      __syncthreads();
+      if (half) {                                    // uniform
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (4 + 2 * h) * BU, ps, h, kf, vf, dk, dv, scale2, lane, masked,
-                            [&](int k, int i) { return ps.seen[i] <= w0 + k * 16 + c16; });
+        for (int i = 0; i < NK * DB; ++i) slot[i * 64] = x[i / DB][i % DB];
+      }
+      __syncthreads();
+      if (!half) {
+#pragma unroll
+        for (int i = 0; i < NK * DB; ++i) x[i / DB][i % DB] += slot[i * 64];
+      }
     };
-    int st = st0;
-    for (; st + 2 <= st1; st += 2) {
-      stage(st, b0, b1);
-      stage(st + 1, b1, b0);
-    }
-    if (st < st1) stage(st, b0, b1);
+    add_halves(dk);
+    add_halves(dv);
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
       const int key = w0 + k * 16 + c16;
-      if (key < s.n_real) store_dkv<HD, M>(a, s.off + key, kvh, dk[k], dv[k], g4);
+      if (!half && key < s.n_real) store_dkv<HD, M>(a, s.off + key, kvh, dk[k], dv[k], g4);
     }
     return;
   }
 
-  // mask rows (and padding): this wavefront's 16 places
+  // mask rows (and padding)
   const int w0 = t0 + wave * 16, mine = w0 + c16;
-  if (w0 >= s.cap) return;                           // (no barrier below)
   const int4 e = order[min(mine, s.cap - 1)];
   const bool branch = mine <= last && e.x >= s.n_real;
-  u32x4 kf[1][KS], vf[1][KS];
+  const uint32_t chain_left = branch ? e.w - mine : 0;   // places that see this row, from its own on
   f32x4 dk[1][DB], dv[1][DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[0][db] = dv[0][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (w0 <= last) {                                  // uniform
-    const int4 el = order[min(mine, last)];
-    const char* const ks_ = at(a.k, s.off + el.x, kvh) + g4 * 16;
-    const char* const vs_ = at(a.v, s.off + el.x, kvh) + g4 * 16;
+  if (t0 <= last) {                                  // uniform
+    u32x4 kf[1][KS], vr[KS];
+    const uint32_t r = s.off + (mine <= last ? e.x : 0);
+    const char* const ks_ = at(a.k, r, kvh) + g4 * 16;
+    const char* const vs_ = at(a.v, r, kvh) + g4 * 16;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       kf[0][ks] = *reinterpret_cast<const u32x4*>(ks_ + ks * 64);
-      vf[0][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
+      vr[ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
     }
-    const int end = order[min(w0 + 15, last)].w * group;
-    u32x4* const qb = (wave & 2 ? b1 : b0) + (wave & 1) * 4 * BU;
-    for (int c0 = w0 * group / 32 * 32; c0 < end; c0 += 32) {   // uniform
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-        load_pairs(c0 + b * 16, order[place(c0 + b * 16)].x, qb + b * BU, qb + (2 + b) * BU);
-      wait_all();
-      const PairStats& st = stats[c0 / 64];
-      dkv_step<HD, 1, M>(qb, qb + 2 * BU, st, (c0 / 32) & 1, kf, vf, dk, dv, scale2, lane, true,
-                         [&](int, int i) { return !branch || st.pos[i] < mine || st.pos[i] >= e.w; });
-      wait_all();                                    // (its reads are done before the next loads)
-    }
+    const auto vf = [&](int, int ks) __attribute__((always_inline)) { return vr[ks]; };
+    const int from = w0 * group, end = w0 <= last ? order[min(w0 + 15, last)].w * group : 0;   // this wavefront's pairs
+    stages(t0 * group / SP, (order[min(t0 + kCodTile - 1, last)].w * group + SP - 1) / SP,
+           [&](int st, const u32x4* cur, const PairStats* ps) __attribute__((always_inline)) {
+#pragma unroll 1
+             for (int h = 0; h < SP / 32; ++h) {
+               const int c0 = st * SP + h * 32;
+               if (c0 >= end || c0 + 32 <= from) continue;   // uniform
+               const PairStats& stat = ps[h / 2];
+               dkv_step<HD, 1, M>(cur + 2 * h * BU, cur + (SB + 2 * h) * BU, stat, h % 2 * 32, kf, vf, dk, dv, scale2, lane,
+                                  true, stat.pos, [&](int, int pos) { return (uint32_t)(pos - mine) >= chain_left; });
+             }
+           });
   }
   if (mine > last) {                                 // (whatever the sample's rows hold)
 #pragma unroll
@@ -440,13 +511,11 @@ __global__ __launch_bounds__(256, 2) void k_cod_dkv(const CodAttnArgs a, unsigne
 
 template <int HD, class M>
 hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
-  constexpr int NQ = 2, NK = HD == 128 ? 1 : 2;
-  const int64_t heads = (int64_t)a.n_tiles * a.n_kv;
-  const int64_t dq = heads * (kCodTile / (64 * NQ)) * a.group;
-  const int64_t real = heads * (kCodTile / (64 * NK)), all = real + heads * (kCodTile / 64);
-  if (dq > 0x7fffffff || all > 0x7fffffff) return hipErrorInvalidValue;
+  constexpr int NQ = 2;
+  const int64_t tiles = (int64_t)a.n_tiles * a.n_kv, dq = tiles * (kCodTile / (64 * NQ)) * a.group;
+  if (dq > 0x7fffffff || 2 * tiles > 0x7fffffff) return hipErrorInvalidValue;
   k_cod_dq<HD, NQ, M><<<(unsigned)dq, 256, 0, st>>>(a);
-  k_cod_dkv<HD, NK, M><<<(unsigned)all, 256, 0, st>>>(a, (unsigned)real);
+  k_cod_dkv<HD, M><<<(unsigned)(2 * tiles), 512, 0, st>>>(a, (unsigned)tiles);
   return hipGetLastError();
 }
 

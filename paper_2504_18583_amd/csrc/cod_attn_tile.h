@@ -22,6 +22,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -118,9 +119,14 @@ __device__ __forceinline__ float sum4g(float x) {
 __device__ __forceinline__ float base2_scale(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-30f); }
 __device__ __forceinline__ uint32_t scale_sign(float scale) { return scale < 0.f ? 0x80008000u : 0u; }
 
-__device__ __forceinline__ char* at(const Heads& h, int64_t row, int head) {
-  return h.data + 2 * (row * h.rs + head * h.hs);
+__device__ __forceinline__ char* at(const Heads16& h, uint32_t row, uint32_t head) {
+  return h.data + (uint64_t)head * h.hs + (uint64_t)row * h.rs;
 }
+__device__ __forceinline__ int quotient(int x, const FastDiv& f) { return (int)(__umulhi((uint32_t)x << 2, f.m) >> f.l); }
+__device__ __forceinline__ int remainder(int x, int q, const FastDiv& f) { return x - q * (int)f.d; }
+
+// s_waitcnt vmcnt(n) lgkmcnt(0).
+constexpr int vm_wait(int n) { return (n & 15) | ((n >> 4) << 14) | 0x70; }
 
 // Everything this wavefront loaded is in LDS and its LDS reads are done; then
 // everyone's.

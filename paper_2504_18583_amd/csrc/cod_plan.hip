@@ -99,10 +99,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_cod_plan(const int32_t* sectio
   if (bad) *v.bad = 1;
 }
 
-// Tiles of all samples, those with the largest index in their sample first:
-// they see the most keys.
+// Tiles of all samples in two orders: those with the largest index in their
+// sample first (as queries they see the most keys), and sample by sample, those
+// with the most tiles first (as keys, the tiles of a sample read the same rows at
+// the same time).
 __global__ __launch_bounds__(kPlanThreads) void k_cod_tiles(int n_samples, int n_levels, const CodPlanView v) {
-  extern __shared__ int level_s[];           // next free place of each level
+  extern __shared__ int level_s[];           // next free place of each level, and of the samples with so many tiles
+  int* const size_s = level_s + n_levels;
   __shared__ int wave_s[kPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63;
   auto tiles_of = [&](int s) { return (int)((v.offsets[s + 1] - v.offsets[s] + kCodTile - 1) / kCodTile); };
@@ -113,6 +116,17 @@ __global__ __launch_bounds__(kPlanThreads) void k_cod_tiles(int n_samples, int n
     if (n > 0) atomicAdd(&level_s[n - 1], 1);
   }
   __syncthreads();
+  // tiles of the samples with more tiles
+  {
+    int carry = 0;
+    for (int b = 0; b < n_levels; b += kPlanThreads) {
+      const int l = n_levels - 1 - (b + tid), x = l >= 0 ? level_s[l] * (l + 1) : 0;
+      int total;
+      const int incl = block_incl_scan(x, wave_s, &total) + carry;
+      if (l >= 0) size_s[l] = incl - x;
+      carry += total;
+    }
+  }
   // samples with exactly l + 1 tiles -> samples with more than l -> tiles of
   // later levels: two scans from the last level down
   for (int pass = 0; pass < 2; ++pass) {
@@ -129,7 +143,14 @@ __global__ __launch_bounds__(kPlanThreads) void k_cod_tiles(int n_samples, int n
   for (int s = tid >> 6; s < n_samples; s += kPlanThreads / 64) {
     const int n = tiles_of(s);
     const CodSampleInfo info = v.samples[s];
-    for (int l = lane; l < n; l += 64) v.tiles[atomicAdd(&level_s[l], 1)] = CodTileInfo{info, s, l, 0};
+    if (n == 0) continue;                    // uniform
+    int base = lane == 0 ? atomicAdd(&size_s[n - 1], n) : 0;
+    base = __shfl(base, 0);
+    for (int l = lane; l < n; l += 64) {
+      const CodTileInfo t{info, s, l, 0};
+      v.tiles[atomicAdd(&level_s[l], 1)] = t;
+      v.by_sample[base + l] = t;
+    }
   }
 }
 
@@ -147,6 +168,7 @@ size_t cod_plan_layout(int64_t rows, int n_samples, void* data, CodPlanView* v) 
   char* const first = take((size_t)rows * sizeof(int));
   char* const samples = take((size_t)n_samples * sizeof(CodSampleInfo));
   char* const tiles = take(((size_t)rows / kCodTile + n_samples) * sizeof(CodTileInfo));
+  char* const by_sample = take(((size_t)rows / kCodTile + n_samples) * sizeof(CodTileInfo));
   char* const offsets = take(((size_t)n_samples + 1) * sizeof(int64_t));
   char* const bad = take(sizeof(int));
   if (v) {
@@ -154,6 +176,7 @@ size_t cod_plan_layout(int64_t rows, int n_samples, void* data, CodPlanView* v) 
     v->first = reinterpret_cast<int*>(first);
     v->samples = reinterpret_cast<CodSampleInfo*>(samples);
     v->tiles = reinterpret_cast<CodTileInfo*>(tiles);
+    v->by_sample = reinterpret_cast<CodTileInfo*>(by_sample);
     v->offsets = reinterpret_cast<int64_t*>(offsets);
     v->bad = reinterpret_cast<int*>(bad);
   }
@@ -167,7 +190,7 @@ hipError_t launch_cod_plan(const int32_t* section, const int32_t* column, const 
   // a region holds at most 64 rows of each of 8192 chains; more is padding
   if (n_levels > 16384) return hipErrorInvalidValue;
   k_cod_plan<<<n_samples, kPlanThreads, (size_t)n_chains * 12, st>>>(section, column, out_len, n_chains, v);
-  k_cod_tiles<<<1, kPlanThreads, (size_t)n_levels * sizeof(int), st>>>(n_samples, n_levels, v);
+  k_cod_tiles<<<1, kPlanThreads, (size_t)n_levels * 2 * sizeof(int), st>>>(n_samples, n_levels, v);
   return hipGetLastError();
 }
 

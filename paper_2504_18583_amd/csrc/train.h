@@ -74,6 +74,7 @@ struct CodPlanView {
   int* first;                              // [off + real token]: its position
   CodSampleInfo* samples;
   CodTileInfo* tiles;                      // later tiles first
+  CodTileInfo* by_sample;                  // samples with the most tiles first, each one's tiles in order
   int64_t* offsets;                        // the caller's out_offsets
   int* bad;                                // nonzero: rows not in the documented form
 };
@@ -81,14 +82,27 @@ size_t cod_plan_layout(int64_t rows, int n_samples, void* data, CodPlanView* v);
 hipError_t launch_cod_plan(const int32_t* section, const int32_t* column, const int32_t* out_len, int n_samples,
                            int max_region, const CodPlanView& v, hipStream_t st);
 
+// Tensor of 16-bit elements: strides in bytes.  32-bit strides make an address
+// one multiply-add per index.
+struct Heads16 {
+  char* data;
+  uint32_t rs, hs;
+};
+// Division of 0 <= x < 2^30 by d <= 1024: x / d = (x m) >> (30 + l) with m =
+// ceil(2^(30 + l) / d), l = ceil(log2 d) (m d exceeds 2^(30 + l) by less than
+// d <= 2^l, which times x stays below 2^(30 + l)).
+struct FastDiv {
+  uint32_t m, l, d;
+};
 struct CodAttnArgs {
   CodPlanView plan;
   int n_tiles, n_samples, n_heads, n_kv, group;
+  FastDiv by_group;
   int64_t rows;                            // of lse
   float scale;
-  Heads q, k, v, out;
+  Heads16 q, k, v, out;
   float* lse;                              // forward: written (may be null); gradient: read
-  Heads d_out, dq, dk, dv;
+  Heads16 d_out, dq, dk, dv;
   void* stats;                             // gradient: the pairs' statistics (workspace)
   int64_t stats_blocks;                    // blocks of 64 pairs of a key head
 };

@@ -83,10 +83,16 @@ pard_status attn_check(const pard_cod_attn_args* a) {
   return a->n_heads > 65535 || a->n_heads / a->n_kv_heads > 1024 ? PARD_ERR_UNSUPPORTED : PARD_OK;
 }
 
-// The kernels read and write 16 bytes of a head at a time.
+// The kernels read and write 16 bytes of a head at a time, and take strides in
+// bytes of 32 bits.
+constexpr int64_t kMaxStride = 0x7fffffff;
 bool attn_heads_ok(const pard_heads* t, const pard_cod_attn_args* a, int heads, bool out) {
   return heads_ok(t, a->plan->rows, heads, a->head_dim, out) && aligned(t->data, 16) && t->row_stride % 8 == 0 &&
-         t->head_stride % 8 == 0;
+         t->head_stride % 8 == 0 && t->row_stride <= kMaxStride && t->head_stride <= kMaxStride;
+}
+
+Heads16 view16(const pard_heads* t) {
+  return Heads16{static_cast<char*>(t->data), (uint32_t)(2 * t->row_stride), (uint32_t)(2 * t->head_stride)};
 }
 
 CodAttnArgs attn_args(const pard_cod_attn_args* a) {
@@ -97,6 +103,9 @@ CodAttnArgs attn_args(const pard_cod_attn_args* a) {
   r.n_heads = a->n_heads;
   r.n_kv = a->n_kv_heads;
   r.group = a->n_heads / a->n_kv_heads;
+  r.by_group.d = r.group;
+  while ((1u << r.by_group.l) < r.by_group.d) ++r.by_group.l;
+  r.by_group.m = (uint32_t)(((1ull << (30 + r.by_group.l)) + r.by_group.d - 1) / r.by_group.d);
   r.rows = a->plan->rows;
   r.scale = a->scale;
   return r;
@@ -232,10 +241,10 @@ pard_status pard_cod_attn(const pard_cod_attn_args* args, const pard_heads* q, c
     return PARD_ERR_ARG;
   if (args->plan->n_tiles == 0) return PARD_OK;
   CodAttnArgs r = attn_args(args);
-  r.q = view(q);
-  r.k = view(k);
-  r.v = view(v);
-  r.out = view(out);
+  r.q = view16(q);
+  r.k = view16(k);
+  r.v = view16(v);
+  r.out = view16(out);
   r.lse = lse;
   return status_of(launch_cod_attn(args->head_dim, args->dtype, r, reinterpret_cast<hipStream_t>(hip_stream)));
 }
@@ -261,15 +270,15 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args* args, const pard_heads*
   if (!lse || !workspace || !aligned(workspace, 256)) return PARD_ERR_ARG;
   if (workspace_bytes < pard_cod_attn_workspace_bytes(args)) return PARD_ERR_NOMEM;
   CodAttnArgs r = attn_args(args);
-  r.q = view(q);
-  r.k = view(k);
-  r.v = view(v);
-  r.out = view(out);
+  r.q = view16(q);
+  r.k = view16(k);
+  r.v = view16(v);
+  r.out = view16(out);
   r.lse = const_cast<float*>(lse);
-  r.d_out = view(d_out);
-  r.dq = view(dq);
-  r.dk = view(dk);
-  r.dv = view(dv);
+  r.d_out = view16(d_out);
+  r.dq = view16(dq);
+  r.dk = view16(dk);
+  r.dv = view16(dv);
   r.stats = workspace;
   return status_of(launch_cod_attn_grad(args->head_dim, args->dtype, r, reinterpret_cast<hipStream_t>(hip_stream)));
 }
