@@ -2,8 +2,13 @@
 //
 //   CE = log sum exp(x) - x[label];  d x = w (exp(x - lse) - [label]),
 // w the row's share of the loss (1 / its subtask's counted rows, weighted).
-// Three launches: the counted rows of every subtask, one workgroup per row,
-// the means.  Bound: memory (the logits in, the gradient out).
+// Three launches: the counted rows of every subtask, the rows, the means.
+//
+// Bound: memory (the logits in, the gradient out).  So a row is read once: its
+// 16-byte vectors stay in the registers of one workgroup (at most 20 a thread
+// of 1024: 163 840 logits of two bytes) from the sum to the gradient, and as
+// soon as a vector's gradient is stored, its registers take the same vector of
+// the workgroup's next row.  Longer rows are read a second time.
 #include "train.h"
 
 #include <algorithm>
@@ -33,10 +38,15 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_count(const CodLossArgs a
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
 }
 
-__device__ __forceinline__ int count_of(const CodLossArgs& a, int k) {
-  int n = 0;
-  for (int b = 0; b < kLossCountBlocks; ++b) n += a.counts[b * kCodMaxSections + k - 1];
-  return n;
+// Counted rows of each subtask, in LDS (one barrier).
+__device__ __forceinline__ void load_counts(const CodLossArgs& a, int (&n_s)[kCodMaxSections]) {
+  for (int k = threadIdx.x; k < a.n_sections; k += blockDim.x) {
+    int n = 0;
+#pragma unroll
+    for (int b = 0; b < kLossCountBlocks; ++b) n += a.counts[b * kCodMaxSections + k];
+    n_s[k] = n;
+  }
+  __syncthreads();
 }
 
 // Joins two (maximum, sum of 2^(z - maximum)) pairs.
@@ -47,86 +57,248 @@ __device__ __forceinline__ void join(float& m, float& l, float om, float ol) {
   m = n;
 }
 
+// 16 bytes of logits.
 template <class E>
-__global__ __launch_bounds__(kLossThreads) void k_loss_row(const CodLossArgs a) {
-  using T = typename E::T;
-  __shared__ float m_s[kLossThreads / 64], l_s[kLossThreads / 64];
-  const int r = blockIdx.x, k = section_of(a, r);
-  const T* x = reinterpret_cast<const T*>(a.logits) + r * a.stride;
-  T* d = a.d_logits ? reinterpret_cast<T*>(a.d_logits) + r * a.d_stride : nullptr;
-  if (k == 0) {                                      // uniform
-    for (int i = threadIdx.x; d && i < a.vocab; i += kLossThreads) d[i] = E::store(0.f);
-    if (threadIdx.x == 0) a.row_loss[r] = 0.f;
-    return;
+struct LossVec {
+  static constexpr int N = 8;
+  uint4 v;
+  __device__ __forceinline__ float operator[](int i) const {
+    const uint32_t w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+    return E::load((uint16_t)(i & 1 ? w >> 16 : w));
   }
-  const int label = a.labels[r];
-  const float x_label = label < a.vocab ? E::load(x[label]) : __builtin_nanf("");
-  float m = -INFINITY, l = 0.f;
-  for (int i = threadIdx.x; i < a.vocab; i += kLossThreads) join(m, l, E::load(x[i]) * kLog2e, 1.f);
-  for (int off = 32; off > 0; off >>= 1) {
-    const float om = __shfl_xor(m, off), ol = __shfl_xor(l, off);
-    join(m, l, om, ol);
+  __device__ __forceinline__ static LossVec pack(const float (&x)[N]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)E::store(x[2 * i]) | ((uint32_t)E::store(x[2 * i + 1]) << 16);
+    return LossVec{uint4{w[0], w[1], w[2], w[3]}};
   }
-  if ((threadIdx.x & 63) == 0) {
-    m_s[threadIdx.x >> 6] = m;
-    l_s[threadIdx.x >> 6] = l;
+};
+template <>
+struct LossVec<ElemF32> {
+  static constexpr int N = 4;
+  float4 v;
+  __device__ __forceinline__ float operator[](int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+  __device__ __forceinline__ static LossVec pack(const float (&x)[N]) { return LossVec{float4{x[0], x[1], x[2], x[3]}}; }
+};
+
+// Adds the elements of C vectors to a thread's (maximum, sum), base 2.
+template <class E, int C>
+__device__ __forceinline__ void add_vectors(const LossVec<E>* v, float& m, float& l) {
+  constexpr int N = LossVec<E>::N;
+  float top = v[0][0];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, v[c][i]);
+  top *= kLog2e;
+  if (top > m) {
+    l *= exp2f(m - top);                             // (m = -infinity: l is 0)
+    m = top;
   }
-  __syncthreads();
-  m = -INFINITY;
-  l = 0.f;
-  for (int w = 0; w < kLossThreads / 64; ++w) join(m, l, m_s[w], l_s[w]);
-  const float lse2 = m + log2f(l);
-  if (threadIdx.x == 0) a.row_loss[r] = lse2 * kLn2 - x_label;
-  if (!d) return;
-  int n = 0;
-  float w = a.grad_scale;
-  if (a.weighted) {
-    n = count_of(a, k);
-    w *= a.weights[k - 1];
-  } else {
-    for (int q = 1; q <= a.n_sections; ++q) n += count_of(a, q);
+  // (no finite logit so far: every term is 0, or NaN for a NaN)
+  const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < N; ++i) l += __builtin_amdgcn_exp2f(fmaf(v[c][i], kLog2e, -ref));
+}
+
+// Rows of T threads, NV vectors each.  A row's elements before its first 16-byte
+// boundary and after its last are a thread's own each (fewer than T).
+// RESIDENT: the vectors stay in registers, and the next row's follow them in;
+// otherwise they are read NV at a time, twice where there is a gradient.
+// SCALAR_OUT: the gradient's rows lie at other offsets from a 16-byte boundary.
+template <class E, int T, int NV, bool RESIDENT, bool SCALAR_OUT>
+__global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
+  using Vec = LossVec<E>;
+  using Elem = typename E::T;
+  constexpr int N = Vec::N, SZ = sizeof(Elem), W = T / 64;
+  constexpr int C = NV % (16 / N) == 0 ? 16 / N : 1;   // vectors added at a time: 16 logits
+  __shared__ float m_s[2][W], l_s[2][W];
+  __shared__ int n_s[kCodMaxSections];
+  load_counts(a, n_s);
+  int n_all = 0;
+  for (int q = 0; q < a.n_sections; ++q) n_all += n_s[q];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Vec v[NV];
+  float edge = -INFINITY;                            // this thread's element outside the vectors
+  float x_label = 0.f;
+  int k = 0, label = -1, head = 0, n_vec = 0;
+  auto shape = [&](int r) __attribute__((always_inline)) {
+    // elements before the first boundary (all of a row shorter than that)
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a.logits) + a.stride * r * SZ;
+    head = min((int)((16 - (at & 15)) & 15) / SZ, a.vocab);
+    n_vec = (a.vocab - head) / N;
+  };
+  // element index of this thread's edge element, -1 if it has none
+  auto edge_at = [&]() __attribute__((always_inline)) {
+    const int i = tid < head ? tid : head + n_vec * N + tid - head;
+    return i < a.vocab ? i : -1;
+  };
+  float low[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) low[i] = -INFINITY;
+  const Vec none = Vec::pack(low);
+  // vector i of this thread in a row whose vectors begin at the (uniform) address
+  // base: a scalar address and a 32-bit offset
+  const uint32_t voff = tid * 16;
+  auto vec_at = [&](const char* base, int i) __attribute__((always_inline)) {
+    return reinterpret_cast<const Vec*>(base + (uint64_t)i * (T * 16) + voff);
+  };
+  auto fetch = [&](const Elem* x, int i0, int i) __attribute__((always_inline)) {
+    const char* const base = reinterpret_cast<const char*>(x + head);
+    if ((i0 + i + 1) * T <= n_vec) {                 // uniform: the whole workgroup's
+      v[i] = *vec_at(base, i0 + i);
+    } else {
+      v[i] = none;
+      if ((i0 + i) * T + tid < n_vec) v[i] = *vec_at(base, i0 + i);
+    }
+  };
+  auto row_of = [&](int r) __attribute__((always_inline)) { return reinterpret_cast<const Elem*>(a.logits) + r * a.stride; };
+  auto meta = [&](int r) __attribute__((always_inline)) {
+    k = section_of(a, r);
+    label = a.labels[r];
+  };
+  const int rounds = RESIDENT ? 1 : (a.vocab / N + NV * T - 1) / (NV * T);
+  if (RESIDENT) {
+    shape(blockIdx.x);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) fetch(row_of(blockIdx.x), 0, i);
   }
-  w = label < a.vocab ? w / n : __builtin_nanf("");
-  __syncthreads();                                   // (x[label] is read: d may be x)
-  for (int i = threadIdx.x; i < a.vocab; i += kLossThreads) {
-    const float p = exp2f(E::load(x[i]) * kLog2e - lse2);
-    d[i] = E::store(w * (i == label ? p - 1.f : p));
+  int turn = 0;
+  for (int r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+    const Elem* const x = row_of(r);
+    Elem* const d = RESIDENT || a.d_logits ? reinterpret_cast<Elem*>(a.d_logits) + r * a.d_stride : nullptr;
+    shape(r);
+    meta(r);
+    const int e = edge_at();
+    edge = e >= 0 ? E::load(x[e]) : -INFINITY;
+    if (k > 0) x_label = label < a.vocab ? E::load(x[label]) : __builtin_nanf("");
+    float m = -INFINITY, l = 0.f;
+    for (int q = 0; q < rounds; ++q) {
+      if (!RESIDENT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) fetch(x, q * NV, i);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; i += C) {
+        add_vectors<E, C>(v + i, m, l);
+        __builtin_amdgcn_sched_barrier(0);           // (few unpacked logits at a time)
+      }
+    }
+    join(m, l, edge * kLog2e, 1.f);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+      const float om = __shfl_xor(m, off), ol = __shfl_xor(l, off);
+      join(m, l, om, ol);
+    }
+    if (lane == 0) {
+      m_s[turn][wave] = m;
+      l_s[turn][wave] = l;
+    }
+    __syncthreads();                                 // (also: x[label] is read before d, which may be x, is written)
+    m = m_s[turn][0];
+    l = l_s[turn][0];
+    for (int w = 1; w < W; ++w) join(m, l, m_s[turn][w], l_s[turn][w]);
+    const float lse2 = m + log2f(l);
+    if (tid == 0) a.row_loss[r] = k > 0 ? lse2 * kLn2 - x_label : 0.f;
+    if (!RESIDENT && !d) continue;
+    const float w = k == 0 ? 0.f : label >= a.vocab ? __builtin_nanf("")
+                           : a.weighted ? a.weights[k - 1] * a.grad_scale / n_s[k - 1] : a.grad_scale / n_all;
+    const int n_now = n_vec, head_now = head;
+    const int r_next = min((int64_t)r + gridDim.x, (int64_t)a.rows - 1);   // (past the last row: that one again, unused)
+    const Elem* const next = row_of(r_next);
+    if (RESIDENT) shape(r_next);
+    const char* const x_base = reinterpret_cast<const char*>(x + head_now);
+    const char* const d_base = reinterpret_cast<const char*>(d + head_now);
+    for (int q = 0; q < rounds; ++q) {
+      if (!RESIDENT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if ((q * NV + i) * T + tid < n_now) v[i] = *vec_at(x_base, q * NV + i);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int at = (q * NV + i) * T + tid;
+        // (unpacked again here: kept from the sum, it would take twice the registers)
+        asm("" : "+v"(v[i].v.x), "+v"(v[i].v.y), "+v"(v[i].v.z), "+v"(v[i].v.w));
+        if ((q * NV + i + 1) * T <= n_now || at < n_now) {   // (the first part uniform)
+          float g[N];
+#pragma unroll
+          for (int j = 0; j < N; ++j) g[j] = k > 0 ? w * __builtin_amdgcn_exp2f(fmaf(v[i][j], kLog2e, -lse2)) : 0.f;
+          if (SCALAR_OUT) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) d[head_now + at * N + j] = E::store(g[j]);
+          } else {
+            *const_cast<Vec*>(vec_at(d_base, q * NV + i)) = Vec::pack(g);
+          }
+        }
+        if (RESIDENT) fetch(next, 0, i);
+        __builtin_amdgcn_sched_barrier(0);           // (one vector at a time: its registers are taken over)
+      }
+    }
+    if (e >= 0) d[e] = E::store(k > 0 ? w * exp2f(edge * kLog2e - lse2) : 0.f);
+    // the label's element again, by the thread that wrote it
+    if (k > 0 && label < a.vocab) {
+      const int in_vec = label - head_now;
+      const bool own = in_vec >= 0 && in_vec < n_now * N ? in_vec / N % T == tid : label == e;
+      if (own) d[label] = E::store(w * (exp2f(x_label * kLog2e - lse2) - 1.f));
+    }
   }
 }
 
 // Workgroup k - 1: subtask k's mean; the last one to end adds the means up.
 __global__ __launch_bounds__(1024) void k_loss_mean(const CodLossArgs a) {
   __shared__ double s_s[16];
-  __shared__ int last_s;
+  __shared__ int n_s[kCodMaxSections];
+  load_counts(a, n_s);
   const int k = blockIdx.x + 1;
   double s = 0.0;
-  for (int r = threadIdx.x; r < a.rows; r += 1024)
-    if (section_of(a, r) == k) s += a.row_loss[r];
+  for (int64_t r = threadIdx.x; r < a.rows; r += 1024)
+    if (section_of(a, (int)r) == k) s += a.row_loss[r];
   for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
   if ((threadIdx.x & 63) == 0) s_s[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x != 0) return;
   s = 0.0;
   for (int w = 0; w < 16; ++w) s += s_s[w];
-  const int n = count_of(a, k);
+  const int n = n_s[k - 1];
   __hip_atomic_store(&a.loss[k], n ? (float)(s / n) : 0.f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  last_s = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-  if (last_s != a.n_sections - 1) return;
+  if (__hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != a.n_sections - 1) return;
   double total = 0.0;
   int64_t all = 0;
   for (int q = 1; q <= a.n_sections; ++q) {
     const double mean = __hip_atomic_load(&a.loss[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const int c = count_of(a, q);
-    total += a.weighted ? a.weights[q - 1] * mean : c * mean;
-    all += c;
+    total += a.weighted ? a.weights[q - 1] * mean : n_s[q - 1] * mean;
+    all += n_s[q - 1];
   }
   a.loss[0] = (float)(a.weighted ? total : all ? total / all : 0.0);
 }
 
+template <class E, int T, int NV, bool RESIDENT, bool SCALAR_OUT = false>
+void launch_variant(const CodLossArgs& a, hipStream_t st) {
+  // resident rows: as many workgroups as the device holds at once (of 1024
+  // threads one a CU, of 256 eight), each with several rows
+  const int most = !RESIDENT ? 1 << 20 : T == 1024 ? 256 : 2048;
+  k_loss_row<E, T, NV, RESIDENT, SCALAR_OUT><<<std::min(a.rows, most), T, 0, st>>>(a);
+}
+
 template <class E>
 hipError_t launch_rows(const CodLossArgs& a, hipStream_t st) {
+  constexpr int N = LossVec<E>::N, SZ = 16 / N;
   k_loss_count<<<kLossCountBlocks, kLossThreads, 0, st>>>(a);
-  if (a.rows > 0) k_loss_row<E><<<a.rows, kLossThreads, 0, st>>>(a);
+  if (a.rows > 0) {
+    const int n = (a.vocab + N - 1) / N;             // vectors of a row
+    const bool same = !a.d_logits || ((a.logits - a.d_logits) % 16 == 0 && (a.rows == 1 || (a.stride - a.d_stride) * SZ % 16 == 0));
+    if (!same) launch_variant<E, 1024, 4, false, true>(a, st);
+    else if (!a.d_logits || n > 20480) n <= 1024 ? launch_variant<E, 256, 4, false>(a, st) : launch_variant<E, 1024, 8, false>(a, st);
+    else if (n <= 256) launch_variant<E, 256, 1, true>(a, st);
+    else if (n <= 1024) launch_variant<E, 256, 4, true>(a, st);
+    else if (n <= 4096) launch_variant<E, 1024, 4, true>(a, st);
+    else if (n <= 8192) launch_variant<E, 1024, 8, true>(a, st);
+    else if (n <= 16384) launch_variant<E, 1024, 16, true>(a, st);
+    else launch_variant<E, 1024, 20, true>(a, st);
+  }
   k_loss_mean<<<a.n_sections, 1024, 0, st>>>(a);
   return hipGetLastError();
 }

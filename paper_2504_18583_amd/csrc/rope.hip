@@ -188,10 +188,274 @@ __global__ __launch_bounds__(64) void k_rope_gain_sum(const float* part, int blo
   }
 }
 
+// Vectorised kernels.  A head is HD / 16 units of 16 elements: unit u < rot / 16
+// turns the pairs 8 u .. 8 u + 7 (half: elements 8 u .. and rot / 2 + 8 u ..;
+// interleaved: 16 u ..), a later unit is the 16 elements 16 u ...  W lanes (the
+// next power of two) hold one head, one unit each, and take the heads of one row
+// H apart, so that a lane's cosines and sines are read once per row.
+template <class E>
+struct Vec8 {
+  static_assert(sizeof(typename E::T) == 2, "two 16-bit elements a word");
+  uint4 v;
+  __device__ __forceinline__ void load(const char* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = E::load((uint16_t)w[i]);
+      x[2 * i + 1] = E::load((uint16_t)(w[i] >> 16));
+    }
+  }
+  __device__ __forceinline__ static void store(char* p, const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)E::store(x[2 * i]) | ((uint32_t)E::store(x[2 * i + 1]) << 16);
+    *reinterpret_cast<uint4*>(p) = uint4{w[0], w[1], w[2], w[3]};
+  }
+};
+template <>
+struct Vec8<ElemF32> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const char* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+  __device__ __forceinline__ static void store(char* p, const float (&x)[8]) {
+    reinterpret_cast<float4*>(p)[0] = float4{x[0], x[1], x[2], x[3]};
+    reinterpret_cast<float4*>(p)[1] = float4{x[4], x[5], x[6], x[7]};
+  }
+};
+
+// 16 elements of a unit turned by the row's angles (INV: back).
+template <int LAYOUT, bool INV>
+__device__ __forceinline__ void turn_unit(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // the pair: (a[i], b[i]), or neighbours
+    float& x = LAYOUT == PARD_ROPE_HALF ? a[i] : (i < 4 ? a[2 * (i & 3)] : b[2 * (i & 3)]);
+    float& y = LAYOUT == PARD_ROPE_HALF ? b[i] : (i < 4 ? a[2 * (i & 3) + 1] : b[2 * (i & 3) + 1]);
+    const float sn = INV ? -s[i] : s[i], u = x * c[i] - y * sn;
+    y = y * c[i] + x * sn;
+    x = u;
+  }
+}
+
+template <class E, int LAYOUT, bool GRAD, bool NORM, int W>
+__global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_step, int rows_per_block) {
+  constexpr int SZ = sizeof(typename E::T), U = GRAD && NORM ? 2 : 4;   // heads in flight
+  const int tid = threadIdx.x, unit = tid % W, slot = tid / W;
+  const int h0 = slot % h_step, row_slot = slot / h_step, row_step = kRopeThreads / W / h_step;
+  const int heads = a.n_q + a.n_k;
+  const bool on = unit * 16 < a.hd, turns = on && unit * 16 < a.rot;
+  // element offsets of this lane's two vectors
+  const int o0 = !on ? 0 : turns && LAYOUT == PARD_ROPE_HALF ? unit * 8 : unit * 16;
+  const int o1 = !on ? 0 : turns && LAYOUT == PARD_ROPE_HALF ? a.rot / 2 + unit * 8 : unit * 16 + 8;
+  float gq[2][8], gk[2][8], dgq[2][8], dgk[2][8];
+  if (NORM) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      gq[0][i] = a.q_gain[o0 + i];
+      gq[1][i] = a.q_gain[o1 + i];
+      gk[0][i] = a.n_k > 0 ? a.k_gain[o0 + i] : 0.f;
+      gk[1][i] = a.n_k > 0 ? a.k_gain[o1 + i] : 0.f;
+      dgq[0][i] = dgq[1][i] = dgk[0][i] = dgk[1][i] = 0.f;
+    }
+  }
+  const float inv_hd = 1.0f / a.hd;
+  const int row_end = min((int64_t)a.rows, ((int64_t)blockIdx.x + 1) * rows_per_block);
+  for (int row = blockIdx.x * rows_per_block + row_slot; row < row_end; row += row_step) {
+    const int pos = a.pos[row];
+    const bool ok = pos >= 0 && pos < a.n_pos;
+    float c[8] = {}, s[8] = {};
+    if (turns) {
+      const float4* t = reinterpret_cast<const float4*>(a.table + (size_t)(ok ? pos : 0) * (a.rot / 2) + unit * 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 v = t[i];
+        c[2 * i] = v.x, s[2 * i] = v.y, c[2 * i + 1] = v.z, s[2 * i + 1] = v.w;
+      }
+    }
+    for (int hb = h0; hb < heads; hb += U * h_step) {
+      Vec8<E> v[U][2], w[U][2];
+      char* dst[U];
+      bool live[U], is_q[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int hh = hb + j * h_step;
+        live[j] = hh < heads && on;
+        is_q[j] = hh < a.n_q;
+        const int head = is_q[j] ? hh : hh - a.n_q;
+        const Heads& hi = is_q[j] ? a.q_in : a.k_in;
+        const Heads& ho = is_q[j] ? a.q_out : a.k_out;
+        dst[j] = ho.data + SZ * (row * ho.rs + head * ho.hs);
+        if (live[j]) {
+          const char* src = hi.data + SZ * (row * hi.rs + head * hi.hs);
+          v[j][0].load(src + SZ * o0);
+          v[j][1].load(src + SZ * o1);
+          if (GRAD && NORM) {
+            const Heads& hx = is_q[j] ? a.q_x : a.k_x;
+            const char* sx = hx.data + SZ * (row * hx.rs + head * hx.hs);
+            w[j][0].load(sx + SZ * o0);
+            w[j][1].load(sx + SZ * o1);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (!NORM && !live[j]) continue;
+        float x[2][8], y[2][8];
+        if (live[j]) {
+          v[j][0].get(x[0]);
+          v[j][1].get(x[1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = 0.f;
+        }
+        if (GRAD) {
+          if (turns) turn_unit<LAYOUT, true>(x[0], x[1], c, s);
+          if (!ok) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = __builtin_nanf("");
+          }
+        }
+        if (NORM) {
+          float(&z)[2][8] = GRAD ? y : x;                  // the head before the norm
+          if (GRAD) {
+            if (live[j]) {
+              w[j][0].get(y[0]);
+              w[j][1].get(y[1]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[0][i] = y[1][i] = 0.f;
+            }
+          }
+          float ss = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) ss += z[0][i] * z[0][i] + z[1][i] * z[1][i];
+          const float r = 1.0f / sqrtf(group_sum<W>(ss) * inv_hd + a.eps);
+          if (!GRAD) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[b][i] *= r * (is_q[j] ? gq[b][i] : gk[b][i]);
+          } else {
+            float dot = 0.f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                y[b][i] *= r;                              // x^
+                const float d = x[b][i] * y[b][i];
+                if (is_q[j]) dgq[b][i] += d;
+                else dgk[b][i] += d;
+                x[b][i] *= is_q[j] ? gq[b][i] : gk[b][i];
+                dot += x[b][i] * y[b][i];
+              }
+            const float mean = group_sum<W>(dot) * inv_hd;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[b][i] = r * (x[b][i] - y[b][i] * mean);
+          }
+        }
+        if (!GRAD) {
+          if (turns) turn_unit<LAYOUT, false>(x[0], x[1], c, s);
+          if (!ok) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = __builtin_nanf("");
+          }
+        }
+        if (live[j]) {
+          Vec8<E>::store(dst[j] + SZ * o0, x[0]);
+          Vec8<E>::store(dst[j] + SZ * o1, x[1]);
+        }
+      }
+    }
+  }
+  if (GRAD && NORM) {
+    // this workgroup's sums of each element, over its slots in their order
+    __shared__ float sum_s[2][kRopeThreads * 16];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = b ? o1 + i : o0 + i;
+        if (on) {
+          sum_s[0][slot * a.hd + e] = dgq[b][i];
+          sum_s[1][slot * a.hd + e] = dgk[b][i];
+        }
+      }
+    __syncthreads();
+    for (int e = tid; e < 2 * a.hd; e += kRopeThreads) {
+      const int kind = e / a.hd, d = e % a.hd;
+      float t = 0.f;
+      for (int q = 0; q < kRopeThreads / W; ++q) t += sum_s[kind][q * a.hd + d];
+      a.part[((size_t)blockIdx.x * 2 + kind) * a.hd + d] = t;
+    }
+  }
+}
+
+// Whether every vector of a tensor is aligned.
+bool vector_fit(const Heads& h, int size, int64_t rows, int heads) {
+  return (reinterpret_cast<uintptr_t>(h.data) & 15) == 0 && (rows == 1 || h.rs * size % 16 == 0) &&
+         (heads == 1 || h.hs * size % 16 == 0);
+}
+
+template <class E>
+bool vectorised(bool grad, const RopeArgs& a) {
+  constexpr int size = sizeof(typename E::T);
+  if (a.hd % 16 || a.hd > 512 || a.rot % 16) return false;
+  auto fit = [&](const Heads& q, const Heads& k) {
+    return vector_fit(q, size, a.rows, a.n_q) && (a.n_k == 0 || vector_fit(k, size, a.rows, a.n_k));
+  };
+  return fit(a.q_in, a.k_in) && fit(a.q_out, a.k_out) && (!grad || !a.q_gain || fit(a.q_x, a.k_x));
+}
+
+// (returns the workgroups launched)
+template <class E, int LAYOUT, bool GRAD, bool NORM, int W>
+int launch_width(const RopeArgs& a, hipStream_t st) {
+  // heads of a row side by side: the power of two that leaves the fewest idle
+  // slots, at least two rounds' loads a lane where there are rows enough
+  const int heads = a.n_q + a.n_k, slots = kRopeThreads / W;
+  int h_step = 1;
+  while (h_step * 2 <= std::min(slots, 16) && (heads + 2 * h_step - 1) / (2 * h_step) * 2 * h_step <= heads + heads / 8) h_step *= 2;
+  while (h_step * 2 <= slots && (int64_t)a.rows * h_step < 2048 && h_step < heads) h_step *= 2;
+  const int row_step = slots / h_step;
+  // gradients of gains: few workgroups, each with a partial sum
+  const int64_t most = GRAD && NORM ? rope_grad_blocks(a) : 1 << 20;
+  const int64_t rows_per_block = ((a.rows + most - 1) / most + row_step - 1) / row_step * row_step;
+  const int blocks = (int)((a.rows + rows_per_block - 1) / rows_per_block);
+  k_rope<E, LAYOUT, GRAD, NORM, W><<<blocks, kRopeThreads, 0, st>>>(a, h_step, (int)rows_per_block);
+  return blocks;
+}
+
+template <class E, int LAYOUT, bool GRAD, bool NORM>
+int launch_vector(const RopeArgs& a, hipStream_t st) {
+  if (a.hd <= 64) return launch_width<E, LAYOUT, GRAD, NORM, 4>(a, st);
+  if (a.hd <= 128) return launch_width<E, LAYOUT, GRAD, NORM, 8>(a, st);
+  if (a.hd <= 256) return launch_width<E, LAYOUT, GRAD, NORM, 16>(a, st);
+  return launch_width<E, LAYOUT, GRAD, NORM, 32>(a, st);
+}
+
 template <class E, int LAYOUT>
 hipError_t launch_layout(bool grad, const RopeArgs& a, float* q_dgain, float* k_dgain, hipStream_t st) {
   const int64_t units = (int64_t)a.rows * (a.n_q + a.n_k);
   const int blocks = (int)std::min<int64_t>((units + 3) / 4, 4096);
+  if (units > 0 && vectorised<E>(grad, a)) {
+    if (!grad) {
+      if (a.q_gain) launch_vector<E, LAYOUT, false, true>(a, st);
+      else launch_vector<E, LAYOUT, false, false>(a, st);
+    } else if (!a.q_gain) {
+      launch_vector<E, LAYOUT, true, false>(a, st);
+    } else {
+      const int blocks = launch_vector<E, LAYOUT, true, true>(a, st);
+      k_rope_gain_sum<<<2 * a.hd, 64, 0, st>>>(a.part, blocks, a.hd, a.n_k, q_dgain, k_dgain);
+    }
+    return hipGetLastError();
+  }
   if (grad && a.q_gain) {
     // (before the rotation: dx may overwrite dy)
     k_rope_gain_any<E, LAYOUT><<<rope_grad_blocks(a), kRopeThreads, 0, st>>>(a);

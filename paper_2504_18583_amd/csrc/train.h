@@ -124,7 +124,7 @@ struct CodLossArgs {
   int* counts;                             // workspace: [kLossCountBlocks][kCodMaxSections]
   int* ticket;                             // workspace: finished sections
 };
-constexpr int kLossCountBlocks = 64;
+constexpr int kLossCountBlocks = 16;
 hipError_t launch_cod_loss(int dtype, const CodLossArgs& a, hipStream_t st);
 
 }  // namespace pard

@@ -295,7 +295,7 @@ pard_status pard_cod_loss(const pard_cod_loss_args* args, void* workspace, size_
   for (int k = 0; a.weights && k < a.n_sections; ++k)
     if (!std::isfinite(a.weights[k])) return PARD_ERR_ARG;
   const int size = elem_size(a.dtype);
-  if (!size || a.rows > 0x7fffffff) return PARD_ERR_UNSUPPORTED;
+  if (!size || a.rows > 0x7fffffff || a.vocab > (1 << 28)) return PARD_ERR_UNSUPPORTED;
   if (!aligned(a.logits, size) || !aligned(a.d_logits, size) || !workspace || !aligned(workspace, 256)) return PARD_ERR_ARG;
   if (workspace_bytes < pard_cod_loss_workspace_bytes(args)) return PARD_ERR_NOMEM;
   CodLossArgs r{};
