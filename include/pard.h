@@ -513,7 +513,7 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads 
  * device, float[1 + n_sections].  Deterministic.
  * Errors: ARG (null pointer, rows < 0, vocab < 1, n_sections outside [1, 64],
  * strides below vocab, non-finite grad_scale or weights), UNSUPPORTED (dtype,
- * 2^31 rows or more), NOMEM (workspace too small), DEVICE. */
+ * above 2^30 rows or a vocab above 2^28), NOMEM (workspace too small), DEVICE. */
 typedef struct {
   int64_t rows;
   int32_t vocab, dtype, n_sections;

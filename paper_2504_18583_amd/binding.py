@@ -285,15 +285,16 @@ def _dtype(t, what: str) -> int:
 
 def _heads(t, what: str, like=None, shape=None) -> pard_heads:
     """A [rows, heads, head_dim] device tensor whose heads are contiguous."""
-    if t.dim() != 3 or not t.is_cuda:
+    st = t.stride()
+    if len(st) != 3 or not t.is_cuda:
         _bad(f"{what}: a [rows, heads, head_dim] device tensor is wanted, got {tuple(t.shape)} on {t.device}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    if st[2] != 1 and t.shape[2] > 1:
         _bad(f"{what}: the elements of a head must be contiguous")
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         _bad(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         _bad(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return pard_heads(t.data_ptr(), t.stride(0), t.stride(1))
+    return pard_heads(t.data_ptr(), st[0], st[1])
 
 
 def _vector(t, what: str, n: int, dtype, device) -> int:
@@ -307,18 +308,20 @@ class _On:
     with that device current: outputs and workspaces made inside belong to the
     stream, and `used` tensors stay alive until it is done with them."""
 
+    __slots__ = ("handle", "stream", "ctx", "used")
+
     def __init__(self, device, stream, *used):
         import torch
-        self.cuda = torch.cuda
-        now = torch.cuda.current_stream(device)
-        self.stream = now if stream is None else stream
-        self.handle = C.c_void_p(self.stream.cuda_stream)
-        self.ctx = None
-        if self.stream != now or torch.cuda.current_device() != self.stream.device_index:
-            if self.stream.device_index != now.device_index:
-                _bad("the stream belongs to another device than the tensors")
-            self.ctx = torch.cuda.stream(self.stream)
-        self.used = used if self.stream != now else ()
+        self.ctx = self.stream = None
+        if stream is None:
+            # (what torch.cuda.current_stream(device).cuda_stream is, without its Python objects)
+            self.handle = torch._C._cuda_getCurrentRawStream(device.index)
+            if torch._C._cuda_getDevice() != device.index:
+                self.ctx = torch.cuda.device(device)
+            return
+        if stream.device_index != device.index:
+            _bad("the stream belongs to another device than the tensors")
+        self.handle, self.ctx, self.stream, self.used = stream.cuda_stream, torch.cuda.stream(stream), stream, used
 
     def __enter__(self):
         if self.ctx is not None:
@@ -326,9 +329,10 @@ class _On:
         return self
 
     def __exit__(self, *exc):
-        for t in self.used:
-            if t is not None:
-                t.record_stream(self.stream)
+        if self.stream is not None:
+            for t in self.used:
+                if t is not None:
+                    t.record_stream(self.stream)
         if self.ctx is not None:
             self.ctx.__exit__(*exc)
 

@@ -2,7 +2,8 @@
 //
 //   CE = log sum exp(x) - x[label];  d x = w (exp(x - lse) - [label]),
 // w the row's share of the loss (1 / its subtask's counted rows, weighted).
-// Three launches: the counted rows of every subtask, the rows, the means.
+// Two launches: the counted rows of every subtask, then the rows, whose last
+// workgroup to end adds the workgroups' sums up (in their order).
 //
 // Bound: memory (the logits in, the gradient out).  So a row is read once: its
 // 16-byte vectors stay in the registers of one workgroup (at most 20 a thread
@@ -15,6 +16,8 @@
 
 namespace pard {
 namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kLossThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -116,6 +119,9 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
   constexpr int C = NV % (16 / N) == 0 ? 16 / N : 1;   // vectors added at a time: 16 logits
   __shared__ float m_s[2][W], l_s[2][W];
   __shared__ int n_s[kCodMaxSections];
+  __shared__ double sum_s[kCodMaxSections];          // this workgroup's losses, in its rows' order
+  __shared__ int last_s;
+  for (int q = threadIdx.x; q < a.n_sections; q += T) sum_s[q] = 0.0;
   load_counts(a, n_s);
   int n_all = 0;
   for (int q = 0; q < a.n_sections; ++q) n_all += n_s[q];
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
     label = a.labels[r];
   };
   const int rounds = RESIDENT ? 1 : (a.vocab / N + NV * T - 1) / (NV * T);
-  if (RESIDENT) {
+  if (RESIDENT && (int)blockIdx.x < a.rows) {
     shape(blockIdx.x);
 #pragma unroll
     for (int i = 0; i < NV; ++i) fetch(row_of(blockIdx.x), 0, i);
@@ -201,7 +207,11 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
     l = l_s[turn][0];
     for (int w = 1; w < W; ++w) join(m, l, m_s[turn][w], l_s[turn][w]);
     const float lse2 = m + log2f(l);
-    if (tid == 0) a.row_loss[r] = k > 0 ? lse2 * kLn2 - x_label : 0.f;
+    if (tid == 0) {
+      const float ce = k > 0 ? lse2 * kLn2 - x_label : 0.f;
+      if (a.row_loss) a.row_loss[r] = ce;
+      if (k > 0) sum_s[k - 1] += ce;
+    }
     if (!RESIDENT && !d) continue;
     const float w = k == 0 ? 0.f : label >= a.vocab ? __builtin_nanf("")
                            : a.weighted ? a.weights[k - 1] * a.grad_scale / n_s[k - 1] : a.grad_scale / n_all;
@@ -230,7 +240,9 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
 #pragma unroll
             for (int j = 0; j < N; ++j) d[head_now + at * N + j] = E::store(g[j]);
           } else {
-            *const_cast<Vec*>(vec_at(d_base, q * NV + i)) = Vec::pack(g);
+            const Vec out = Vec::pack(g);
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, out.v),
+                                        reinterpret_cast<u32x4*>(const_cast<Vec*>(vec_at(d_base, q * NV + i))));
           }
         }
         if (RESIDENT) fetch(next, 0, i);
@@ -245,61 +257,61 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
       if (own) d[label] = E::store(w * (exp2f(x_label * kLog2e - lse2) - 1.f));
     }
   }
-}
 
-// Workgroup k - 1: subtask k's mean; the last one to end adds the means up.
-__global__ __launch_bounds__(1024) void k_loss_mean(const CodLossArgs a) {
-  __shared__ double s_s[16];
-  __shared__ int n_s[kCodMaxSections];
-  load_counts(a, n_s);
-  const int k = blockIdx.x + 1;
-  double s = 0.0;
-  for (int64_t r = threadIdx.x; r < a.rows; r += 1024)
-    if (section_of(a, (int)r) == k) s += a.row_loss[r];
-  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
-  if ((threadIdx.x & 63) == 0) s_s[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  s = 0.0;
-  for (int w = 0; w < 16; ++w) s += s_s[w];
-  const int n = n_s[k - 1];
-  __hip_atomic_store(&a.loss[k], n ? (float)(s / n) : 0.f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  if (__hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) != a.n_sections - 1) return;
-  double total = 0.0;
-  int64_t all = 0;
-  for (int q = 1; q <= a.n_sections; ++q) {
-    const double mean = __hip_atomic_load(&a.loss[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    total += a.weighted ? a.weights[q - 1] * mean : n_s[q - 1] * mean;
-    all += n_s[q - 1];
+  // the workgroups' sums: [workgroup][subtask]
+  // (device-scope stores, complete before the ticket, and device-scope loads
+  // after it: a release and an acquire would write back and drop whole caches)
+  if (tid == 0) {
+    for (int q = 0; q < a.n_sections; ++q)
+      __hip_atomic_store(&a.sums[(size_t)blockIdx.x * a.n_sections + q], sum_s[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
+    asm volatile("" ::: "memory");
+    last_s = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
   }
-  a.loss[0] = (float)(a.weighted ? total : all ? total / all : 0.0);
+  __syncthreads();
+  if (!last_s) return;                               // uniform
+  for (int q = wave; q < a.n_sections; q += W) {     // a wavefront a subtask
+    double s = 0.0;
+    for (int b = lane; b < (int)gridDim.x; b += 64)
+      s += __hip_atomic_load(&a.sums[(size_t)b * a.n_sections + q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+    if (lane == 0) {
+      sum_s[q] = s;
+      a.loss[1 + q] = n_s[q] ? (float)(s / n_s[q]) : 0.f;
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    double total = 0.0;
+    for (int q = 0; q < a.n_sections; ++q) total += a.weighted ? (n_s[q] ? a.weights[q] * (sum_s[q] / n_s[q]) : 0.0) : sum_s[q];
+    a.loss[0] = (float)(a.weighted ? total : n_all ? total / n_all : 0.0);
+  }
 }
 
 template <class E, int T, int NV, bool RESIDENT, bool SCALAR_OUT = false>
 void launch_variant(const CodLossArgs& a, hipStream_t st) {
   // resident rows: as many workgroups as the device holds at once (of 1024
   // threads one a CU, of 256 eight), each with several rows
-  const int most = !RESIDENT ? 1 << 20 : T == 1024 ? 256 : 2048;
-  k_loss_row<E, T, NV, RESIDENT, SCALAR_OUT><<<std::min(a.rows, most), T, 0, st>>>(a);
+  const int most = !RESIDENT ? kLossMaxBlocks : T == 1024 ? 256 : 2048;
+  k_loss_row<E, T, NV, RESIDENT, SCALAR_OUT><<<std::max(1, std::min(a.rows, most)), T, 0, st>>>(a);
 }
 
 template <class E>
 hipError_t launch_rows(const CodLossArgs& a, hipStream_t st) {
   constexpr int N = LossVec<E>::N, SZ = 16 / N;
   k_loss_count<<<kLossCountBlocks, kLossThreads, 0, st>>>(a);
-  if (a.rows > 0) {
-    const int n = (a.vocab + N - 1) / N;             // vectors of a row
-    const bool same = !a.d_logits || ((a.logits - a.d_logits) % 16 == 0 && (a.rows == 1 || (a.stride - a.d_stride) * SZ % 16 == 0));
-    if (!same) launch_variant<E, 1024, 4, false, true>(a, st);
-    else if (!a.d_logits || n > 20480) n <= 1024 ? launch_variant<E, 256, 4, false>(a, st) : launch_variant<E, 1024, 8, false>(a, st);
-    else if (n <= 256) launch_variant<E, 256, 1, true>(a, st);
-    else if (n <= 1024) launch_variant<E, 256, 4, true>(a, st);
-    else if (n <= 4096) launch_variant<E, 1024, 4, true>(a, st);
-    else if (n <= 8192) launch_variant<E, 1024, 8, true>(a, st);
-    else if (n <= 16384) launch_variant<E, 1024, 16, true>(a, st);
-    else launch_variant<E, 1024, 20, true>(a, st);
-  }
-  k_loss_mean<<<a.n_sections, 1024, 0, st>>>(a);
+  const int n = (a.vocab + N - 1) / N;               // vectors of a row
+  const bool same = !a.d_logits || ((a.logits - a.d_logits) % 16 == 0 && (a.rows == 1 || (a.stride - a.d_stride) * SZ % 16 == 0));
+  if (!same) launch_variant<E, 1024, 4, false, true>(a, st);
+  else if (!a.d_logits || n > 20480) n <= 1024 ? launch_variant<E, 256, 4, false>(a, st) : launch_variant<E, 512, 8, false>(a, st);
+  else if (n <= 256) launch_variant<E, 256, 1, true>(a, st);
+  else if (n <= 1024) launch_variant<E, 256, 4, true>(a, st);
+  else if (n <= 4096) launch_variant<E, 1024, 4, true>(a, st);
+  else if (n <= 8192) launch_variant<E, 1024, 8, true>(a, st);
+  else if (n <= 16384) launch_variant<E, 1024, 16, true>(a, st);
+  else launch_variant<E, 1024, 20, true>(a, st);
   return hipGetLastError();
 }
 

@@ -122,8 +122,10 @@ struct CodLossArgs {
   float weights[kCodMaxSections];
   float *loss, *row_loss;
   int* counts;                             // workspace: [kLossCountBlocks][kCodMaxSections]
-  int* ticket;                             // workspace: finished sections
+  int* ticket;                             // workspace: finished workgroups
+  double* sums;                            // workspace: [workgroups][n_sections]
 };
+constexpr int kLossMaxBlocks = 4096;       // workgroups of the rows
 constexpr int kLossCountBlocks = 16;
 hipError_t launch_cod_loss(int dtype, const CodLossArgs& a, hipStream_t st);
 

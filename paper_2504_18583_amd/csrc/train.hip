@@ -115,15 +115,15 @@ bool loss_ok(const pard_cod_loss_args* a) {
   return a && a->rows >= 0 && a->vocab >= 1 && a->n_sections >= 1 && a->n_sections <= kCodMaxSections;
 }
 
-// Workspace of the loss: partial counts, the ticket, the rows' losses.
+// Workspace of the loss: partial counts, the ticket, the workgroups' sums.
 size_t loss_layout(const pard_cod_loss_args* a, char* base, CodLossArgs* r) {
   const size_t counts = align256(sizeof(int) * kLossCountBlocks * kCodMaxSections);
   if (r) {
     r->counts = reinterpret_cast<int*>(base);
     r->ticket = reinterpret_cast<int*>(base + counts);
-    if (!r->row_loss) r->row_loss = reinterpret_cast<float*>(base + counts + 256);
+    r->sums = reinterpret_cast<double*>(base + counts + 256);
   }
-  return counts + 256 + (a->row_loss ? 0 : align256(sizeof(float) * (size_t)a->rows));
+  return counts + 256 + align256(sizeof(double) * kLossMaxBlocks * a->n_sections);
 }
 
 }  // namespace
@@ -295,7 +295,7 @@ pard_status pard_cod_loss(const pard_cod_loss_args* args, void* workspace, size_
   for (int k = 0; a.weights && k < a.n_sections; ++k)
     if (!std::isfinite(a.weights[k])) return PARD_ERR_ARG;
   const int size = elem_size(a.dtype);
-  if (!size || a.rows > 0x7fffffff || a.vocab > (1 << 28)) return PARD_ERR_UNSUPPORTED;
+  if (!size || a.rows > (1 << 30) || a.vocab > (1 << 28)) return PARD_ERR_UNSUPPORTED;
   if (!aligned(a.logits, size) || !aligned(a.d_logits, size) || !workspace || !aligned(workspace, 256)) return PARD_ERR_ARG;
   if (workspace_bytes < pard_cod_loss_workspace_bytes(args)) return PARD_ERR_NOMEM;
   CodLossArgs r{};
