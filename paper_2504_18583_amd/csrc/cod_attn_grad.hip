@@ -7,10 +7,10 @@
 //   k_cod_dq  as the forward kernel: a workgroup owns 64 NQ (row, head) pairs of
 //     a key head and walks their keys.  It also leaves lse, delta, the real
 //     tokens seen and the place of every pair, in pair order, for the other.
-//   k_cod_dkv  a workgroup owns 128 real tokens of a key head (K and V in operand
+//   k_cod_dkv  a workgroup owns 64 NK real tokens of a key head (K and V in operand
 //     registers) and walks the pairs that see them, all heads of the group, in
 //     stages through LDS.  Mask rows are seen by the rows of
-//     their chain alone: workgroups behind those own 128 places of the order and
+//     their chain alone: workgroups behind those own 64 places of the order and
 //     walk the pairs from the first place to the last chain's end.
 #include "cod_attn_tile.h"
 
@@ -22,6 +22,10 @@ namespace {
 using namespace cod;
 
 constexpr int kStage = 64;                           // keys of a stage (dq)
+constexpr int kPairs = 64;                           // pairs of a stage (dkv)
+// Blocks of 16 keys of a dkv wavefront: at head_dim 128 the sums of two, with K
+// and V, leave too few registers.
+constexpr int dkv_blocks(int hd) { return hd == 64 ? 2 : 1; }
 
 // Statistics of 64 pairs of one key head: base-2 log-sum (+infinity past the
 // sample: probability 0), -delta, real tokens seen, place in the order.
@@ -34,9 +38,9 @@ struct PairStats {
 __device__ __forceinline__ int64_t stats_base(const CodAttnArgs& a, int64_t off, int sample) {
   return off * a.group / 64 + sample;
 }
-// Blocks of one key head; a stage may read one past its sample's.
+// Blocks of one key head.
 __host__ __device__ inline int64_t stats_blocks(int64_t rows, int group, int n_samples) {
-  return rows * group / 64 + n_samples + 2;
+  return rows * group / 64 + n_samples + 1;
 }
 
 template <int HD, int NQ, class M>
@@ -249,13 +253,14 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   }
 }
 
-// dK and dV of NK blocks of 16 keys (operands kf and vf(k, ks)) over 32 pairs in
-// two LDS blocks each of Q and dO, the pairs i0 .. of statistics st; if masked,
+// dK and dV of NK blocks of 16 keys (operands kf, vf) over 32 pairs in two LDS
+// blocks each of Q and dO, the pairs i0 .. of statistics st; if masked,
 // key block k of this lane is hidden from the pairs for whose `by` entry (st.seen
 // or st.pos) hidden(k, entry) holds.  dO V^T starts from -delta.
-template <int HD, int NK, class M, class V, class H>
+template <int HD, int NK, class M, class H>
 __device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const PairStats& st, int i0,
-                                         const u32x4 (&kf)[NK][HD / 32], V&& vf, f32x4 (&dk)[NK][HD / 16],
+                                         const u32x4 (&kf)[NK][HD / 32],
+                                         const u32x4 (&vf)[NK][HD / 32], f32x4 (&dk)[NK][HD / 16],
                                          f32x4 (&dv)[NK][HD / 16], float scale2, int lane, bool masked, const int* by,
                                          H&& hidden) {
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
@@ -277,7 +282,7 @@ __device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
         sc[k] = M::mma(qf, kf[k][ks], sc[k]);
-        dp[k] = M::mma(gf, vf(k, ks), dp[k]);
+        dp[k] = M::mma(gf, vf[k][ks], dp[k]);
       }
     }
     float x[NK][4];
@@ -325,95 +330,76 @@ __device__ __forceinline__ void store_dkv(const CodAttnArgs& a, uint32_t row, in
   }
 }
 
-// Eight wavefronts.  Real tokens: wavefront w has keys 32 (w % 4) .. of the
-// workgroup's 128 and half w / 4 of every stage's pairs; the halves are added at
-// the end.  Mask rows: wavefront w has 16 of 128 places and all pairs.  The pairs
-// are walked from the last to the first, so that the tiles of a sample, which all
-// end with its last pair, read the same stages at the same time.
+// Four wavefronts, of which several workgroups share a CU: between two barriers a
+// wavefront's LDS reads, products and exponentials follow each other, and other
+// workgroups fill the units meanwhile.  Real tokens: wavefront w has keys 16 NK w
+// .. of the workgroup's 64 NK; mask rows: 16 of 64 places.  The pairs are walked
+// from the last to the first, so that the tiles of a sample, which all end with
+// its last pair, read the same stages at the same time.
 template <int HD, class M>
-__global__ __launch_bounds__(512, 2) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
-  constexpr int NK = 2, KW = 16 * NK;                // keys per wavefront
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
+  constexpr int NK = dkv_blocks(HD), KW = 16 * NK;   // keys per wavefront
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
-  // a stage: SP pairs, their blocks of Q and of dO (32 KiB in all) and statistics;
-  // a ring of three stages, in arrays of their own
-  constexpr int SP = HD == 64 ? 128 : 64, SB = SP / 16, SU = 2 * SB * BU + SP;
-  // at head_dim 128 the real tokens' V stays in LDS (in registers it would leave too few)
-  constexpr bool VL = HD == 128;
-  __shared__ __attribute__((aligned(16))) u32x4 b0[SU], b1[SU], b2[SU], v_s[VL ? 8 * BU : 1];
+  // a stage: four blocks of Q, four of dO, the pairs' statistics; two arrays of
+  // their own
+  constexpr int SU = 8 * BU + 64;
+  __shared__ __attribute__((aligned(16))) u32x4 b0[SU], b1[SU];
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = a.group;
   const float scale2 = a.scale * kLog2e;
   const bool real = blockIdx.x < real_blocks;        // uniform
   const unsigned id = real ? blockIdx.x : blockIdx.x - real_blocks;
-  const int kvh = id % a.n_kv;
-  const CodTileInfo tile = a.plan.by_sample[id / a.n_kv];
+  const int keys = real ? 4 * KW : 64, per_tile = kCodTile / keys;
+  const int kvh = id % a.n_kv, rest = id / a.n_kv;
+  const CodTileInfo tile = a.plan.by_sample[rest / per_tile];
   const CodSampleInfo s = tile.s;
   const int4* const order = a.plan.order + s.off;
-  const int last = s.len - 1, n_pairs = s.len * group, t0 = tile.tile * kCodTile;
+  const int last = s.len - 1, n_pairs = s.len * group;
+  const int t0 = tile.tile * kCodTile + rest % per_tile * keys;
   if (t0 >= (real ? s.n_real : s.cap)) return;       // uniform
   const PairStats* const stats =
       reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.sample);
 
   // Stages: a wavefront loads 16 pairs (past the sample: its last row) of Q and of
-  // dO (HD 64), or wavefronts 0 .. 3 of Q and 4 .. 7 of dO, and part of the
-  // statistics.  Data is loaded two stages ahead, the packed rows that it is at
-  // four: a wavefront's loads go out in one fixed order, packed rows before data,
-  // so that the wait for a stage's data covers the rows of the stage two on and
-  // leaves the newer loads in flight.  Stages past the first repeat it.
-  const int part = wave % SB, in_stage = part * 16 + block_row(lane);
-  auto fence = [&]() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+  // dO, and a quarter of the statistics; the packed rows that a stage is at are
+  // read a stage before its loads.
+  const int in_stage = wave * 16 + block_row(lane);
   auto stages = [&](int st0, int st1, auto step) __attribute__((always_inline)) {
-    constexpr int ND = (SB == 8 ? 2 : 1) * (HD / 32) + 1;   // data loads of a stage and wavefront
-    int packed[3];
-    auto find = [&](int slot, int st) __attribute__((always_inline)) {
-      packed[slot] = order[min(quotient(max(st, st0) * SP + in_stage, a.by_group), last)].x;
-      fence();
+    int packed = 0;
+    auto find = [&](int st) __attribute__((always_inline)) {
+      packed = order[min(quotient(max(st, st0) * kPairs + in_stage, a.by_group), last)].x;
     };
-    auto load = [&](u32x4* buf, int slot, int at_stage) __attribute__((always_inline)) {
-      const int st = max(at_stage, st0), x = st * SP + in_stage;
-      const uint32_t head = kvh * group + remainder(x, quotient(x, a.by_group), a.by_group), r = s.off + packed[slot];
-      if (SB == 8 || wave < 4) load_block<HD>(at(a.q, r, head) + block_byte(lane), buf + part * BU);
-      if (SB == 8 || wave >= 4) load_block<HD>(at(a.d_out, r, head) + block_byte(lane), buf + (SB + part) * BU);
+    auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
+      const int x = st * kPairs + in_stage;
+      const uint32_t head = kvh * group + remainder(x, quotient(x, a.by_group), a.by_group), r = s.off + packed;
+      load_block<HD>(at(a.q, r, head) + block_byte(lane), buf + wave * BU);
+      load_block<HD>(at(a.d_out, r, head) + block_byte(lane), buf + (4 + wave) * BU);
       __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st * (SP / 64)) + part * 256 + lane * 4),
-          (__attribute__((address_space(3))) void*)(buf + 2 * SB * BU + part * 16), 4, 0, 0);
-      fence();
+          (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st) + wave * 256 + lane * 4),
+          (__attribute__((address_space(3))) void*)(buf + 8 * BU + wave * 16), 4, 0, 0);
+      find(st - 1);
     };
-    find(0, st1 - 1);
-    find(1, st1 - 2);
-    find(2, st1 - 3);
-    load(b0, 0, st1 - 1);
-    find(0, st1 - 4);
-    load(b1, 1, st1 - 2);
-    // stage st (ring phase ph): its buffer cur; the one of the stage before it
-    // (read before the last barrier) takes the stage two on
-    auto one = [&](int st, int ph, const u32x4* cur, u32x4* dst) __attribute__((always_inline)) {
-      fence();
-      __builtin_amdgcn_s_waitcnt(vm_wait(ND + 1));
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      fence();
-      find((ph + 1) % 3, st - 4);
-      load(dst, (ph + 2) % 3, st - 2);
-      if (st >= st0) step(st, cur, reinterpret_cast<const PairStats*>(cur + 2 * SB * BU));   // uniform
+    auto one = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
+      wait_and_meet();
+      if (st > st0) load(nxt, st - 1);               // uniform
+      __builtin_amdgcn_sched_barrier(0);
+      step(st, cur, *reinterpret_cast<const PairStats*>(cur + 8 * BU));
     };
-    for (int st = st1 - 1; st >= st0; st -= 3) {
-      one(st, 0, b0, b2);
-      one(st - 1, 1, b1, b0);
-      one(st - 2, 2, b2, b1);
+    find(st1 - 1);
+    load(b0, st1 - 1);
+    int st = st1 - 1;
+    for (; st > st0; st -= 2) {
+      one(st, b0, b1);
+      one(st - 1, b1, b0);
     }
-    wait_all();                                      // (the loads still in flight, before LDS is used again)
+    if (st == st0) one(st, b0, b1);
   };
 
   if (real) {
-    const int kw = wave & 3, half = wave >> 2;       // this wavefront's keys and pairs
-    const int w0 = t0 + kw * KW;
-    u32x4 kf[NK][KS], vr[VL ? 1 : NK][VL ? 1 : KS];
+    const int w0 = t0 + wave * KW;                   // this wavefront's first key
+    u32x4 kf[NK][KS], vf[NK][KS];
     f32x4 dk[NK][DB], dv[NK][DB];
-    if (VL) load_block<HD>(at(a.v, s.off + min(t0 + wave * 16 + block_row(lane), s.n_real - 1), kvh) + block_byte(lane),
-                           v_s + (VL ? wave * BU : 0));
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
       const uint32_t key = s.off + min(w0 + k * 16 + c16, s.n_real - 1);
@@ -422,50 +408,29 @@ __global__ __launch_bounds__(512, 2) void k_cod_dkv(const CodAttnArgs a, unsigne
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         kf[k][ks] = *reinterpret_cast<const u32x4*>(ks_ + ks * 64);
-        if (!VL) vr[VL ? 0 : k][VL ? 0 : ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
+        vf[k][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) dk[k][db] = dv[k][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const auto vf = [&](int k, int ks) __attribute__((always_inline)) {
-      return VL ? rows_frag(v_s + (2 * kw + k) * BU, ks, lane) : vr[VL ? 0 : k][VL ? 0 : ks];
-    };
     // pairs from which on this wavefront's first and last key are seen
     const int* const first = a.plan.first + s.off;
     const int from = first[min(w0, s.n_real - 1)] * group, free = first[min(w0 + KW, s.n_real) - 1] * group;
-    stages(first[t0] * group / SP, (n_pairs + SP - 1) / SP,
-           [&](int st, const u32x4* cur, const PairStats* ps) __attribute__((always_inline)) {
+    stages(first[t0] * group / kPairs, (n_pairs + kPairs - 1) / kPairs,
+           [&](int st, const u32x4* cur, const PairStats& ps) __attribute__((always_inline)) {
 #pragma unroll 1
-             for (int h = half * (SP / 64); h < (half + 1) * (SP / 64); ++h) {
-               const int c0 = st * SP + h * 32;
-               if (c0 + 32 <= from || c0 >= n_pairs) continue;   // uniform: no pair that sees this wavefront's keys
-               const PairStats& stat = ps[h / 2];
+             for (int h = 0; h < 2; ++h) {
+               const int c0 = st * kPairs + h * 32;
+               if (c0 + 32 <= from) continue;        // uniform: no pair sees this wavefront's keys
                // (before `free` some pair does not see some key)
-               dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (SB + 2 * h) * BU, stat, h % 2 * 32, kf, vf, dk, dv, scale2, lane,
-                                   c0 < free, stat.seen, [&](int k, int seen) { return seen <= w0 + k * 16 + c16; });
+               dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (4 + 2 * h) * BU, ps, h * 32, kf, vf, dk, dv, scale2, lane,
+                                   c0 < free, ps.seen, [&](int k, int seen) { return seen <= w0 + k * 16 + c16; });
              }
            });
-    // the second half's sums through LDS: dK, then dV (a wavefront's in half a buffer)
-    static_assert(2 * NK * DB * 64 <= SU, "two slots in a buffer");
-    f32x4* const slot = reinterpret_cast<f32x4*>(kw & 2 ? b1 : b0) + (kw & 1) * NK * DB * 64 + lane;
-    auto add_halves = [&](f32x4 (&x)[NK][DB]) __attribute__((always_inline)) {
-      __syncthreads();
-      if (half) {                                    // uniform
-#pragma unroll
-        for (int i = 0; i < NK * DB; ++i) slot[i * 64] = x[i / DB][i % DB];
-      }
-      __syncthreads();
-      if (!half) {
-#pragma unroll
-        for (int i = 0; i < NK * DB; ++i) x[i / DB][i % DB] += slot[i * 64];
-      }
-    };
-    add_halves(dk);
-    add_halves(dv);
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
       const int key = w0 + k * 16 + c16;
-      if (!half && key < s.n_real) store_dkv<HD, M>(a, s.off + key, kvh, dk[k], dv[k], g4);
+      if (key < s.n_real) store_dkv<HD, M>(a, s.off + key, kvh, dk[k], dv[k], g4);
     }
     return;
   }
@@ -479,26 +444,24 @@ __global__ __launch_bounds__(512, 2) void k_cod_dkv(const CodAttnArgs a, unsigne
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[0][db] = dv[0][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (t0 <= last) {                                  // uniform
-    u32x4 kf[1][KS], vr[KS];
+    u32x4 kf[1][KS], vf[1][KS];
     const uint32_t r = s.off + (mine <= last ? e.x : 0);
     const char* const ks_ = at(a.k, r, kvh) + g4 * 16;
     const char* const vs_ = at(a.v, r, kvh) + g4 * 16;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       kf[0][ks] = *reinterpret_cast<const u32x4*>(ks_ + ks * 64);
-      vr[ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
+      vf[0][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
     }
-    const auto vf = [&](int, int ks) __attribute__((always_inline)) { return vr[ks]; };
     const int from = w0 * group, end = w0 <= last ? order[min(w0 + 15, last)].w * group : 0;   // this wavefront's pairs
-    stages(t0 * group / SP, (order[min(t0 + kCodTile - 1, last)].w * group + SP - 1) / SP,
-           [&](int st, const u32x4* cur, const PairStats* ps) __attribute__((always_inline)) {
+    stages(t0 * group / kPairs, (order[min(t0 + 63, last)].w * group + kPairs - 1) / kPairs,
+           [&](int st, const u32x4* cur, const PairStats& ps) __attribute__((always_inline)) {
 #pragma unroll 1
-             for (int h = 0; h < SP / 32; ++h) {
-               const int c0 = st * SP + h * 32;
+             for (int h = 0; h < 2; ++h) {
+               const int c0 = st * kPairs + h * 32;
                if (c0 >= end || c0 + 32 <= from) continue;   // uniform
-               const PairStats& stat = ps[h / 2];
-               dkv_step<HD, 1, M>(cur + 2 * h * BU, cur + (SB + 2 * h) * BU, stat, h % 2 * 32, kf, vf, dk, dv, scale2, lane,
-                                  true, stat.pos, [&](int, int pos) { return (uint32_t)(pos - mine) >= chain_left; });
+               dkv_step<HD, 1, M>(cur + 2 * h * BU, cur + (4 + 2 * h) * BU, ps, h * 32, kf, vf, dk, dv, scale2, lane, true,
+                                  ps.pos, [&](int, int pos) { return (uint32_t)(pos - mine) >= chain_left; });
              }
            });
   }
@@ -513,9 +476,10 @@ template <int HD, class M>
 hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
   constexpr int NQ = 2;
   const int64_t tiles = (int64_t)a.n_tiles * a.n_kv, dq = tiles * (kCodTile / (64 * NQ)) * a.group;
-  if (dq > 0x7fffffff || 2 * tiles > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t real = tiles * (kCodTile / (64 * dkv_blocks(HD))), all = real + tiles * (kCodTile / 64);
+  if (dq > 0x7fffffff || all > 0x7fffffff) return hipErrorInvalidValue;
   k_cod_dq<HD, NQ, M><<<(unsigned)dq, 256, 0, st>>>(a);
-  k_cod_dkv<HD, M><<<(unsigned)(2 * tiles), 512, 0, st>>>(a, (unsigned)tiles);
+  k_cod_dkv<HD, M><<<(unsigned)all, 256, 0, st>>>(a, (unsigned)real);
   return hipGetLastError();
 }
 
