@@ -22,10 +22,11 @@ namespace {
 using namespace cod;
 
 constexpr int kStage = 64;                           // keys of a stage (dq)
-constexpr int kPairs = 64;                           // pairs of a stage (dkv)
 // Blocks of 16 keys of a dkv wavefront: at head_dim 128 the sums of two, with K
 // and V, leave too few registers.
 constexpr int dkv_blocks(int hd) { return hd == 64 ? 2 : 1; }
+// Pairs of a stage (dkv): three workgroups' stages fit a CU's LDS.
+constexpr int dkv_pairs(int hd) { return hd == 64 ? 64 : 32; }
 
 // Statistics of 64 pairs of one key head: base-2 log-sum (+infinity past the
 // sample: probability 0), -delta, real tokens seen, place in the order.
@@ -337,12 +338,12 @@ __device__ __forceinline__ void store_dkv(const CodAttnArgs& a, uint32_t row, in
 // from the last to the first, so that the tiles of a sample, which all end with
 // its last pair, read the same stages at the same time.
 template <int HD, class M>
-__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
+__global__ __launch_bounds__(256, 3) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
   constexpr int NK = dkv_blocks(HD), KW = 16 * NK;   // keys per wavefront
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
-  // a stage: four blocks of Q, four of dO, the pairs' statistics; two arrays of
-  // their own
-  constexpr int SU = 8 * BU + 64;
+  // a stage: SB blocks of Q, SB of dO, the pairs' statistics (of 64); two arrays
+  // of their own
+  constexpr int SP = dkv_pairs(HD), SB = SP / 16, SU = 2 * SB * BU + 64;
   __shared__ __attribute__((aligned(16))) u32x4 b0[SU], b1[SU];
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -362,29 +363,29 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_cod_dkv(const CodAttn
       reinterpret_cast<const PairStats*>(a.stats) + kvh * a.stats_blocks + stats_base(a, s.off, tile.sample);
 
   // Stages: a wavefront loads 16 pairs (past the sample: its last row) of Q and of
-  // dO, and a quarter of the statistics; the packed rows that a stage is at are
-  // read a stage before its loads.
-  const int in_stage = wave * 16 + block_row(lane);
+  // dO, or of one of them, and a quarter of the statistics; the packed rows that a
+  // stage is at are read a stage before its loads.
+  const int part = wave % SB, in_stage = part * 16 + block_row(lane);
   auto stages = [&](int st0, int st1, auto step) __attribute__((always_inline)) {
     int packed = 0;
     auto find = [&](int st) __attribute__((always_inline)) {
-      packed = order[min(quotient(max(st, st0) * kPairs + in_stage, a.by_group), last)].x;
+      packed = order[min(quotient(max(st, st0) * SP + in_stage, a.by_group), last)].x;
     };
     auto load = [&](u32x4* buf, int st) __attribute__((always_inline)) {
-      const int x = st * kPairs + in_stage;
+      const int x = st * SP + in_stage;
       const uint32_t head = kvh * group + remainder(x, quotient(x, a.by_group), a.by_group), r = s.off + packed;
-      load_block<HD>(at(a.q, r, head) + block_byte(lane), buf + wave * BU);
-      load_block<HD>(at(a.d_out, r, head) + block_byte(lane), buf + (4 + wave) * BU);
+      if (SB == 4 || wave < 2) load_block<HD>(at(a.q, r, head) + block_byte(lane), buf + part * BU);
+      if (SB == 4 || wave >= 2) load_block<HD>(at(a.d_out, r, head) + block_byte(lane), buf + (SB + part) * BU);
       __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st) + wave * 256 + lane * 4),
-          (__attribute__((address_space(3))) void*)(buf + 8 * BU + wave * 16), 4, 0, 0);
+          (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(stats + st * SP / 64) + wave * 256 + lane * 4),
+          (__attribute__((address_space(3))) void*)(buf + 2 * SB * BU + wave * 16), 4, 0, 0);
       find(st - 1);
     };
     auto one = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
       wait_and_meet();
       if (st > st0) load(nxt, st - 1);               // uniform
       __builtin_amdgcn_sched_barrier(0);
-      step(st, cur, *reinterpret_cast<const PairStats*>(cur + 8 * BU));
+      step(st, cur, *reinterpret_cast<const PairStats*>(cur + 2 * SB * BU));
     };
     find(st1 - 1);
     load(b0, st1 - 1);
@@ -416,14 +417,14 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_cod_dkv(const CodAttn
     // pairs from which on this wavefront's first and last key are seen
     const int* const first = a.plan.first + s.off;
     const int from = first[min(w0, s.n_real - 1)] * group, free = first[min(w0 + KW, s.n_real) - 1] * group;
-    stages(first[t0] * group / kPairs, (n_pairs + kPairs - 1) / kPairs,
+    stages(first[t0] * group / SP, (n_pairs + SP - 1) / SP,
            [&](int st, const u32x4* cur, const PairStats& ps) __attribute__((always_inline)) {
 #pragma unroll 1
-             for (int h = 0; h < 2; ++h) {
-               const int c0 = st * kPairs + h * 32;
+             for (int h = 0; h < SP / 32; ++h) {
+               const int c0 = st * SP + h * 32;
                if (c0 + 32 <= from) continue;        // uniform: no pair sees this wavefront's keys
                // (before `free` some pair does not see some key)
-               dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (4 + 2 * h) * BU, ps, h * 32, kf, vf, dk, dv, scale2, lane,
+               dkv_step<HD, NK, M>(cur + 2 * h * BU, cur + (SB + 2 * h) * BU, ps, c0 % 64, kf, vf, dk, dv, scale2, lane,
                                    c0 < free, ps.seen, [&](int k, int seen) { return seen <= w0 + k * 16 + c16; });
              }
            });
@@ -454,13 +455,13 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_cod_dkv(const CodAttn
       vf[0][ks] = *reinterpret_cast<const u32x4*>(vs_ + ks * 64);
     }
     const int from = w0 * group, end = w0 <= last ? order[min(w0 + 15, last)].w * group : 0;   // this wavefront's pairs
-    stages(t0 * group / kPairs, (order[min(t0 + 63, last)].w * group + kPairs - 1) / kPairs,
+    stages(t0 * group / SP, (order[min(t0 + 63, last)].w * group + SP - 1) / SP,
            [&](int st, const u32x4* cur, const PairStats& ps) __attribute__((always_inline)) {
 #pragma unroll 1
-             for (int h = 0; h < 2; ++h) {
-               const int c0 = st * kPairs + h * 32;
+             for (int h = 0; h < SP / 32; ++h) {
+               const int c0 = st * SP + h * 32;
                if (c0 >= end || c0 + 32 <= from) continue;   // uniform
-               dkv_step<HD, 1, M>(cur + 2 * h * BU, cur + (4 + 2 * h) * BU, ps, h * 32, kf, vf, dk, dv, scale2, lane, true,
+               dkv_step<HD, 1, M>(cur + 2 * h * BU, cur + (SB + 2 * h) * BU, ps, c0 % 64, kf, vf, dk, dv, scale2, lane, true,
                                   ps.pos, [&](int, int pos) { return (uint32_t)(pos - mine) >= chain_left; });
              }
            });
