@@ -65,7 +65,8 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   const int chain0 = max(w_row0 - s.reach, 0);
   int row[NQ], head[NQ];                             // this pair's place and query head
   int4 e[NQ] = {};                                   // packed row, real tokens seen, first mask row seen (and chain's end)
-  float lse2[NQ], delta[NQ];
+  float lse2[NQ];
+  f32x4 ndelta[NQ];                                  // -delta, as dO V^T starts from
   u32x4 q[NQ][KS], go[NQ][KS];
   f32x4 dq[NQ][DB];
 #pragma unroll
@@ -132,20 +133,20 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
           sum = fmaf(x[1], y[1], sum);
         }
       }
-      delta[t] = sum4g(sum);
+      const float delta = sum4g(sum);
+      ndelta[t] = f32x4{-delta, -delta, -delta, -delta};
       const int in_sample = p0 * group + pair0 + wave * QW + t * 16 + c16;   // (below 2^30)
       if (g4 == 0 && (in_sample & ~63) < s.len * group) {
         PairStats& st = reinterpret_cast<PairStats*>(a.stats)[kvh * a.stats_blocks + stats_base(a, s.off, tile.sample) + in_sample / 64];
         const int i = in_sample & 63;
         st.lse2[i] = row[t] <= last ? lse2[t] : INFINITY;
-        st.ndelta[i] = -delta[t];
+        st.ndelta[i] = -delta;
         st.seen[i] = e[t].y;
         st.pos[i] = min(row[t], last);
       }
     }
 
-    // dQ += dS K over 32 keys: their scores and dO V^T products are in sc and
-    // dp, K in two LDS blocks; hidden(t, kb, i): key kb * 16 + 4 g4 + i
+    // dQ += dS K over 32 keys: their scores and dO V^T - delta are in sc and dp, K in two LDS blocks; hidden(t, kb, i): key kb * 16 + 4 g4 + i
     auto add = [&](f32x4 (&sc)[NQ][2], f32x4 (&dp)[NQ][2], const u32x4* kblocks, bool masked, auto hidden)
                    __attribute__((always_inline)) {
       u32x4 ds[NQ];
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
             for (int i = 0; i < 4; ++i) x[i] = hidden(t, kb, i) ? 0.f : x[i];
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] *= dp[t][kb][i] - delta[t];
+          for (int i = 0; i < 4; ++i) x[i] *= dp[t][kb][i];
           ds[t][kb * 2] = M::pack(x[0], x[1]);
           ds[t][kb * 2 + 1] = M::pack(x[2], x[3]);
         }
@@ -180,7 +181,10 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
     for (int c0 = chain0; c0 <= w_last && s.reach > 0; c0 += 32) {           // uniform
       f32x4 sc[NQ][2], dp[NQ][2];
 #pragma unroll
-      for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = dp[t][0] = dp[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < NQ; ++t) {
+        sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        dp[t][0] = dp[t][1] = ndelta[t];
+      }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -216,7 +220,10 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
       for (int hh = 0; hh < 2; ++hh) {
         f32x4 sc[NQ][2], dp[NQ][2];
 #pragma unroll
-        for (int t = 0; t < NQ; ++t) sc[t][0] = sc[t][1] = dp[t][0] = dp[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NQ; ++t) {
+        sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        dp[t][0] = dp[t][1] = ndelta[t];
+      }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
