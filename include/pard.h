@@ -360,8 +360,9 @@ pard_status pard_cod_build_noalloc(const int32_t *tokens, const int64_t *tok_off
  * Status codes as everywhere; there is no context, so no message.
  * ------------------------------------------------------------------------ */
 
-/* A [rows][heads][head_dim] tensor: strides in elements (positive; heads do
- * not overlap), the elements of a head contiguous. */
+/* A [rows][heads][head_dim] tensor: strides in elements (not negative), the
+ * elements of a head contiguous.  The heads of an output do not overlap; those
+ * of an input may (stride 0: one row or head for all). */
 typedef struct {
   void *data;
   int64_t row_stride, head_stride;
@@ -403,13 +404,14 @@ pard_status pard_rope_table(const pard_rope_spec *spec, int32_t n_pos, float *ta
  * Everything is computed in float32 and rounded once to dtype (PARD_F32,
  * PARD_BF16 or PARD_F16).  A row whose position is outside [0, n_pos) gets
  * NaN.  Outputs may be the inputs themselves (same data and strides), but may
- * not overlap them otherwise.  n_k = 0: no keys (k, k_out, k_gain unused).
+ * not overlap them otherwise, nor each other.  n_k = 0: no keys (k, k_out, k_gain unused).
  * Vectorised where data and strides are multiples of 16 bytes, head_dim and
  * rot_dim of 16 and head_dim <= 512; slower otherwise.
  * Errors: ARG (null pointer, rows < 0, n_q < 1, n_k < 0, head_dim outside [2,
  * 1024], rot_dim not even or outside [2, head_dim], n_pos outside [1, 2^24],
  * unknown layout, one gain without the other, negative or non-finite eps,
- * strides < 1 or below an overlap), UNSUPPORTED (dtype; rows * (n_q + n_k)
+ * negative strides, overlapping heads of an output, an output where an input
+ * starts but with other strides), UNSUPPORTED (dtype; rows * (n_q + n_k)
  * above 2^31 - 1), DEVICE. */
 enum { PARD_ROPE_HALF = 0, PARD_ROPE_INTERLEAVED = 1 };
 typedef struct {
@@ -428,7 +430,7 @@ pard_status pard_qk_rope(const pard_rope_args *args, const pard_heads *q, const 
  * gains, q and k are the forward call's inputs and the gains' gradients are
  * written to q_dgain and k_dgain (float[head_dim], sums over rows and heads,
  * deterministic); without, q, k, q_dgain and k_dgain are not used and may be
- * null.  dx may be dy itself.  The workspace is needed with gains only.
+ * null.  dx may be dy itself, but not x.  The workspace is needed with gains only.
  * Errors: as pard_qk_rope; NOMEM (workspace too small). */
 size_t pard_qk_rope_workspace_bytes(const pard_rope_args *args);
 pard_status pard_qk_rope_grad(const pard_rope_args *args, const pard_heads *q_dy, const pard_heads *k_dy,
@@ -449,7 +451,8 @@ pard_status pard_qk_rope_grad(const pard_rope_args *args, const pard_heads *q_dy
  * refers to it.  The call waits for its result, so it cannot be captured.
  * Errors: ARG (null pointer, misaligned plan_data, n_samples < 1, offsets
  * negative or descending, rows not in the form above: then *plan is not set),
- * UNSUPPORTED (2^31 rows or more, a region above 2^19), NOMEM (plan_bytes too small), DEVICE. */
+ * UNSUPPORTED (2^31 rows or more, a region above 2^19, 2^22 samples or more),
+ * NOMEM (plan_bytes too small), DEVICE. */
 typedef struct {
   int64_t rows;                    /* out_offsets[n_samples] */
   int32_t n_samples, n_tiles;
@@ -470,13 +473,15 @@ pard_status pard_cod_plan_build(const int32_t *section, const int32_t *column, c
  * = 0 and lse = -inf; rows outside the regions are left as they are; neither's
  * inputs are used, whatever they hold.  (A NaN or an infinity in a sample's
  * own rows may reach any row of that sample.)  Scores, softmax and sums are
- * float32; probabilities are rounded to dtype for the product with V.
- * Results are deterministic.  No output may overlap an input.
+ * float32 (scores within +-1e30); probabilities are rounded to dtype for the
+ * product with V.  Results are deterministic.  No output may overlap an input.
  * Errors: ARG (null pointer, a plan that was not built, head counts < 1,
  * n_heads not a multiple of n_kv_heads, scale not finite, data not 16-byte
- * aligned, strides not multiples of 8 elements or above 2^31 - 1), UNSUPPORTED
- * (head_dim not 64 or 128, dtype not PARD_BF16 or PARD_F16, n_heads above
- * 65535 or 1024 n_kv_heads), DEVICE. */
+ * aligned, strides negative, not multiples of 8 elements or above 2^31 - 1,
+ * overlapping heads of an output, an output that starts where another tensor
+ * does), UNSUPPORTED (head_dim not 64 or 128, dtype not PARD_BF16 or PARD_F16,
+ * n_heads above 65535 or 1024 n_kv_heads, tiles * max(n_heads, 4 n_kv_heads)
+ * of 2^24 or more), DEVICE. */
 typedef struct {
   const pard_cod_plan *plan;
   int32_t n_heads, n_kv_heads, head_dim, dtype;
@@ -488,7 +493,8 @@ pard_status pard_cod_attn(const pard_cod_attn_args *args, const pard_heads *q, c
 /* Gradient of pard_cod_attn: out and lse are the forward call's outputs.
  * Padding rows of dq, dk and dv get 0, rows outside the regions are left as
  * they are.  Probabilities and score gradients are rounded to dtype for the
- * products; sums over a key head's query heads are float32.  Deterministic.
+ * products; sums over a key head's query heads are float32.  Deterministic.  No
+ * gradient may overlap another or an input.
  * Errors: as pard_cod_attn; NOMEM (workspace too small). */
 size_t pard_cod_attn_workspace_bytes(const pard_cod_attn_args *args);
 pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads *d_out, const pard_heads *q,
@@ -506,13 +512,15 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads 
  *           = mean of CE over all counted rows        (weights null)
  *   row_loss[r] = CE, 0 for rows that do not count (may be null)
  *   d_logits = grad_scale * d loss[0] / d logits (may be null: loss only; may
- *              be logits itself); rows that do not count get 0
+ *              be logits itself, same data and stride, but not overlap it
+ *              otherwise); rows that do not count get 0
  * A label of vocab or more makes its row's loss and gradient NaN.  Sums are
  * float32, means over rows float64.  logits, d_logits: dtype (PARD_F32,
  * PARD_BF16, PARD_F16), [rows][vocab] with row strides in elements; loss:
  * device, float[1 + n_sections].  Deterministic.
  * Errors: ARG (null pointer, rows < 0, vocab < 1, n_sections outside [1, 64],
- * strides below vocab, non-finite grad_scale or weights), UNSUPPORTED (dtype,
+ * strides below vocab, d_logits at logits with another stride, non-finite
+ * grad_scale or weights), UNSUPPORTED (dtype,
  * above 2^30 rows or a vocab above 2^28), NOMEM (workspace too small), DEVICE. */
 typedef struct {
   int64_t rows;

@@ -261,7 +261,6 @@ template <int HD, class M>
 hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
   constexpr int NQ = 2;
   const int64_t blocks = (int64_t)a.n_tiles * (kCodTile / (64 * NQ)) * a.group * a.n_kv;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
   k_cod_attn<HD, NQ, M><<<(unsigned)blocks, 256, 0, st>>>(a);
   return hipGetLastError();
 }

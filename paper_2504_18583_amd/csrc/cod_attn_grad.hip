@@ -15,8 +15,6 @@
 //     walk the pairs from the first place to the last chain's end.
 #include "cod_attn_tile.h"
 
-#include <algorithm>
-
 namespace pard {
 namespace {
 
@@ -289,10 +287,10 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   }
 }
 
-// dK and dV of NK blocks of 16 keys (operands kf, vf) over 32 pairs in two LDS
-// blocks each of Q and dO, the pairs i0 .. of statistics st; if masked,
-// key block k of this lane is hidden from the pairs for whose `by` entry (st.seen
-// or st.pos) hidden(k, entry) holds.  dO V^T starts from -delta.
+// dK and dV of NK blocks of 16 keys (operands kf, vf) over 32 pairs, two LDS
+// blocks each of Q and dO, with the statistics st from i0 on.  If masked, key
+// block k of this lane is hidden from the pairs for whose `by` entry (st.seen or
+// st.pos) hidden(k, entry) holds.  dO V^T starts from -delta.
 template <int HD, int NK, class M, class H>
 __device__ __forceinline__ void dkv_step(const u32x4* qb, const u32x4* gb, const PairStats& st, int i0,
                                          const u32x4 (&kf)[NK][HD / 32],
@@ -513,7 +511,6 @@ hipError_t launch_hd(const CodAttnArgs& a, hipStream_t st) {
   constexpr int NQ = 2;
   const int64_t tiles = (int64_t)a.n_tiles * a.n_kv, dq = tiles * (kCodTile / (64 * NQ)) * a.group;
   const int64_t real = tiles * (kCodTile / (64 * dkv_blocks(HD))), all = real + tiles * (kCodTile / 64);
-  if (dq > 0x7fffffff || all > 0x7fffffff) return hipErrorInvalidValue;
   k_cod_dq<HD, NQ, M, true><<<(unsigned)dq, 256, 0, st>>>(a);
   k_cod_dq<HD, NQ, M, false><<<(unsigned)dq, 256, 0, st>>>(a);
   k_cod_dkv<HD, M><<<(unsigned)all, 256, 0, st>>>(a, (unsigned)real);

@@ -125,9 +125,6 @@ __device__ __forceinline__ char* at(const Heads16& h, uint32_t row, uint32_t hea
 __device__ __forceinline__ int quotient(int x, const FastDiv& f) { return (int)(__umulhi((uint32_t)x << 2, f.m) >> f.l); }
 __device__ __forceinline__ int remainder(int x, int q, const FastDiv& f) { return x - q * (int)f.d; }
 
-// s_waitcnt vmcnt(n) lgkmcnt(0).
-constexpr int vm_wait(int n) { return (n & 15) | ((n >> 4) << 14) | 0x70; }
-
 // Everything this wavefront loaded is in LDS and its LDS reads are done; then
 // everyone's.
 __device__ __forceinline__ void wait_all() {

@@ -52,11 +52,15 @@ __device__ __forceinline__ void load_counts(const CodLossArgs& a, int (&n_s)[kCo
   __syncthreads();
 }
 
-// Joins two (maximum, sum of 2^(z - maximum)) pairs.
+// Joins two (maximum, sum of exp(x - maximum)) pairs.  Logits are subtracted
+// before they are scaled to base 2: the type's lowest value does not overflow.
 __device__ __forceinline__ void join(float& m, float& l, float om, float ol) {
-  if (om == -INFINITY) return;                       // (a NaN goes on: it makes l NaN)
+  if (om == -INFINITY) {
+    l += ol;                                         // (0, or NaN)
+    return;
+  }
   const float n = m == -INFINITY ? om : fmaxf(m, om);
-  l = l * exp2f(m - n) + ol * exp2f(om - n);
+  l = l * exp2f((m - n) * kLog2e) + ol * exp2f((om - n) * kLog2e);
   m = n;
 }
 
@@ -84,7 +88,7 @@ struct LossVec<ElemF32> {
   __device__ __forceinline__ static LossVec pack(const float (&x)[N]) { return LossVec{float4{x[0], x[1], x[2], x[3]}}; }
 };
 
-// Adds the elements of C vectors to a thread's (maximum, sum), base 2.
+// Adds the elements of C vectors to a thread's (maximum, sum).
 template <class E, int C>
 __device__ __forceinline__ void add_vectors(const LossVec<E>* v, float& m, float& l) {
   constexpr int N = LossVec<E>::N;
@@ -93,9 +97,8 @@ __device__ __forceinline__ void add_vectors(const LossVec<E>* v, float& m, float
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fmaxf(top, v[c][i]);
-  top *= kLog2e;
   if (top > m) {
-    l *= exp2f(m - top);                             // (m = -infinity: l is 0)
+    l *= exp2f((m - top) * kLog2e);                  // (m = -infinity: l is 0)
     m = top;
   }
   // (no finite logit so far: every term is 0, or NaN for a NaN)
@@ -103,7 +106,7 @@ __device__ __forceinline__ void add_vectors(const LossVec<E>* v, float& m, float
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int i = 0; i < N; ++i) l += __builtin_amdgcn_exp2f(fmaf(v[c][i], kLog2e, -ref));
+    for (int i = 0; i < N; ++i) l += __builtin_amdgcn_exp2f((v[c][i] - ref) * kLog2e);
 }
 
 // Rows of T threads, NV vectors each.  A row's elements before its first 16-byte
@@ -192,7 +195,7 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
         __builtin_amdgcn_sched_barrier(0);           // (few unpacked logits at a time)
       }
     }
-    join(m, l, edge * kLog2e, 1.f);
+    join(m, l, edge, edge == -INFINITY ? 0.f : 1.f);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
       const float om = __shfl_xor(m, off), ol = __shfl_xor(l, off);
@@ -206,9 +209,9 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
     m = m_s[turn][0];
     l = l_s[turn][0];
     for (int w = 1; w < W; ++w) join(m, l, m_s[turn][w], l_s[turn][w]);
-    const float lse2 = m + log2f(l);
+    const float log2_l = log2f(l);                   // log sum exp = m + ln(l)
     if (tid == 0) {
-      const float ce = k > 0 ? lse2 * kLn2 - x_label : 0.f;
+      const float ce = k > 0 ? fmaf(log2_l, kLn2, m - x_label) : 0.f;
       if (a.row_loss) a.row_loss[r] = ce;
       if (k > 0) sum_s[k - 1] += ce;
     }
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
         if ((q * NV + i + 1) * T <= n_now || at < n_now) {   // (the first part uniform)
           float g[N];
 #pragma unroll
-          for (int j = 0; j < N; ++j) g[j] = k > 0 ? w * __builtin_amdgcn_exp2f(fmaf(v[i][j], kLog2e, -lse2)) : 0.f;
+          for (int j = 0; j < N; ++j) g[j] = k > 0 ? w * __builtin_amdgcn_exp2f(fmaf(v[i][j] - m, kLog2e, -log2_l)) : 0.f;
           if (SCALAR_OUT) {
 #pragma unroll
             for (int j = 0; j < N; ++j) d[head_now + at * N + j] = E::store(g[j]);
@@ -249,12 +252,12 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
         __builtin_amdgcn_sched_barrier(0);           // (one vector at a time: its registers are taken over)
       }
     }
-    if (e >= 0) d[e] = E::store(k > 0 ? w * exp2f(edge * kLog2e - lse2) : 0.f);
+    if (e >= 0) d[e] = E::store(k > 0 ? w * exp2f(fmaf(edge - m, kLog2e, -log2_l)) : 0.f);
     // the label's element again, by the thread that wrote it
     if (k > 0 && label < a.vocab) {
       const int in_vec = label - head_now;
       const bool own = in_vec >= 0 && in_vec < n_now * N ? in_vec / N % T == tid : label == e;
-      if (own) d[label] = E::store(w * (exp2f(x_label * kLog2e - lse2) - 1.f));
+      if (own) d[label] = E::store(w * (exp2f(fmaf(x_label - m, kLog2e, -log2_l)) - 1.f));
     }
   }
 

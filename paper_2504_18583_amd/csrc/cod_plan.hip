@@ -187,8 +187,6 @@ hipError_t launch_cod_plan(const int32_t* section, const int32_t* column, const 
                            int max_region, const CodPlanView& v, hipStream_t st) {
   const int n_chains = std::min(kMaxChains, (max_region + 63) / 64 * 64);
   const int n_levels = (max_region + kCodTile - 1) / kCodTile;
-  // a region holds at most 64 rows of each of 8192 chains; more is padding
-  if (n_levels > 16384) return hipErrorInvalidValue;
   k_cod_plan<<<n_samples, kPlanThreads, (size_t)n_chains * 12, st>>>(section, column, out_len, n_chains, v);
   k_cod_tiles<<<1, kPlanThreads, (size_t)n_levels * 2 * sizeof(int), st>>>(n_samples, n_levels, v);
   return hipGetLastError();

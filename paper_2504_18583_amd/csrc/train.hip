@@ -31,6 +31,13 @@ bool heads_ok(const pard_heads* t, int64_t rows, int heads, int hd, bool out) {
   return by_row || by_head;
 }
 
+// Whether an output may lie where an input does: as the input, or apart from it
+// (overlaps of tensors that start elsewhere are the caller's to avoid).
+bool apart(const pard_heads* a, const pard_heads* b) { return a->data != b->data; }
+bool same_or_apart(const pard_heads* a, const pard_heads* b, int64_t rows, int heads) {
+  return apart(a, b) || ((rows == 1 || a->row_stride == b->row_stride) && (heads == 1 || a->head_stride == b->head_stride));
+}
+
 Heads view(const pard_heads* t) {
   return t ? Heads{static_cast<char*>(t->data), t->row_stride, t->head_stride} : Heads{nullptr, 0, 0};
 }
@@ -79,8 +86,12 @@ pard_status attn_check(const pard_cod_attn_args* a) {
     return PARD_ERR_ARG;
   if ((a->head_dim != 64 && a->head_dim != 128) || (a->dtype != PARD_BF16 && a->dtype != PARD_F16))
     return PARD_ERR_UNSUPPORTED;
-  // (pairs of a sample and key head are numbered in 32 bits)
-  return a->n_heads > 65535 || a->n_heads / a->n_kv_heads > 1024 ? PARD_ERR_UNSUPPORTED : PARD_OK;
+  // (pairs of a sample and key head are numbered in 32 bits; a launch has fewer
+  // than 2^32 threads, 256 to a workgroup)
+  if (a->n_heads > 65535 || a->n_heads / a->n_kv_heads > 1024 ||
+      (int64_t)a->plan->n_tiles * std::max(a->n_heads, 4 * a->n_kv_heads) >= 1 << 24)
+    return PARD_ERR_UNSUPPORTED;
+  return PARD_OK;
 }
 
 // The kernels read and write 16 bytes of a head at a time, and take strides in
@@ -149,6 +160,9 @@ pard_status pard_qk_rope(const pard_rope_args* args, const pard_heads* q, const 
       (a.n_k > 0 && (!heads_ok(k, a.rows, a.n_k, a.head_dim, false) || !heads_ok(k_out, a.rows, a.n_k, a.head_dim, true))))
     return PARD_ERR_ARG;
   if (a.rows == 0) return PARD_OK;
+  if (!same_or_apart(q, q_out, a.rows, a.n_q) ||
+      (a.n_k > 0 && (!same_or_apart(k, k_out, a.rows, a.n_k) || !apart(q, k_out) || !apart(k, q_out) || !apart(q_out, k_out))))
+    return PARD_ERR_ARG;
   RopeArgs r = rope_args(args);
   r.q_in = view(q);
   r.q_out = view(q_out);
@@ -178,6 +192,11 @@ pard_status pard_qk_rope_grad(const pard_rope_args* args, const pard_heads* q_dy
   if (norm && (!in(q, a.n_q) || !q_dgain || (keys && (!in(k, a.n_k) || !k_dgain)))) return PARD_ERR_ARG;
   if (norm && (!workspace || !aligned(workspace, 256))) return PARD_ERR_ARG;
   if (norm && workspace_bytes < pard_qk_rope_workspace_bytes(args)) return PARD_ERR_NOMEM;
+  if (a.rows > 0 &&
+      (!same_or_apart(q_dy, q_dx, a.rows, a.n_q) || (norm && !apart(q, q_dx)) ||
+       (keys && (!same_or_apart(k_dy, k_dx, a.rows, a.n_k) || !apart(q_dy, k_dx) || !apart(k_dy, q_dx) || !apart(q_dx, k_dx) ||
+                 (norm && (!apart(k, k_dx) || !apart(q, k_dx) || !apart(k, q_dx)))))))
+    return PARD_ERR_ARG;
   if (a.rows == 0 && !norm) return PARD_OK;
   RopeArgs r = rope_args(args);
   r.q_in = view(q_dy);
@@ -213,7 +232,8 @@ pard_status pard_cod_plan_build(const int32_t* section, const int32_t* column, c
   }
   const int64_t rows = out_offsets[n_samples];
   if (rows > 0 && (!section || !column)) return PARD_ERR_ARG;
-  if (rows > 0x7fffffff || longest > (int64_t)kCodMaxSections * 8192) return PARD_ERR_UNSUPPORTED;
+  // (n_samples: workgroups of 1024 threads, fewer than 2^32 in a launch)
+  if (rows > 0x7fffffff || longest > (int64_t)kCodMaxSections * 8192 || n_samples >= 1 << 22) return PARD_ERR_UNSUPPORTED;
   if (plan_bytes < pard_cod_plan_bytes(rows, n_samples)) return PARD_ERR_NOMEM;
   CodPlanView v;
   cod_plan_layout(rows, n_samples, plan_data, &v);
@@ -240,6 +260,7 @@ pard_status pard_cod_attn(const pard_cod_attn_args* args, const pard_heads* q, c
       !attn_heads_ok(out, args, nq, true))
     return PARD_ERR_ARG;
   if (args->plan->n_tiles == 0) return PARD_OK;
+  if (!apart(q, out) || !apart(k, out) || !apart(v, out)) return PARD_ERR_ARG;
   CodAttnArgs r = attn_args(args);
   r.q = view16(q);
   r.k = view16(k);
@@ -269,6 +290,10 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args* args, const pard_heads*
   if (args->plan->n_tiles == 0) return PARD_OK;
   if (!lse || !workspace || !aligned(workspace, 256)) return PARD_ERR_ARG;
   if (workspace_bytes < pard_cod_attn_workspace_bytes(args)) return PARD_ERR_NOMEM;
+  for (const pard_heads* y : {dq, dk, dv})
+    for (const pard_heads* x : {d_out, q, k, v, out})
+      if (!apart(x, y)) return PARD_ERR_ARG;
+  if (!apart(dq, dk) || !apart(dq, dv) || !apart(dk, dv)) return PARD_ERR_ARG;
   CodAttnArgs r = attn_args(args);
   r.q = view16(q);
   r.k = view16(k);
@@ -292,6 +317,7 @@ pard_status pard_cod_loss(const pard_cod_loss_args* args, void* workspace, size_
   const pard_cod_loss_args& a = *args;
   if (a.rows > 0 && (!a.logits || !a.labels || (!a.section && a.n_sections != 1))) return PARD_ERR_ARG;
   if (a.rows > 1 && (a.logits_stride < a.vocab || (a.d_logits && a.d_stride < a.vocab))) return PARD_ERR_ARG;
+  if (a.rows > 1 && a.d_logits == a.logits && a.d_stride != a.logits_stride) return PARD_ERR_ARG;
   for (int k = 0; a.weights && k < a.n_sections; ++k)
     if (!std::isfinite(a.weights[k])) return PARD_ERR_ARG;
   const int size = elem_size(a.dtype);

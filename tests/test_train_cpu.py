@@ -157,6 +157,57 @@ def test_cod_loss_refuses(b):
 
 
 @needs_lib
+def test_outputs_on_other_tensors_are_refused(b):
+    """An output that starts where another tensor does: refused, but for the
+    rotation and the loss in place with the same strides."""
+    h = lambda i, rs=256, hs=64: b.pard_heads(P * (i + 1), rs, hs)  # noqa: E731
+    a, n = _rope_args(b), 1 << 30
+    rope = lambda q, k, qo, ko: b.lib.pard_qk_rope(a, q, k, qo, ko, None)  # noqa: E731
+    assert rope(h(0), h(1), h(0, 512), h(2)) == rope(h(0), h(1), h(0, 256, 128), h(2)) == rope(h(0), h(1), h(1), h(2)) == b.PARD_ERR_ARG
+    assert rope(h(0), h(1), h(2), h(0)) == rope(h(0), h(1), h(2), h(2)) == rope(h(0), h(1), h(2), h(1, 512)) == b.PARD_ERR_ARG
+    g = _rope_args(b, q_gain=P, k_gain=P)
+    grad = lambda qd, kd, qo, ko: b.lib.pard_qk_rope_grad(g, qd, kd, h(0), h(1), qo, ko, P, P, P, n, None)  # noqa: E731
+    for t in ((h(2), h(3), h(2, 512), h(4)), (h(2), h(3), h(0), h(4)), (h(2), h(3), h(4), h(1)), (h(2), h(3), h(3), h(4)),
+              (h(2), h(3), h(4), h(2)), (h(2), h(3), h(4), h(4)), (h(2), h(3), h(1), h(4)), (h(2), h(3), h(4), h(0))):
+        assert grad(*t) == b.PARD_ERR_ARG
+    plan = b.pard_cod_plan(100, 1, 1, P)
+    at = b.pard_cod_attn_args(plan=C.pointer(plan), n_heads=4, n_kv_heads=2, head_dim=64, dtype=b.PARD_BF16, scale=0.125)
+    for i in range(3):
+        assert b.lib.pard_cod_attn(at, h(0), h(1), h(2), h(i), P, None) == b.PARD_ERR_ARG
+    for o in range(3):                               # dq, dk, dv at one of the inputs, or at each other
+        for i in range(8):
+            if i != 5 + o:
+                outs = [h(5), h(6), h(7)]
+                outs[o] = h(i)
+                assert b.lib.pard_cod_attn_grad(at, h(0), h(1), h(2), h(3), h(4), P, *outs, P, 1 << 40, None) == b.PARD_ERR_ARG
+    loss = b.pard_cod_loss_args(rows=4, vocab=10, dtype=b.PARD_F32, n_sections=1, grad_scale=1.0, logits=P, logits_stride=10, labels=P,
+                                section=None, weights=None, d_logits=P, d_stride=12, loss=P, row_loss=None)
+    assert b.lib.pard_cod_loss(loss, P, 1 << 30, None) == b.PARD_ERR_ARG
+
+
+@needs_lib
+def test_sizes_past_a_launch_are_refused(b):
+    def attn(n_tiles, nq, nk):
+        plan = b.pard_cod_plan(100, 1, n_tiles, P)
+        a = b.pard_cod_attn_args(plan=C.pointer(plan), n_heads=nq, n_kv_heads=nk, head_dim=64, dtype=b.PARD_BF16, scale=0.125)
+        return b.lib.pard_cod_attn(a, *[b.pard_heads(P, 256, 64)] * 4, P, None), b.lib.pard_cod_attn_workspace_bytes(a)
+    assert attn(1 << 21, 8, 1) == attn(1 << 19, 8, 8) == (b.PARD_ERR_UNSUPPORTED, 0)
+    assert attn(1, 1025, 1) == (b.PARD_ERR_UNSUPPORTED, 0)
+    assert attn((1 << 21) - 1, 8, 1)[1] > 0
+    offs = (C.c_int64 * ((1 << 22) + 1))()
+    got = b.lib.pard_cod_plan_build(P, P, C.cast(offs, C.POINTER(C.c_int64)), P, 1 << 22, P, 1 << 40, None, b.pard_cod_plan())
+    assert got == b.PARD_ERR_UNSUPPORTED
+    h = lambda rs: b.pard_heads(P, rs, 64)  # noqa: E731
+    plan = b.pard_cod_plan(100, 1, 1, P)
+    a = b.pard_cod_attn_args(plan=C.pointer(plan), n_heads=4, n_kv_heads=2, head_dim=64, dtype=b.PARD_BF16, scale=0.125)
+    assert b.lib.pard_cod_attn(a, h(1 << 31), h(256), h(256), h(256), P, None) == b.PARD_ERR_ARG
+    assert b.lib.pard_cod_attn(a, b.pard_heads(P, 256, 1 << 31), h(256), h(256), h(256), P, None) == b.PARD_ERR_ARG
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        a.scale = bad
+        assert b.lib.pard_cod_attn(a, h(256), h(256), h(256), h(256), P, None) == b.PARD_ERR_ARG
+
+
+@needs_lib
 def test_binding_refuses_what_no_pointer_shows(b):
     """Tensors that the binding turns away before it calls the library (host
     tensors here, as any tensor that is not on a GPU)."""
