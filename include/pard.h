@@ -405,8 +405,8 @@ pard_status pard_rope_table(const pard_rope_spec *spec, int32_t n_pos, float *ta
  * PARD_BF16 or PARD_F16).  A row whose position is outside [0, n_pos) gets
  * NaN.  Outputs may be the inputs themselves (same data and strides), but may
  * not overlap them otherwise, nor each other.  n_k = 0: no keys (k, k_out, k_gain unused).
- * Vectorised where data and strides are multiples of 16 bytes, head_dim and
- * rot_dim of 16 and head_dim <= 512; slower otherwise.
+ * Vectorised where head_dim (up to 512) and rot_dim are multiples of 8 and data
+ * and strides of 8 bytes (PARD_F32: 16); slower otherwise.
  * Errors: ARG (null pointer, rows < 0, n_q < 1, n_k < 0, head_dim outside [2,
  * 1024], rot_dim not even or outside [2, head_dim], n_pos outside [1, 2^24],
  * unknown layout, one gain without the other, negative or non-finite eps,

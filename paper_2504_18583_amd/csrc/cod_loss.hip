@@ -276,8 +276,16 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
   if (!last_s) return;                               // uniform
   for (int q = wave; q < a.n_sections; q += W) {     // a wavefront a subtask
     double s = 0.0;
-    for (int b = lane; b < (int)gridDim.x; b += 64)
-      s += __hip_atomic_load(&a.sums[(size_t)b * a.n_sections + q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int b0 = lane; b0 < (int)gridDim.x; b0 += 64 * 16) {   // 16 loads in flight
+      double x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int b = min(b0 + 64 * i, (int)gridDim.x - 1);
+        x[i] = __hip_atomic_load(&a.sums[(size_t)b * a.n_sections + q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s += b0 + 64 * i < (int)gridDim.x ? x[i] : 0.0;
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
     if (lane == 0) {

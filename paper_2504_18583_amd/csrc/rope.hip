@@ -47,11 +47,28 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-// Sum over groups of W consecutive lanes (W a power of two), in every lane.
+// x of another lane of the same 16 (DPP control CTRL).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+// Sum over groups of W consecutive lanes (W a power of two from 4 to 64), in
+// every lane, by lane permutations of the VALU: neighbours, pairs, then mirrored
+// (whose two halves are uniform by then), then swapped rows and halves.
 template <int W>
 __device__ __forceinline__ float group_sum(float x) {
-#pragma unroll
-  for (int off = W / 2; off > 0; off >>= 1) x += __shfl_xor(x, off, W);
+  x += dpp<0xB1>(x);                                 // quad_perm 1,0,3,2
+  x += dpp<0x4E>(x);                                 // quad_perm 2,3,0,1
+  if (W >= 8) x += dpp<0x141>(x);                    // row_half_mirror
+  if (W >= 16) x += dpp<0x140>(x);                   // row_mirror
+  if (W >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if (W >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
   return x;
 }
 
@@ -188,98 +205,111 @@ __global__ __launch_bounds__(64) void k_rope_gain_sum(const float* part, int blo
   }
 }
 
-// Vectorised kernels.  A head is HD / 16 units of 16 elements: unit u < rot / 16
-// turns the pairs 8 u .. 8 u + 7 (half: elements 8 u .. and rot / 2 + 8 u ..;
-// interleaved: 16 u ..), a later unit is the 16 elements 16 u ...  W lanes (the
-// next power of two) hold one head, one unit each, and take the heads of one row
-// H apart, so that a lane's cosines and sines are read once per row.
-template <class E>
-struct Vec8 {
+// Vectorised kernels, V = 8 or 4 elements a vector.  A head is units of two
+// vectors: unit u < rot / 2V turns the pairs V u .. V u + V - 1 (half: elements
+// V u .. and rot / 2 + V u ..; interleaved: 2V u ..), a later unit is the 2V
+// elements 2V u ...  W lanes (the next power of two) hold one head, one unit
+// each, and take the heads of one row H apart, so that a lane's cosines and sines
+// are read once per row.
+template <class E, int V>
+struct Vec {
   static_assert(sizeof(typename E::T) == 2, "two 16-bit elements a word");
-  uint4 v;
-  __device__ __forceinline__ void load(const char* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  typedef uint32_t Words __attribute__((ext_vector_type(V / 2)));
+  Words w;
+  __device__ __forceinline__ void load(const char* p) { w = *reinterpret_cast<const Words*>(p); }
+  __device__ __forceinline__ void get(float (&x)[V]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < V / 2; ++i) {
       x[2 * i] = E::load((uint16_t)w[i]);
       x[2 * i + 1] = E::load((uint16_t)(w[i] >> 16));
     }
   }
-  __device__ __forceinline__ static void store(char* p, const float (&x)[8]) {
-    uint32_t w[4];
+  __device__ __forceinline__ static void store(char* p, const float (&x)[V]) {
+    Words w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)E::store(x[2 * i]) | ((uint32_t)E::store(x[2 * i + 1]) << 16);
-    *reinterpret_cast<uint4*>(p) = uint4{w[0], w[1], w[2], w[3]};
+    for (int i = 0; i < V / 2; ++i) w[i] = (uint32_t)E::store(x[2 * i]) | ((uint32_t)E::store(x[2 * i + 1]) << 16);
+    *reinterpret_cast<Words*>(p) = w;
   }
 };
-template <>
-struct Vec8<ElemF32> {
-  float4 a, b;
+template <int V>
+struct Vec<ElemF32, V> {
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4 w[V / 4];
   __device__ __forceinline__ void load(const char* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = reinterpret_cast<const f32x4*>(p)[i];
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  __device__ __forceinline__ void get(float (&x)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = w[i / 4][i % 4];
   }
-  __device__ __forceinline__ static void store(char* p, const float (&x)[8]) {
-    reinterpret_cast<float4*>(p)[0] = float4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<float4*>(p)[1] = float4{x[4], x[5], x[6], x[7]};
+  __device__ __forceinline__ static void store(char* p, const float (&x)[V]) {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i)
+      reinterpret_cast<f32x4*>(p)[i] = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
   }
 };
 
-// 16 elements of a unit turned by the row's angles (INV: back).
-template <int LAYOUT, bool INV>
-__device__ __forceinline__ void turn_unit(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) {
+// The elements of a unit turned by the row's angles (INV: back).
+template <int LAYOUT, bool INV, int V>
+__device__ __forceinline__ void turn_unit(float (&a)[V], float (&b)[V], const float (&c)[V], const float (&s)[V]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < V; ++i) {
     // the pair: (a[i], b[i]), or neighbours
-    float& x = LAYOUT == PARD_ROPE_HALF ? a[i] : (i < 4 ? a[2 * (i & 3)] : b[2 * (i & 3)]);
-    float& y = LAYOUT == PARD_ROPE_HALF ? b[i] : (i < 4 ? a[2 * (i & 3) + 1] : b[2 * (i & 3) + 1]);
+    constexpr int H = V / 2;
+    float& x = LAYOUT == PARD_ROPE_HALF ? a[i] : (i < H ? a[2 * (i % H)] : b[2 * (i % H)]);
+    float& y = LAYOUT == PARD_ROPE_HALF ? b[i] : (i < H ? a[2 * (i % H) + 1] : b[2 * (i % H) + 1]);
     const float sn = INV ? -s[i] : s[i], u = x * c[i] - y * sn;
     y = y * c[i] + x * sn;
     x = u;
   }
 }
 
-template <class E, int LAYOUT, bool GRAD, bool NORM, int W>
+template <class E, int LAYOUT, bool GRAD, bool NORM, int V, int W>
 __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_step, int rows_per_block) {
   constexpr int SZ = sizeof(typename E::T), U = GRAD && NORM ? 2 : 4;   // heads in flight
   const int tid = threadIdx.x, unit = tid % W, slot = tid / W;
   const int h0 = slot % h_step, row_slot = slot / h_step, row_step = kRopeThreads / W / h_step;
   const int heads = a.n_q + a.n_k;
-  const bool on = unit * 16 < a.hd, turns = on && unit * 16 < a.rot;
+  const bool on = unit * 2 * V < a.hd, turns = on && unit * 2 * V < a.rot;
   // element offsets of this lane's two vectors
-  const int o0 = !on ? 0 : turns && LAYOUT == PARD_ROPE_HALF ? unit * 8 : unit * 16;
-  const int o1 = !on ? 0 : turns && LAYOUT == PARD_ROPE_HALF ? a.rot / 2 + unit * 8 : unit * 16 + 8;
-  float gq[2][8], gk[2][8], dgq[2][8], dgk[2][8];
+  const int o0 = !on ? 0 : turns && LAYOUT == PARD_ROPE_HALF ? unit * V : unit * 2 * V;
+  const int o1 = !on ? 0 : turns && LAYOUT == PARD_ROPE_HALF ? a.rot / 2 + unit * V : unit * 2 * V + V;
+  float gq[2][V], gk[2][V], dgq[2][V], dgk[2][V];
   if (NORM) {
+    // (16-byte loads; gains may lie at any float)
+    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    const float* const kg = a.n_k > 0 ? a.k_gain : a.q_gain;   // (no keys: not used)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      gq[0][i] = a.q_gain[o0 + i];
-      gq[1][i] = a.q_gain[o1 + i];
-      gk[0][i] = a.n_k > 0 ? a.k_gain[o0 + i] : 0.f;
-      gk[1][i] = a.n_k > 0 ? a.k_gain[o1 + i] : 0.f;
-      dgq[0][i] = dgq[1][i] = dgk[0][i] = dgk[1][i] = 0.f;
-    }
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(a.q_gain + (b ? o1 : o0) + i);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(kg + (b ? o1 : o0) + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          gq[b][i + j] = x[j];
+          gk[b][i + j] = y[j];
+          dgq[b][i + j] = dgk[b][i + j] = 0.f;
+        }
+      }
   }
   const float inv_hd = 1.0f / a.hd;
   const int row_end = min((int64_t)a.rows, ((int64_t)blockIdx.x + 1) * rows_per_block);
   for (int row = blockIdx.x * rows_per_block + row_slot; row < row_end; row += row_step) {
     const int pos = a.pos[row];
     const bool ok = pos >= 0 && pos < a.n_pos;
-    float c[8] = {}, s[8] = {};
+    float c[V] = {}, s[V] = {};
     if (turns) {
-      const float4* t = reinterpret_cast<const float4*>(a.table + (size_t)(ok ? pos : 0) * (a.rot / 2) + unit * 8);
+      const float4* t = reinterpret_cast<const float4*>(a.table + (size_t)(ok ? pos : 0) * (a.rot / 2) + unit * V);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < V / 2; ++i) {
         const float4 v = t[i];
         c[2 * i] = v.x, s[2 * i] = v.y, c[2 * i + 1] = v.z, s[2 * i + 1] = v.w;
       }
     }
     for (int hb = h0; hb < heads; hb += U * h_step) {
-      Vec8<E> v[U][2], w[U][2];
+      Vec<E, V> v[U][2], w[U][2];
       char* dst[U];
       bool live[U], is_q[U];
 #pragma unroll
@@ -306,47 +336,47 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_s
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         if (!NORM && !live[j]) continue;
-        float x[2][8], y[2][8];
+        float x[2][V], y[2][V];
         if (live[j]) {
           v[j][0].get(x[0]);
           v[j][1].get(x[1]);
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = 0.f;
+          for (int i = 0; i < V; ++i) x[0][i] = x[1][i] = 0.f;
         }
         if (GRAD) {
-          if (turns) turn_unit<LAYOUT, true>(x[0], x[1], c, s);
+          if (turns) turn_unit<LAYOUT, true, V>(x[0], x[1], c, s);
           if (!ok) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = __builtin_nanf("");
+            for (int i = 0; i < V; ++i) x[0][i] = x[1][i] = __builtin_nanf("");
           }
         }
         if (NORM) {
-          float(&z)[2][8] = GRAD ? y : x;                  // the head before the norm
+          float(&z)[2][V] = GRAD ? y : x;                  // the head before the norm
           if (GRAD) {
             if (live[j]) {
               w[j][0].get(y[0]);
               w[j][1].get(y[1]);
             } else {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) y[0][i] = y[1][i] = 0.f;
+              for (int i = 0; i < V; ++i) y[0][i] = y[1][i] = 0.f;
             }
           }
           float ss = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) ss += z[0][i] * z[0][i] + z[1][i] * z[1][i];
+          for (int i = 0; i < V; ++i) ss += z[0][i] * z[0][i] + z[1][i] * z[1][i];
           const float r = 1.0f / sqrtf(group_sum<W>(ss) * inv_hd + a.eps);
           if (!GRAD) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) x[b][i] *= r * (is_q[j] ? gq[b][i] : gk[b][i]);
+              for (int i = 0; i < V; ++i) x[b][i] *= r * (is_q[j] ? gq[b][i] : gk[b][i]);
           } else {
             float dot = 0.f;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
+              for (int i = 0; i < V; ++i) {
                 y[b][i] *= r;                              // x^
                 const float d = x[b][i] * y[b][i];
                 if (is_q[j]) dgq[b][i] += d;
@@ -358,30 +388,30 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_s
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) x[b][i] = r * (x[b][i] - y[b][i] * mean);
+              for (int i = 0; i < V; ++i) x[b][i] = r * (x[b][i] - y[b][i] * mean);
           }
         }
         if (!GRAD) {
-          if (turns) turn_unit<LAYOUT, false>(x[0], x[1], c, s);
+          if (turns) turn_unit<LAYOUT, false, V>(x[0], x[1], c, s);
           if (!ok) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[0][i] = x[1][i] = __builtin_nanf("");
+            for (int i = 0; i < V; ++i) x[0][i] = x[1][i] = __builtin_nanf("");
           }
         }
         if (live[j]) {
-          Vec8<E>::store(dst[j] + SZ * o0, x[0]);
-          Vec8<E>::store(dst[j] + SZ * o1, x[1]);
+          Vec<E, V>::store(dst[j] + SZ * o0, x[0]);
+          Vec<E, V>::store(dst[j] + SZ * o1, x[1]);
         }
       }
     }
   }
   if (GRAD && NORM) {
     // this workgroup's sums of each element, over its slots in their order
-    __shared__ float sum_s[2][kRopeThreads * 16];
+    __shared__ float sum_s[2][kRopeThreads * 2 * V];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < V; ++i) {
         const int e = b ? o1 + i : o0 + i;
         if (on) {
           sum_s[0][slot * a.hd + e] = dgq[b][i];
@@ -399,23 +429,24 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_s
 }
 
 // Whether every vector of a tensor is aligned.
-bool vector_fit(const Heads& h, int size, int64_t rows, int heads) {
-  return (reinterpret_cast<uintptr_t>(h.data) & 15) == 0 && (rows == 1 || h.rs * size % 16 == 0) &&
-         (heads == 1 || h.hs * size % 16 == 0);
+bool vector_fit(const Heads& h, int v, int size, int64_t rows, int heads) {
+  const int bytes = std::min(v * size, 16);
+  return reinterpret_cast<uintptr_t>(h.data) % bytes == 0 && (rows == 1 || h.rs * size % bytes == 0) &&
+         (heads == 1 || h.hs * size % bytes == 0);
 }
 
 template <class E>
-bool vectorised(bool grad, const RopeArgs& a) {
+bool vectorised(int v, bool grad, const RopeArgs& a) {
   constexpr int size = sizeof(typename E::T);
-  if (a.hd % 16 || a.hd > 512 || a.rot % 16) return false;
+  if (a.hd % (2 * v) || a.hd > 512 || a.rot % (2 * v)) return false;
   auto fit = [&](const Heads& q, const Heads& k) {
-    return vector_fit(q, size, a.rows, a.n_q) && (a.n_k == 0 || vector_fit(k, size, a.rows, a.n_k));
+    return vector_fit(q, v, size, a.rows, a.n_q) && (a.n_k == 0 || vector_fit(k, v, size, a.rows, a.n_k));
   };
   return fit(a.q_in, a.k_in) && fit(a.q_out, a.k_out) && (!grad || !a.q_gain || fit(a.q_x, a.k_x));
 }
 
 // (returns the workgroups launched)
-template <class E, int LAYOUT, bool GRAD, bool NORM, int W>
+template <class E, int LAYOUT, bool GRAD, bool NORM, int V, int W>
 int launch_width(const RopeArgs& a, hipStream_t st) {
   // heads of a row side by side: the power of two that leaves the fewest idle
   // slots, at least two rounds' loads a lane where there are rows enough
@@ -424,36 +455,46 @@ int launch_width(const RopeArgs& a, hipStream_t st) {
   while (h_step * 2 <= std::min(slots, 16) && (heads + 2 * h_step - 1) / (2 * h_step) * 2 * h_step <= heads + heads / 8) h_step *= 2;
   while (h_step * 2 <= slots && (int64_t)a.rows * h_step < 2048 && h_step < heads) h_step *= 2;
   const int row_step = slots / h_step;
-  // gradients of gains: few workgroups, each with a partial sum
-  const int64_t most = GRAD && NORM ? rope_grad_blocks(a) : 1 << 20;
+  // gains: few workgroups, which read them (and leave partial sums of their
+  // gradients) once
+  const int64_t most = !NORM ? 1 << 20 : GRAD ? rope_grad_blocks(a) : 2048;
   const int64_t rows_per_block = ((a.rows + most - 1) / most + row_step - 1) / row_step * row_step;
   const int blocks = (int)((a.rows + rows_per_block - 1) / rows_per_block);
-  k_rope<E, LAYOUT, GRAD, NORM, W><<<blocks, kRopeThreads, 0, st>>>(a, h_step, (int)rows_per_block);
+  k_rope<E, LAYOUT, GRAD, NORM, V, W><<<blocks, kRopeThreads, 0, st>>>(a, h_step, (int)rows_per_block);
   return blocks;
 }
 
-template <class E, int LAYOUT, bool GRAD, bool NORM>
+template <class E, int LAYOUT, bool GRAD, bool NORM, int V>
 int launch_vector(const RopeArgs& a, hipStream_t st) {
-  if (a.hd <= 64) return launch_width<E, LAYOUT, GRAD, NORM, 4>(a, st);
-  if (a.hd <= 128) return launch_width<E, LAYOUT, GRAD, NORM, 8>(a, st);
-  if (a.hd <= 256) return launch_width<E, LAYOUT, GRAD, NORM, 16>(a, st);
-  return launch_width<E, LAYOUT, GRAD, NORM, 32>(a, st);
+  if (a.hd <= 64) return launch_width<E, LAYOUT, GRAD, NORM, V, 32 / V>(a, st);
+  if (a.hd <= 128) return launch_width<E, LAYOUT, GRAD, NORM, V, 64 / V>(a, st);
+  if (a.hd <= 256) return launch_width<E, LAYOUT, GRAD, NORM, V, 128 / V>(a, st);
+  return launch_width<E, LAYOUT, GRAD, NORM, V, 256 / V>(a, st);
+}
+
+template <class E, int LAYOUT, int V>
+void launch_kind(bool grad, const RopeArgs& a, float* q_dgain, float* k_dgain, hipStream_t st) {
+  if (!grad) {
+    if (a.q_gain) launch_vector<E, LAYOUT, false, true, V>(a, st);
+    else launch_vector<E, LAYOUT, false, false, V>(a, st);
+  } else if (!a.q_gain) {
+    launch_vector<E, LAYOUT, true, false, V>(a, st);
+  } else {
+    const int blocks = launch_vector<E, LAYOUT, true, true, V>(a, st);
+    k_rope_gain_sum<<<2 * a.hd, 64, 0, st>>>(a.part, blocks, a.hd, a.n_k, q_dgain, k_dgain);
+  }
 }
 
 template <class E, int LAYOUT>
 hipError_t launch_layout(bool grad, const RopeArgs& a, float* q_dgain, float* k_dgain, hipStream_t st) {
   const int64_t units = (int64_t)a.rows * (a.n_q + a.n_k);
   const int blocks = (int)std::min<int64_t>((units + 3) / 4, 4096);
-  if (units > 0 && vectorised<E>(grad, a)) {
-    if (!grad) {
-      if (a.q_gain) launch_vector<E, LAYOUT, false, true>(a, st);
-      else launch_vector<E, LAYOUT, false, false>(a, st);
-    } else if (!a.q_gain) {
-      launch_vector<E, LAYOUT, true, false>(a, st);
-    } else {
-      const int blocks = launch_vector<E, LAYOUT, true, true>(a, st);
-      k_rope_gain_sum<<<2 * a.hd, 64, 0, st>>>(a.part, blocks, a.hd, a.n_k, q_dgain, k_dgain);
-    }
+  if (units > 0 && vectorised<E>(8, grad, a)) {
+    launch_kind<E, LAYOUT, 8>(grad, a, q_dgain, k_dgain, st);
+    return hipGetLastError();
+  }
+  if (units > 0 && vectorised<E>(4, grad, a)) {
+    launch_kind<E, LAYOUT, 4>(grad, a, q_dgain, k_dgain, st);
     return hipGetLastError();
   }
   if (grad && a.q_gain) {

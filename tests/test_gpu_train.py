@@ -34,7 +34,9 @@ def _gen(seed):
 # rows, query heads, key heads, head_dim, turned dims
 ROPE_SHAPES = [(1, 1, 1, 64, 64), (3, 2, 1, 64, 32), (67, 14, 2, 64, 64), (40, 32, 8, 128, 128), (33, 5, 1, 80, 80), (9, 3, 3, 96, 48),
                (7, 4, 2, 256, 128), (5, 2, 2, 6, 4), (4, 3, 1, 34, 34), (300, 1, 1, 2, 2), (6, 2, 1, 1024, 1024), (11, 2, 0, 64, 64),
-               (129, 7, 3, 112, 16), (2, 1, 1, 512, 512), (2, 1, 1, 528, 528)]
+               (129, 7, 3, 112, 16), (2, 1, 1, 512, 512), (2, 1, 1, 528, 528),
+               (41, 5, 1, 80, 40), (13, 3, 2, 24, 8), (70, 8, 8, 40, 40), (5, 2, 1, 264, 136), (3, 2, 2, 504, 8), (500, 3, 1, 72, 24),
+               (2500, 2, 1, 64, 64), (3000, 1, 1, 8, 8)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
