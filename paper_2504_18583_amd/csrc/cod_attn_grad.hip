@@ -62,6 +62,8 @@ __global__ __launch_bounds__(256, 2) void k_cod_dq(const CodAttnArgs a) {
   const CodSampleInfo s = tile.s;
   const int pair0 = (rest % per_tile) * 64 * NQ, p0 = tile.tile * kCodTile;
   if (p0 + pair0 / group >= s.cap) return;           // uniform
+  // (a chain has at most reach + 1 places, so place p sees more than p / (reach + 1) tokens)
+  if (FIND && p0 >= 2 * kStage * (s.reach + 1)) return;   // uniform
   const int4* const order = a.plan.order + s.off;
   const int last = s.len - 1;
   // (as in the forward kernel: the places of all rows read first, then the rows)
