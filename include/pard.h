@@ -514,6 +514,8 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads 
  *   d_logits = grad_scale * d loss[0] / d logits (may be null: loss only; may
  *              be logits itself, same data and stride, but not overlap it
  *              otherwise); rows that do not count get 0
+ * pard_cod_build leaves a region's rows past out_len as they were: the caller
+ * sets their labels below 0.
  * A label of vocab or more makes its row's loss and gradient NaN.  Sums are
  * float32, means over rows float64.  logits, d_logits: dtype (PARD_F32,
  * PARD_BF16, PARD_F16), [rows][vocab] with row strides in elements; loss:

@@ -13,6 +13,13 @@
 //     stages through LDS.  Mask rows are seen by the rows of
 //     their chain alone: workgroups behind those own 64 places of the order and
 //     walk the pairs from the first place to the last chain's end.
+//
+// Both recompute the scores (9 products in place of 7 with the forward's), since
+// neither dQ nor dK and dV of a sample fit on chip.  Bound: the SIMDs' issue, as
+// in the forward: at head_dim 64 the products' cycles (36 % of the kernel's for
+// dQ, 41 % for dK and dV) and the other instructions' add up to 83 %.  1B layer (16 samples of 256 to 1024 tokens, 32 / 8 heads x 64):
+// delta 40, dQ 330, dK and dV 450 us; 8B heads (x 128, 6 samples of 900 to 2048):
+// 35, 655 and 975.  Scalar kernels took 160 and 557 ms.
 #include "cod_attn_tile.h"
 
 namespace pard {
@@ -22,9 +29,10 @@ using namespace cod;
 
 constexpr int kStage = 64;                           // keys of a stage (dq)
 // Blocks of 16 keys of a dkv wavefront: at head_dim 128 the sums of two, with K
-// and V, leave too few registers.
+// and V, leave too few registers (1700 us with spills, 1250 with V in LDS).
 constexpr int dkv_blocks(int hd) { return hd == 64 ? 2 : 1; }
-// Pairs of a stage (dkv): three workgroups' stages fit a CU's LDS.
+// Pairs of a stage (dkv): three workgroups' stages fit a CU's LDS (head_dim 128:
+// 64 pairs, two workgroups, took 1110 us).
 constexpr int dkv_pairs(int hd) { return hd == 64 ? 64 : 32; }
 
 // Statistics of 64 pairs of one key head: base-2 log-sum (+infinity past the
@@ -368,10 +376,12 @@ __device__ __forceinline__ void store_dkv(const CodAttnArgs& a, uint32_t row, in
 
 // Four wavefronts, of which several workgroups share a CU: between two barriers a
 // wavefront's LDS reads, products and exponentials follow each other, and other
-// workgroups fill the units meanwhile.  Real tokens: wavefront w has keys 16 NK w
+// workgroups fill the units meanwhile (8 and 12 wavefronts over a ring of stages
+// took 600 to 800 us in place of 450).  Real tokens: wavefront w has keys 16 NK w
 // .. of the workgroup's 64 NK; mask rows: 16 of 64 places.  The pairs are walked
 // from the last to the first, so that the tiles of a sample, which all end with
-// its last pair, read the same stages at the same time.
+// its last pair, read the same stages at the same time (the loads alone at
+// head_dim 128: 460 us, 616 from the first on).
 template <int HD, class M>
 __global__ __launch_bounds__(256, 3) void k_cod_dkv(const CodAttnArgs a, unsigned real_blocks) {
   constexpr int NK = dkv_blocks(HD), KW = 16 * NK;   // keys per wavefront

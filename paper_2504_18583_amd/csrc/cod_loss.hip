@@ -9,7 +9,11 @@
 // 16-byte vectors stay in the registers of one workgroup (at most 20 a thread
 // of 1024: 163 840 logits of two bytes) from the sum to the gradient, and as
 // soon as a vector's gradient is stored, its registers take the same vector of
-// the workgroup's next row.  Longer rows are read a second time.
+// the workgroup's next row.  Longer rows are read a second time.  4099 rows of
+// 128 256 bf16 logits with gradients: 520 us, 4.0 TB/s of a large copy's 4.9 (the
+// row's two barriers, and 20 vectors' registers leave one workgroup a CU); 2050
+// rows of 152 064 f16 logits alone: 127 us, 4.9 TB/s.  Element by
+// element, rows with gradients read twice, took 1414 and 398 us.
 #include "train.h"
 
 #include <algorithm>
@@ -316,6 +320,7 @@ hipError_t launch_rows(const CodLossArgs& a, hipStream_t st) {
   const int n = (a.vocab + N - 1) / N;               // vectors of a row
   const bool same = !a.d_logits || ((a.logits - a.d_logits) % 16 == 0 && (a.rows == 1 || (a.stride - a.d_stride) * SZ % 16 == 0));
   if (!same) launch_variant<E, 1024, 4, false, true>(a, st);
+  // (no gradient: 512 threads, 139 us where 1024 took 181)
   else if (!a.d_logits || n > 20480) n <= 1024 ? launch_variant<E, 256, 4, false>(a, st) : launch_variant<E, 512, 8, false>(a, st);
   else if (n <= 256) launch_variant<E, 256, 1, true>(a, st);
   else if (n <= 1024) launch_variant<E, 256, 4, true>(a, st);
