@@ -393,7 +393,7 @@ def qk_rope(q, k, positions, table, layout: str = "half", q_gain=None, k_gain=No
     (q_out, k_out), new tensors unless given; they may be q and k themselves."""
     import torch
     hq = _heads(q, "q")
-    hk = None if k is None else _heads(k, "k", q, (q.shape[0], k.shape[1], q.shape[2]))
+    hk = None if k is None else _heads(k, "k", q, (*q.shape[:1], *k.shape[1:2], *q.shape[2:]))
     args = _rope_args(q, k, positions, table, layout, q_gain, k_gain, eps)
     with _On(q.device, stream, q, k, positions, table, q_gain, k_gain, q_out, k_out) as on:
         if q_out is None:
@@ -413,7 +413,7 @@ def qk_rope_grad(q_dy, k_dy, positions, table, layout: str = "half", q=None, k=N
     None without gains; q_dx and k_dx may be q_dy and k_dy themselves."""
     import torch
     hdq = _heads(q_dy, "q_dy")
-    hdk = None if k_dy is None else _heads(k_dy, "k_dy", q_dy, (q_dy.shape[0], k_dy.shape[1], q_dy.shape[2]))
+    hdk = None if k_dy is None else _heads(k_dy, "k_dy", q_dy, (*q_dy.shape[:1], *k_dy.shape[1:2], *q_dy.shape[2:]))
     args = _rope_args(q_dy, k_dy, positions, table, layout, q_gain, k_gain, eps)
     hq = hk = None
     if q_gain is not None:
@@ -428,7 +428,7 @@ def qk_rope_grad(q_dy, k_dy, positions, table, layout: str = "half", q=None, k=N
         oq = _heads(q_dx, "q_dx", q_dy, q_dy.shape)
         ok = None if k_dy is None else _heads(k_dx, "k_dx", k_dy, k_dy.shape)
         q_dg = None if q_gain is None else new(q_gain)
-        k_dg = None if q_gain is None or k_dy is None else new(k_gain)
+        k_dg = None if q_gain is None or k_dy is None else new(k_gain) if k_dy.shape[1] else torch.zeros_like(k_gain)
         n_ws = lib.pard_qk_rope_workspace_bytes(args) if q_gain is not None else 0
         ws = _workspace(n_ws, q_dy.device) if n_ws else None
         _done(lib.pard_qk_rope_grad(args, hdq, hdk, hq, hk, oq, ok, q_dg.data_ptr() if q_dg is not None else None,
@@ -474,6 +474,8 @@ def cod_plan(section, column, out_offsets: Sequence[int], out_len, stream=None) 
 
 
 def _attn_args(q, k, v, plan: CodPlan, scale):
+    if q.dim() != 3:
+        _bad(f"q: a [rows, heads, head_dim] device tensor is wanted, got {tuple(q.shape)}")
     rows, n_q, hd = q.shape
     if plan.device != q.device:
         _bad(f"cod_attn: the plan is on {plan.device}, the tensors on {q.device}")

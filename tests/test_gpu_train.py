@@ -229,6 +229,61 @@ def test_attention(B, lengths, k_max, heads, hd, dtype):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+def test_attention_many_query_heads_of_a_key_head(B, hd):
+    """Groups that fill a wavefront's pairs, a workgroup's, and neither evenly."""
+    for heads in ((33, 1), (64, 2), (130, 1)):
+        _check_attn(B, [23, 6], 4, *heads, hd, "bf16", slack=1)
+
+
+def test_strides_that_pass_32_bits(B):
+    """Rows whose byte offsets pass 2^32: the results of the same rows close together."""
+    g, hq, hk, hd = _gen(77), 4, 2, 64
+    section, column, offs, lens, rows = T.pack([200, 400], 4)
+    plan = _plan(B, section, column, offs, lens)
+    wide = (1 << 32) // rows // 16 * 16 + 4096       # elements a row: the last half of the rows is past 2^32 bytes
+    assert rows * wide * 2 > 1 << 33
+    near = _attn_inputs(g, rows, hq, hk, hd, torch.bfloat16)
+    d_out = _randn(g, rows, hq, hd, dtype=torch.bfloat16)
+    big = torch.empty(rows, wide, device="cuda", dtype=torch.bfloat16)
+    at = 0
+    def place(t):
+        nonlocal at
+        n = t.shape[1] * hd
+        view = big[:, at:at + n].unflatten(1, (t.shape[1], hd))
+        at += n
+        return view.copy_(t)
+    far = [place(t) for t in near]
+    out, lse = B.cod_attn(*near, plan)
+    fout, flse = B.cod_attn(*far, plan, out=place(torch.zeros_like(near[0])))
+    assert torch.equal(out, fout) and torch.equal(lse, flse)
+    grads = B.cod_attn_grad(d_out, *near, out, lse, plan)
+    fgrads = B.cod_attn_grad(place(d_out), *far, fout, flse, plan, dq=place(torch.zeros_like(near[0])),
+                             dk=place(torch.zeros_like(near[1])), dv=place(torch.zeros_like(near[2])))
+    assert all(torch.equal(a, b) for a, b in zip(grads, fgrads))
+    table, gain = B.rope_table(512, hd, 1e4), 1 + _randn(g, hd, std=0.1)
+    pos = torch.from_numpy(np.clip(column, 0, 511)).cuda()
+    want = B.qk_rope(near[0], near[1], pos, table, "half", gain, gain)
+    got = B.qk_rope(far[0], far[1], pos, table, "half", gain, gain, q_out=far[0], k_out=far[1])
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    del big, far, fout, fgrads, got
+    logits = torch.zeros(20_000, 128_256, device="cuda", dtype=torch.bfloat16)      # 5.1 GB
+    logits[-3:] = _randn(g, 3, 128_256, dtype=torch.bfloat16)
+    labels = torch.full((20_000,), -1, device="cuda", dtype=torch.int32)
+    labels[-3:] = torch.tensor([5, 100_000, 128_255], device="cuda", dtype=torch.int32)
+    want = B.cod_loss(logits[-3:].clone(), labels[-3:], None, 1)
+    got = B.cod_loss(logits, labels, None, 1, d_logits=logits)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[2], got[2][-3:]) and torch.equal(want[3], logits[-3:])
+    assert not logits[:-3].any()
+
+
+def test_rope_gradient_of_no_key_heads(B):
+    q, k = torch.ones(4, 2, 64, device="cuda"), torch.ones(4, 0, 64, device="cuda")
+    pos, g = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda")
+    _, dk, dg, dgk = B.qk_rope_grad(q, k, pos, B.rope_table(8, 64, 1e4), q=q, k=k, q_gain=g, k_gain=g)
+    assert dk.shape == (4, 0, 64) and dg.isfinite().all() and torch.equal(dgk, torch.zeros_like(g))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 def test_attention_everything_kept(B, hd):
     """r = 1: every chain is K long (K = 64: chains longer than a wavefront's rows)."""
     _check_attn(B, [90], 64, 2, 1, hd, "f16", r=1.0)
