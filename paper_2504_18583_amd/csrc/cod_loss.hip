@@ -6,10 +6,10 @@
 // workgroup to end adds the workgroups' sums up (in their order).
 //
 // Bound: memory (the logits in, the gradient out).  So a row is read once: its
-// 16-byte vectors stay in the registers of one workgroup (at most 20 a thread
-// of 1024: 163 840 logits of two bytes) from the sum to the gradient, and as
-// soon as a vector's gradient is stored, its registers take the same vector of
-// the workgroup's next row.  Longer rows are read a second time.  4099 rows of
+// 16-byte vectors stay in the registers of one wavefront (up to 16 KiB) or
+// workgroup (at most 20 a thread of 1024: 163 840 logits of two bytes) from the
+// sum to the gradient, and as soon as a vector's gradient is stored, its registers
+// take the same vector of the next row.  Longer rows are read a second time.  4099 rows of
 // 128 256 bf16 logits with gradients: 520 us, 4.0 TB/s of a large copy's 4.9 (the
 // row's two barriers, and 20 vectors' registers leave one workgroup a CU); 2050
 // rows of 152 064 f16 logits alone: 127 us, 4.9 TB/s.  Element by
@@ -113,26 +113,31 @@ __device__ __forceinline__ void add_vectors(const LossVec<E>* v, float& m, float
     for (int i = 0; i < N; ++i) l += __builtin_amdgcn_exp2f((v[c][i] - ref) * kLog2e);
 }
 
-// Rows of T threads, NV vectors each.  A row's elements before its first 16-byte
+// Rows of T threads, NV vectors each; a workgroup's R sets of T threads take rows
+// of their own (T = 64: a wavefront a row, no barrier).  A row's elements before its first 16-byte
 // boundary and after its last are a thread's own each (fewer than T).
 // RESIDENT: the vectors stay in registers, and the next row's follow them in;
 // otherwise they are read NV at a time, twice where there is a gradient.
 // SCALAR_OUT: the gradient's rows lie at other offsets from a 16-byte boundary.
-template <class E, int T, int NV, bool RESIDENT, bool SCALAR_OUT>
-__global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
+template <class E, int T, int R, int NV, bool RESIDENT, bool SCALAR_OUT>
+__global__ __launch_bounds__(T * R) void k_loss_row(const CodLossArgs a) {
   using Vec = LossVec<E>;
   using Elem = typename E::T;
   constexpr int N = Vec::N, SZ = sizeof(Elem), W = T / 64;
   constexpr int C = NV % (16 / N) == 0 ? 16 / N : 1;   // vectors added at a time: 16 logits
   __shared__ float m_s[2][W], l_s[2][W];
   __shared__ int n_s[kCodMaxSections];
-  __shared__ double sum_s[kCodMaxSections];          // this workgroup's losses, in its rows' order
+  static_assert(R == 1 || T == 64, "sets of several wavefronts would meet at the rows' barriers");
+  __shared__ double sum_s[R][kCodMaxSections];       // each set's losses, in its rows' order
   __shared__ int last_s;
-  for (int q = threadIdx.x; q < a.n_sections; q += T) sum_s[q] = 0.0;
+  for (int q = threadIdx.x; q < R * kCodMaxSections; q += T * R) sum_s[q / kCodMaxSections][q % kCodMaxSections] = 0.0;
   load_counts(a, n_s);
   int n_all = 0;
   for (int q = 0; q < a.n_sections; ++q) n_all += n_s[q];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // (sets of one wavefront: in scalar registers)
+  const int set = R == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / T);
+  const int tid = threadIdx.x - set * T, lane = tid & 63, wave = tid >> 6;
+  const int row0 = blockIdx.x * R + set, row_step = gridDim.x * R;
   Vec v[NV];
   float edge = -INFINITY;                            // this thread's element outside the vectors
   float x_label = 0.f;
@@ -173,13 +178,13 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
     label = a.labels[r];
   };
   const int rounds = RESIDENT ? 1 : (a.vocab / N + NV * T - 1) / (NV * T);
-  if (RESIDENT && (int)blockIdx.x < a.rows) {
-    shape(blockIdx.x);
+  if (RESIDENT && row0 < a.rows) {
+    shape(row0);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) fetch(row_of(blockIdx.x), 0, i);
+    for (int i = 0; i < NV; ++i) fetch(row_of(row0), 0, i);
   }
   int turn = 0;
-  for (int r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
+  for (int r = row0; r < a.rows; r += row_step, turn ^= 1) {
     const Elem* const x = row_of(r);
     Elem* const d = RESIDENT || a.d_logits ? reinterpret_cast<Elem*>(a.d_logits) + r * a.d_stride : nullptr;
     shape(r);
@@ -205,25 +210,31 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
       const float om = __shfl_xor(m, off), ol = __shfl_xor(l, off);
       join(m, l, om, ol);
     }
-    if (lane == 0) {
-      m_s[turn][wave] = m;
-      l_s[turn][wave] = l;
+    // (also: x[label] is read before d, which may be x, is written)
+    if (W > 1) {
+      if (lane == 0) {
+        m_s[turn][wave] = m;
+        l_s[turn][wave] = l;
+      }
+      __syncthreads();
+      m = m_s[turn][0];
+      l = l_s[turn][0];
+      for (int w = 1; w < W; ++w) join(m, l, m_s[turn][w], l_s[turn][w]);
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0)
+      asm volatile("" ::: "memory");
     }
-    __syncthreads();                                 // (also: x[label] is read before d, which may be x, is written)
-    m = m_s[turn][0];
-    l = l_s[turn][0];
-    for (int w = 1; w < W; ++w) join(m, l, m_s[turn][w], l_s[turn][w]);
     const float log2_l = log2f(l);                   // log sum exp = m + ln(l)
     if (tid == 0) {
       const float ce = k > 0 ? fmaf(log2_l, kLn2, m - x_label) : 0.f;
       if (a.row_loss) a.row_loss[r] = ce;
-      if (k > 0) sum_s[k - 1] += ce;
+      if (k > 0) sum_s[set][k - 1] += ce;
     }
     if (!RESIDENT && !d) continue;
     const float w = k == 0 ? 0.f : label >= a.vocab ? __builtin_nanf("")
                            : a.weighted ? a.weights[k - 1] * a.grad_scale / n_s[k - 1] : a.grad_scale / n_all;
     const int n_now = n_vec, head_now = head;
-    const int r_next = min((int64_t)r + gridDim.x, (int64_t)a.rows - 1);   // (past the last row: that one again, unused)
+    const int r_next = min((int64_t)r + row_step, (int64_t)a.rows - 1);   // (past the last row: that one again, unused)
     const Elem* const next = row_of(r_next);
     if (RESIDENT) shape(r_next);
     const char* const x_base = reinterpret_cast<const char*>(x + head_now);
@@ -268,9 +279,13 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
   // the workgroups' sums: [workgroup][subtask]
   // (device-scope stores, complete before the ticket, and device-scope loads
   // after it: a release and an acquire would write back and drop whole caches)
-  if (tid == 0) {
-    for (int q = 0; q < a.n_sections; ++q)
-      __hip_atomic_store(&a.sums[(size_t)blockIdx.x * a.n_sections + q], sum_s[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (R > 1) __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int q = 0; q < a.n_sections; ++q) {
+      double s = 0.0;
+      for (int i = 0; i < R; ++i) s += sum_s[i][q];
+      __hip_atomic_store(&a.sums[(size_t)blockIdx.x * a.n_sections + q], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
     asm volatile("" ::: "memory");
@@ -278,7 +293,7 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
   }
   __syncthreads();
   if (!last_s) return;                               // uniform
-  for (int q = wave; q < a.n_sections; q += W) {     // a wavefront a subtask
+  for (int q = threadIdx.x / 64; q < a.n_sections; q += W * R) {   // a wavefront a subtask
     double s = 0.0;
     for (int b0 = lane; b0 < (int)gridDim.x; b0 += 64 * 16) {   // 16 loads in flight
       double x[16];
@@ -293,41 +308,54 @@ __global__ __launch_bounds__(T) void k_loss_row(const CodLossArgs a) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
     if (lane == 0) {
-      sum_s[q] = s;
+      sum_s[0][q] = s;
       a.loss[1 + q] = n_s[q] ? (float)(s / n_s[q]) : 0.f;
     }
   }
   __syncthreads();
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     double total = 0.0;
-    for (int q = 0; q < a.n_sections; ++q) total += a.weighted ? (n_s[q] ? a.weights[q] * (sum_s[q] / n_s[q]) : 0.0) : sum_s[q];
+    for (int q = 0; q < a.n_sections; ++q)
+      total += a.weighted ? (n_s[q] ? a.weights[q] * (sum_s[0][q] / n_s[q]) : 0.0) : sum_s[0][q];
     a.loss[0] = (float)(a.weighted ? total : n_all ? total / n_all : 0.0);
   }
 }
 
-template <class E, int T, int NV, bool RESIDENT, bool SCALAR_OUT = false>
+template <class E, int T, int R, int NV, bool RESIDENT, bool SCALAR_OUT = false>
 void launch_variant(const CodLossArgs& a, hipStream_t st) {
-  // resident rows: as many workgroups as the device holds at once (of 1024
-  // threads one a CU, of 256 eight), each with several rows
-  const int most = !RESIDENT ? kLossMaxBlocks : T == 1024 ? 256 : 2048;
-  k_loss_row<E, T, NV, RESIDENT, SCALAR_OUT><<<std::max(1, std::min(a.rows, most)), T, 0, st>>>(a);
+  // short and resident rows: as many workgroups as 256 CUs hold at once (1024
+  // threads a CU, 2048 of those with few vectors), each with several rows
+  const int most = RESIDENT || T <= 256 ? 256 * (NV <= 8 ? 2048 : 1024) / (T * R) : kLossMaxBlocks;
+  const int blocks = std::max(1, std::min((a.rows + R - 1) / R, most));
+  k_loss_row<E, T, R, NV, RESIDENT, SCALAR_OUT><<<blocks, T * R, 0, st>>>(a);
 }
 
+// A row's threads: as few as hold it with 8 or 16 vectors each, so that a CU has
+// several rows, which wait at different times (bf16 with gradients: 60 000 rows of
+// 1024 logits 95 us by wavefronts, 180 by 256 threads; 30 000 of 4096 132 and 167;
+// 4000 of 32 000 113 by 256 threads, 149 by 1024).
 template <class E>
 hipError_t launch_rows(const CodLossArgs& a, hipStream_t st) {
   constexpr int N = LossVec<E>::N, SZ = 16 / N;
   k_loss_count<<<kLossCountBlocks, kLossThreads, 0, st>>>(a);
   const int n = (a.vocab + N - 1) / N;               // vectors of a row
   const bool same = !a.d_logits || ((a.logits - a.d_logits) % 16 == 0 && (a.rows == 1 || (a.stride - a.d_stride) * SZ % 16 == 0));
-  if (!same) launch_variant<E, 1024, 4, false, true>(a, st);
-  // (no gradient: 512 threads, 139 us where 1024 took 181)
-  else if (!a.d_logits || n > 20480) n <= 1024 ? launch_variant<E, 256, 4, false>(a, st) : launch_variant<E, 512, 8, false>(a, st);
-  else if (n <= 256) launch_variant<E, 256, 1, true>(a, st);
-  else if (n <= 1024) launch_variant<E, 256, 4, true>(a, st);
-  else if (n <= 4096) launch_variant<E, 1024, 4, true>(a, st);
-  else if (n <= 8192) launch_variant<E, 1024, 8, true>(a, st);
-  else if (n <= 16384) launch_variant<E, 1024, 16, true>(a, st);
-  else launch_variant<E, 1024, 20, true>(a, st);
+  if (!same) launch_variant<E, 1024, 1, 4, false, true>(a, st);
+  else if (!a.d_logits || n > 20480) {
+    // (2050 rows of 152 064 logits: 512 threads 139 us, 1024 181)
+    if (n <= 256) launch_variant<E, 64, 4, 4, false>(a, st);
+    else if (n <= 1024) launch_variant<E, 64, 4, 8, false>(a, st);
+    else if (n <= 4096) launch_variant<E, 256, 1, 8, false>(a, st);
+    else launch_variant<E, 512, 1, 8, false>(a, st);
+  }
+  else if (n <= 64) launch_variant<E, 64, 4, 1, true>(a, st);
+  else if (n <= 256) launch_variant<E, 64, 4, 4, true>(a, st);
+  else if (n <= 1024) launch_variant<E, 64, 4, 16, true>(a, st);
+  else if (n <= 2048) launch_variant<E, 256, 1, 8, true>(a, st);
+  else if (n <= 4096) launch_variant<E, 256, 1, 16, true>(a, st);
+  else if (n <= 8192) launch_variant<E, 512, 1, 16, true>(a, st);
+  else if (n <= 16384) launch_variant<E, 1024, 1, 16, true>(a, st);
+  else launch_variant<E, 1024, 1, 20, true>(a, st);
   return hipGetLastError();
 }
 

@@ -488,7 +488,9 @@ def test_loss_in_place_and_strided(B):
 
 
 @pytest.mark.parametrize("dtype,rows,vocab", [("bf16", 2500, 40), ("f16", 2049, 2000), ("f32", 300, 4100), ("bf16", 270, 40_001),
-                                              ("f32", 4500, 33)])
+                                              ("f32", 4500, 33), ("bf16", 9000, 40), ("f32", 8300, 700), ("f32", 4200, 3001),
+                                              ("f32", 2100, 5002), ("f32", 1100, 9003), ("f32", 530, 20_001), ("f32", 260, 40_003),
+                                              ("f16", 258, 150_001)])
 def test_loss_more_rows_than_workgroups(B, dtype, rows, vocab):
     """Rows that a workgroup takes after its first, with gradients in tensors at
     another place in 16 bytes, and without."""
