@@ -301,9 +301,10 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_s
       }
   }
   const float inv_hd = 1.0f / a.hd;
-  const int row_end = min((int64_t)a.rows, ((int64_t)blockIdx.x + 1) * rows_per_block);
-  for (int row = blockIdx.x * rows_per_block + row_slot; row < row_end; row += row_step) {
-    const int pos = a.pos[row];
+  // (counted from the workgroup's first row: a row index past the last may not fit an int)
+  const int row0 = blockIdx.x * rows_per_block, n_rows = min(a.rows - row0, rows_per_block);
+  for (int i_row = row_slot; i_row < n_rows; i_row += row_step) {
+    const int row = row0 + i_row, pos = a.pos[row];
     const bool ok = pos >= 0 && pos < a.n_pos;
     float c[V] = {}, s[V] = {};
     if (turns) {
