@@ -342,7 +342,9 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int h_s
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        if (!NORM && !live[j]) continue;
+        // (a head's lanes leave together: its sums stay whole.  A head that is not
+        // there has no norm: with eps = 0 it would leave NaN in the gains' sums)
+        if (NORM ? hb + j * h_step >= heads : !live[j]) continue;
         float x[2][V], y[2][V];
         if (live[j]) {
           v[j][0].get(x[0]);

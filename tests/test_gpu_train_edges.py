@@ -59,3 +59,29 @@ def test_rope_of_the_most_rows(B, rows):
         _, _, dg, _ = B.qk_rope_grad(d, None, pos, table, q=x, q_gain=norm, q_dx=d)
         check(d, want, "gradient")
         assert norm is None or dg.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("shape", [(77, 32, 8, 128, 128), (5, 2, 1, 64, 64), (300, 2, 1, 64, 32), (41, 5, 1, 80, 40), (9, 3, 2, 24, 8),
+                                   (33, 3, 0, 64, 64), (7, 4, 2, 256, 128), (6, 3, 1, 34, 34)], ids=str)
+def test_rope_norm_without_epsilon(B, shape, layout, dtype):
+    """eps = 0 and no head of zeros: finite sums, also where the heads are no
+    multiple of those that a workgroup takes together."""
+    rows, hq, hk, hd, rot = shape
+    g, dt = _gen(rows + hd), T.DTYPES[dtype]
+    say(f"[gpu] rope without epsilon {shape} {layout} {dtype}")
+    table = B.rope_table(50, rot, 1e4)
+    pos = torch.randint(0, 50, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    q, dq = (_randn(g, rows, hq, hd, dtype=dt) for _ in range(2))
+    k, dk = (_randn(g, rows, hk, hd, dtype=dt) if hk else None for _ in range(2))
+    gq, gk = 1 + _randn(g, hd, std=0.2), 1 + _randn(g, hd, std=0.2) if hk else None
+    yq, yk = B.qk_rope(q, k, pos, table, layout, gq, gk, eps=0.0)
+    xq, xk, gdq, gdk = B.qk_rope_grad(dq, dk, pos, table, layout, q, k, gq, gk, eps=0.0)
+    for name, x, y, gain, dy, dx, dg in (("q", q, yq, gq, dq, xq, gdq), ("k", k, yk, gk, dk, xk, gdk)):
+        if x is None:
+            continue
+        T.assert_within(y, *T.rope_ref(x, pos, table, layout, gain, 0.0), name)
+        want, bound, want_g, bound_g = T.rope_grad_ref(dy, x, pos, table, layout, gain, 0.0)
+        T.assert_within(dx, want, bound, f"d{name}")
+        T.assert_within(dg, want_g, bound_g, f"d{name} gain")
