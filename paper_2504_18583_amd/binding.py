@@ -303,6 +303,15 @@ def _vector(t, what: str, n: int, dtype, device) -> int:
     return t.data_ptr()
 
 
+def _no_graph(what: str, grad_of: str) -> None:
+    """Turns away tensors that require gradients where torch would record them:
+    what the library returns has no graph, and a model would train without this part."""
+    import torch
+    if torch.is_grad_enabled():
+        _bad(f"{what} records no gradient for tensors that require one: call it in a torch.autograd.Function whose "
+             f"backward calls {grad_of}, or under torch.no_grad()")
+
+
 class _On:
     """Runs a call on `stream` (a torch stream; None: the device's current one)
     with that device current: outputs and workspaces made inside belong to the
@@ -390,8 +399,13 @@ def qk_rope(q, k, positions, table, layout: str = "half", q_gain=None, k_gain=No
             k_out=None, stream=None):
     """Rotary positions of queries and keys [rows, heads, head_dim], with gains
     after an RMSNorm of every head (pard_qk_rope).  k may be None.  Returns
-    (q_out, k_out), new tensors unless given; they may be q and k themselves."""
+    (q_out, k_out), new tensors unless given; they may be q and k themselves.
+    Records no graph: where torch records gradients, tensors that require them
+    are turned away (qk_rope_grad is the gradient)."""
     import torch
+    if (q.requires_grad or k is not None and k.requires_grad or q_gain is not None and q_gain.requires_grad
+            or k_gain is not None and k_gain.requires_grad):
+        _no_graph("qk_rope", "qk_rope_grad")
     hq = _heads(q, "q")
     hk = None if k is None else _heads(k, "k", q, (*q.shape[:1], *k.shape[1:2], *q.shape[2:]))
     args = _rope_args(q, k, positions, table, layout, q_gain, k_gain, eps)
@@ -491,8 +505,11 @@ def cod_attn(q, k, v, plan: CodPlan, scale: Optional[float] = None, out=None, st
     """Attention over packed rows (pard_cod_attn): q [rows, heads, head_dim], k
     and v [rows, kv heads, head_dim]; scale: head_dim ** -0.5 unless given.
     Returns (out, lse), lse [heads, plan rows] in float32.  Rows that belong to
-    no sample's region are left as they are (out given) or hold nothing (new)."""
+    no sample's region are left as they are (out given) or hold nothing (new).
+    Records no graph, as qk_rope (cod_attn_grad is the gradient)."""
     import torch
+    if q.requires_grad or k.requires_grad or v.requires_grad:
+        _no_graph("cod_attn", "cod_attn_grad")
     args, (hq, hk, hv) = _attn_args(q, k, v, plan, scale)
     with _On(q.device, stream, q, k, v, plan.data, out) as on:
         if out is None:
@@ -530,7 +547,8 @@ def cod_loss(logits, labels, section, n_sections: int, weights: Optional[Sequenc
     labels, section: int32 [rows] (cod_build's; section None: one subtask);
     weights: of the subtasks' means, None: the mean over all counted rows.
     Returns (loss [], subtask means [n_sections], row losses [rows], d_logits or
-    None); d_logits may be logits itself."""
+    None); d_logits may be logits itself.  The loss has no graph: gradients go on
+    from d_logits (logits.backward(d_logits))."""
     import torch
     if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
         _bad("cod_loss: logits: a [rows, vocab] device tensor with contiguous rows is wanted")

@@ -85,3 +85,52 @@ def test_rope_norm_without_epsilon(B, shape, layout, dtype):
         want, bound, want_g, bound_g = T.rope_grad_ref(dy, x, pos, table, layout, gain, 0.0)
         T.assert_within(dx, want, bound, f"d{name}")
         T.assert_within(dg, want_g, bound_g, f"d{name} gain")
+
+
+def test_attention_and_rotation_in_autograd(B):
+    """The calls inside autograd Functions: their gradients, bit for bit, and in
+    place of a graph without them an error."""
+    section, column, offs, lens, rows = T.pack([40, 9], 4)
+    plan = B.cod_plan(torch.from_numpy(section).cuda(), torch.from_numpy(column).cuda(), offs, torch.from_numpy(lens).cuda())
+    table, pos = B.rope_table(64, 64, 1e4), torch.from_numpy(column).cuda()
+    g = _gen(5)
+
+    class Rotated(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, gq, gk):
+            ctx.save_for_backward(q, k, gq, gk)
+            return B.qk_rope(q, k, pos, table, q_gain=gq, k_gain=gk)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            q, k, gq, gk = ctx.saved_tensors
+            return B.qk_rope_grad(dq, dk, pos, table, q=q, k=k, q_gain=gq, k_gain=gk)
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v):
+            out, lse = B.cod_attn(q, k, v, plan)
+            ctx.save_for_backward(q, k, v, out, lse)
+            return out
+
+        @staticmethod
+        def backward(ctx, d_out):
+            return B.cod_attn_grad(d_out, *ctx.saved_tensors, plan)
+
+    q, k, v = (_randn(g, rows, h, 64, dtype=torch.bfloat16).requires_grad_() for h in (4, 2, 2))
+    gq, gk = (1 + _randn(g, 64, std=0.1) for _ in range(2))
+    gq.requires_grad_(), gk.requires_grad_()
+    with pytest.raises(B.PardError, match="autograd.Function"):
+        B.cod_attn(q, k, v, plan)
+    with pytest.raises(B.PardError, match="autograd.Function"):
+        B.qk_rope(q.detach(), k.detach(), pos, table, q_gain=gq, k_gain=gk)
+    d_out = _randn(g, rows, 4, 64, dtype=torch.bfloat16)
+    rq, rk = Rotated.apply(q, k, gq, gk)
+    Attention.apply(rq, rk, v).backward(d_out)
+    with torch.no_grad():
+        sq, sk = B.qk_rope(q, k, pos, table, q_gain=gq, k_gain=gk)
+        out, lse = B.cod_attn(sq, sk, v, plan)
+        dq, dk, dv = B.cod_attn_grad(d_out, sq, sk, v, out, lse, plan)
+        want = (*B.qk_rope_grad(dq, dk, pos, table, q=q, k=k, q_gain=gq, k_gain=gk), dv)
+    for got, w in zip((q.grad, k.grad, gq.grad, gk.grad, v.grad), want):
+        assert torch.equal(got, w)
