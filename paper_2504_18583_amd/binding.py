@@ -371,6 +371,8 @@ def rope_table(n_pos: int, rot_dim: int, theta: float, scaling: Optional[str] = 
     if lib.pard_rope_table_bytes(C.byref(spec), n_pos) == 0:
         _bad("rope_table: bad sizes or scaling parameters")
     device = torch.device(device)
+    if device.type != "cuda":
+        _bad(f"rope_table: a GPU is wanted, got {device}")
     if device.index is None:
         device = torch.device(device.type, torch.cuda.current_device())
     with _On(device, stream) as on:

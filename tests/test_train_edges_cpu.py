@@ -32,3 +32,11 @@ def test_tensors_that_require_gradients_are_refused(b):
         with torch.no_grad(), pytest.raises((b.PardError, AttributeError)) as e:
             f()
         assert "autograd" not in str(e.value)
+
+
+def test_rope_table_of_a_host_device_is_refused(b):
+    """The kernel would write to host memory."""
+    for device in ("cpu", torch.device("cpu"), "cpu:0", "meta"):
+        with pytest.raises(b.PardError, match="GPU") as e:
+            b.rope_table(8, 64, 1e4, device=device)
+        assert e.value.status == b.PARD_ERR_ARG
