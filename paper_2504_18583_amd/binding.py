@@ -477,6 +477,8 @@ def cod_plan(section, column, out_offsets: Sequence[int], out_len, stream=None) 
         if t.dtype != torch.int32 or t.device != dev or t.dim() != 1 or len(t) < rows or not t.is_contiguous():
             _bad(f"cod_plan: {name}: a contiguous int32 tensor of at least {rows} on {dev} is wanted")
     _vector(out_len, "out_len", n, torch.int32, dev)
+    if dev.type != "cuda":
+        _bad(f"cod_plan: device tensors are wanted, got tensors on {dev}")
     n_bytes = lib.pard_cod_plan_bytes(rows, n)
     if n_bytes == 0:
         raise PardError(PARD_ERR_UNSUPPORTED, "cod_plan: too many rows")

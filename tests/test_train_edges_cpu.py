@@ -40,3 +40,10 @@ def test_rope_table_of_a_host_device_is_refused(b):
         with pytest.raises(b.PardError, match="GPU") as e:
             b.rope_table(8, 64, 1e4, device=device)
         assert e.value.status == b.PARD_ERR_ARG
+
+
+def test_cod_plan_of_host_tensors_is_refused(b):
+    z = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(b.PardError, match="device tensors") as e:
+        b.cod_plan(z, z, [0, 4], z[:1])
+    assert e.value.status == b.PARD_ERR_ARG
