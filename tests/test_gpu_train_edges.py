@@ -134,3 +134,120 @@ def test_attention_and_rotation_in_autograd(B):
         want = (*B.qk_rope_grad(dq, dk, pos, table, q=q, k=k, q_gain=gq, k_gain=gk), dv)
     for got, w in zip((q.grad, k.grad, gq.grad, gk.grad, v.grad), want):
         assert torch.equal(got, w)
+
+
+def _attn_rows(q, k, v, d_out, section, column, rows, scale):
+    """Attention of one sample in float64 on the device, for the queries `rows`
+    alone: (value, bound) of out, lse and dq [len(rows), ..], and of dk and dv as
+    those rows add to them.  Bounds as train_common.attn_ref counts them."""
+    hq, hk = q.shape[1], k.shape[1]
+    u, F = T.unit(q.dtype), T.F
+    z = lambda *s: torch.zeros(*s, dtype=torch.float64, device="cuda")  # noqa: E731
+    n, hd = len(rows), q.shape[2]
+    res = {name: (z(n, hq, hd), z(n, hq, hd)) for name in ("out", "dq")} | {"lse": (z(hq, n), z(hq, n))}
+    res |= {name: (z(*k.shape), z(*k.shape)) for name in ("dk", "dv")}
+    chain = column - section
+    for a in range(0, n, 512):
+        sl = slice(a, min(a + 512, n))
+        r = rows[sl]
+        ka, ja = section[r][:, None], column[r][:, None]
+        seen = torch.where(section == 1, column <= ja - ka + 1, (section <= ka) & (chain == ja - ka))
+        terms = int(seen.sum(-1).max())
+        for h in range(hq):
+            g = h * hk // hq
+            Q, G, K, V = q[r, h].double(), d_out[r, h].double(), k[:, g].double(), v[:, g].double()
+            KT, VT = K.T.contiguous(), V.T.contiguous()
+            sc = (Q @ KT * scale).masked_fill_(~seen, -np.inf)
+            lse = torch.logsumexp(sc, -1)
+            P = torch.exp(sc - lse[:, None])
+            out, A = P @ V, P @ V.abs()
+            ds_max = ((Q.abs() @ KT.abs() * abs(scale)) * seen).amax(-1) * (hd + 8) * F
+            rel = 2 * ds_max[:, None] + (terms + 32) * F
+            e_out = u * (A + out.abs()) + A * rel
+            res["out"][0][sl, h], res["out"][1][sl, h] = out, e_out
+            res["lse"][0][h, sl], res["lse"][1][h, sl] = lse, ds_max + (terms + 16) * F + 4 * F * lse.abs()
+            delta = (G * out).sum(-1, keepdim=True)
+            e_delta = (G.abs() * e_out).sum(-1, keepdim=True) + hd * F * (G.abs() * out.abs()).sum(-1, keepdim=True)
+            dS = P * (G @ VT - delta)
+            e_dS = (u * dS.abs() + P * e_delta + 2 * rel * P * (G.abs() @ VT.abs() + delta.abs())) * seen
+            e_P = P * (u + 2 * rel) * seen
+            sums = (n * hq // hk + terms) * F
+            dq, mag = scale * dS @ K, abs(scale) * dS.abs() @ K.abs()
+            res["dq"][0][sl, h], res["dq"][1][sl, h] = dq, abs(scale) * e_dS @ K.abs() + sums * mag + u * dq.abs()
+            for name, m, e, x, f in (("dk", dS, e_dS, Q, scale), ("dv", P, e_P, G, 1.0)):
+                res[name][0][:, g] += f * (m.T.contiguous() @ x)
+                res[name][1][:, g] += abs(f) * ((e + sums * m.abs()).T.contiguous() @ x.abs())
+    for name in ("dk", "dv"):
+        res[name][1].add_(u * res[name][0].abs())
+    return res
+
+
+def _check_rows(B, section, column, heads, hd, rows, keys):
+    """One sample, its rows in `rows` and keys in `keys` (seen by no others than
+    `rows`), and a second short sample behind it."""
+    hq, hk = heads
+    s2, c2, _, _, n2 = T.pack([21], 4)
+    n = len(section)
+    sec, col = (torch.from_numpy(np.concatenate(x).astype(np.int32)).cuda() for x in ((section, s2), (column, c2)))
+    plan = B.cod_plan(sec, col, [0, n, n + n2], torch.tensor([n, n2], dtype=torch.int32, device="cuda"))
+    g = _gen(n)
+    q, d_out = (_randn(g, n + n2, hq, hd, dtype=torch.bfloat16) for _ in range(2))
+    k, v = (_randn(g, n + n2, hk, hd, dtype=torch.bfloat16) for _ in range(2))
+    say(f"[gpu] attention: {n} rows of one sample, {hq}/{hk} heads x {hd}")
+    out, lse = B.cod_attn(q, k, v, plan)
+    dq, dk, dv = B.cod_attn_grad(d_out, q, k, v, out, lse, plan)
+    got = {"out": out[rows], "lse": lse[:, rows], "dq": dq[rows], "dk": dk[keys], "dv": dv[keys]}
+    ref = _attn_rows(q[:n], k[:n], v[:n], d_out[:n], sec[:n].long(), col[:n].long(), rows, hd ** -0.5)
+    for name, (want, bound) in ref.items():
+        pick = keys if name in ("dk", "dv") else slice(None)
+        T.assert_within(got[name], want[pick].cpu(), bound[pick].cpu(), name)
+    want = T.attn_ref(q[n:], k[n:], v[n:], s2, c2, np.array([0, n2]), [n2], hd ** -0.5, d_out[n:])
+    for name, x in (("out", out[n:]), ("lse", lse[:, n:]), ("dq", dq[n:]), ("dk", dk[n:]), ("dv", dv[n:])):
+        T.assert_within(x, *want[name], f"{name} of the sample behind")
+
+
+@pytest.mark.parametrize("heads,hd", [((2, 1), 64), ((1, 1), 128)])
+def test_attention_of_the_longest_sample(B, heads, hd):
+    """8192 columns: every row and key."""
+    section, column, _, _, n = T.pack([8192], 8)
+    rows = torch.arange(n, device="cuda")
+    _check_rows(B, section, column, heads, hd, rows, rows)
+
+
+def test_attention_of_the_largest_sample(B):
+    """8192 columns of which 64 subtasks keep everything, 522 272 rows: rows of
+    the first, some middle and the last chains, and the keys that only they see."""
+    section = np.concatenate([np.full(8192 - k + 1, k) for k in range(1, 65)])
+    column = np.concatenate([np.arange(k - 1, 8192) for k in range(1, 65)])
+    chain = torch.from_numpy(column - section + 1).cuda()
+    picked = torch.isin(chain, torch.tensor([0, 1, 127, 4096, 8191 - 63, *range(8186, 8192)], device="cuda"))
+    rows = picked.nonzero()[:, 0]
+    late = (chain >= 8186) | (picked & (torch.from_numpy(section).cuda() > 1))
+    _check_rows(B, section, column, (2, 1), 64, rows, late.nonzero()[:, 0])
+
+
+def test_more_columns_than_a_sample_may_have(B):
+    n = 8193
+    section = torch.ones(n, dtype=torch.int32, device="cuda")
+    column = torch.arange(n, dtype=torch.int32, device="cuda")
+    for m in (n, 8192):
+        length = torch.tensor([m], dtype=torch.int32, device="cuda")
+        if m == 8192:
+            B.cod_plan(section, column, [0, n], length)
+            continue
+        with pytest.raises(B.PardError) as e:
+            B.cod_plan(section, column, [0, n], length)
+        assert e.value.status == B.PARD_ERR_ARG
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (128, "f16")])
+def test_attention_gradient_again(B, hd, dtype):
+    """A second gradient of the same tensors gives the same bits."""
+    section, column, offs, lens, rows = T.pack([130, 60, 700], 8)
+    plan = B.cod_plan(torch.from_numpy(section).cuda(), torch.from_numpy(column).cuda(), offs, torch.from_numpy(lens).cuda())
+    g = _gen(6)
+    q, k, v, d_out = (_randn(g, rows, h, hd, dtype=T.DTYPES[dtype]) for h in (4, 2, 2, 4))
+    out, lse = B.cod_attn(q, k, v, plan)
+    first = B.cod_attn_grad(d_out, q, k, v, out, lse, plan)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, B.cod_attn_grad(d_out, q, k, v, out, lse, plan)))
