@@ -431,6 +431,9 @@ pard_status pard_qk_rope(const pard_rope_args *args, const pard_heads *q, const 
  * written to q_dgain and k_dgain (float[head_dim], sums over rows and heads,
  * deterministic); without, q, k, q_dgain and k_dgain are not used and may be
  * null.  dx may be dy itself, but not x.  The workspace is needed with gains only.
+ * Every row counts in the gains' gradients, one that belongs to no sample as
+ * well: its dy must be 0 (as pard_cod_attn_grad leaves padding rows), its x
+ * finite and its position inside the table.
  * Errors: as pard_qk_rope; NOMEM (workspace too small). */
 size_t pard_qk_rope_workspace_bytes(const pard_rope_args *args);
 pard_status pard_qk_rope_grad(const pard_rope_args *args, const pard_heads *q_dy, const pard_heads *k_dy,
@@ -515,7 +518,8 @@ pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads 
  *              be logits itself, same data and stride, but not overlap it
  *              otherwise); rows that do not count get 0
  * pard_cod_build leaves a region's rows past out_len as they were: the caller
- * sets their labels below 0.
+ * sets their labels below 0 (and their ids and positions to valid ones, for what
+ * it computes of them before).
  * A label of vocab or more makes its row's loss and gradient NaN.  Sums are
  * float32, means over rows float64.  logits, d_logits: dtype (PARD_F32,
  * PARD_BF16, PARD_F16), [rows][vocab] with row strides in elements; loss:

@@ -426,7 +426,9 @@ def qk_rope_grad(q_dy, k_dy, positions, table, layout: str = "half", q=None, k=N
                  eps: float = 1e-6, q_dx=None, k_dx=None, stream=None):
     """Gradient of qk_rope (pard_qk_rope_grad).  With gains, q and k are the
     forward call's inputs.  Returns (q_dx, k_dx, q_dgain, k_dgain), the last two
-    None without gains; q_dx and k_dx may be q_dy and k_dy themselves."""
+    None without gains; q_dx and k_dx may be q_dy and k_dy themselves.  Every row
+    counts in the gains' gradients: those of no sample need a dy of 0, finite
+    heads and a position in the table."""
     import torch
     hdq = _heads(q_dy, "q_dy")
     hdk = None if k_dy is None else _heads(k_dy, "k_dy", q_dy, (*q_dy.shape[:1], *k_dy.shape[1:2], *q_dy.shape[2:]))

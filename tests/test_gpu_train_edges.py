@@ -251,3 +251,38 @@ def test_attention_gradient_again(B, hd, dtype):
     first = B.cod_attn_grad(d_out, q, k, v, out, lse, plan)
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(first, B.cod_attn_grad(d_out, q, k, v, out, lse, plan)))
+
+
+def test_a_padded_batch(B):
+    """Regions longer than their samples, whose last rows hold anything: with
+    ids, positions and labels cleared there, nothing of them reaches the loss or a
+    gradient, the gains' among them."""
+    k_max, hd, vocab, dt = 5, 64, 300, torch.bfloat16
+    rng = np.random.default_rng(3)
+    lengths = [2, 30, 7, 111]
+    token_offsets = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    tokens = torch.from_numpy(rng.integers(0, vocab - 1, size=int(token_offsets[-1])).astype(np.int32)).cuda()
+    offsets, data, lens = B.cod_build(tokens, token_offsets, k_max, 1.0, 0.2, vocab - 1, 9)
+    inside = torch.cat([torch.arange(b - a, device="cuda") < n for a, b, n in zip(offsets, offsets[1:], lens)])
+    assert not inside.all()
+    g = _gen(11)
+    emb, w = _randn(g, vocab, 8 * hd, dtype=dt), _randn(g, 4 * hd, vocab, dtype=dt, std=0.05)
+    gq, gk, table = 1 + _randn(g, hd, std=0.1), 1 + _randn(g, hd, std=0.1), B.rope_table(128, hd, 1e4)
+    want = None
+    for anything in (0, -1, 2 ** 31 - 1, -2 ** 31):
+        say(f"[gpu] a padded batch, {anything} past the samples")
+        rows = {name: t.masked_fill(~inside, anything) for name, t in data.items()}
+        ids, labels, pos = (rows[name].masked_fill(~inside, x) for name, x in (("ids", 0), ("labels", -1), ("pos", 0)))
+        plan = B.cod_plan(rows["section"], rows["column"], offsets, lens)
+        q, k, v = (t.unflatten(1, (-1, hd)) for t in emb[ids.long()].split((4 * hd, 2 * hd, 2 * hd), 1))
+        rq, rk = B.qk_rope(q, k, pos, table, q_gain=gq, k_gain=gk)
+        out, lse = B.cod_attn(rq, rk, v, plan)
+        loss, parts, by_row, d_logits = B.cod_loss(out.flatten(1) @ w, labels, rows["section"], k_max, grad_scale=64.0)
+        d_out = (d_logits @ w.T.contiguous()).unflatten(1, (4, hd))
+        dq, dk, dv = B.cod_attn_grad(d_out, rq, rk, v, out, lse, plan)
+        got = (loss, parts, by_row, dv, *B.qk_rope_grad(dq, dk, pos, table, q=q, k=k, q_gain=gq, k_gain=gk))
+        assert all(t.isfinite().all() for t in got)
+        assert all((t[~inside] == 0).all() for t in got[2:6])
+        assert got[6].abs().max() > 0 and got[7].abs().max() > 0
+        want = want or got
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
