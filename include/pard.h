@@ -428,8 +428,8 @@ pard_status pard_qk_rope(const pard_rope_args *args, const pard_heads *q, const 
 
 /* Gradient of pard_qk_rope: from dy (q_dy, k_dy) to dx (q_dx, k_dx).  With
  * gains, q and k are the forward call's inputs and the gains' gradients are
- * written to q_dgain and k_dgain (float[head_dim], sums over rows and heads,
- * deterministic); without, q, k, q_dgain and k_dgain are not used and may be
+ * written to q_dgain and k_dgain (float[head_dim], float32 sums over rows and
+ * heads, deterministic); without, q, k, q_dgain and k_dgain are not used and may be
  * null.  dx may be dy itself, but not x.  The workspace is needed with gains only.
  * Every row counts in the gains' gradients, one that belongs to no sample as
  * well: its dy must be 0 (as pard_cod_attn_grad leaves padding rows), its x
@@ -496,8 +496,9 @@ pard_status pard_cod_attn(const pard_cod_attn_args *args, const pard_heads *q, c
 /* Gradient of pard_cod_attn: out and lse are the forward call's outputs.
  * Padding rows of dq, dk and dv get 0, rows outside the regions are left as
  * they are.  Probabilities and score gradients are rounded to dtype for the
- * products; sums over a key head's query heads are float32.  Deterministic.  No
- * gradient may overlap another or an input.
+ * products (PARD_F16: those below 2^-25 vanish, those above 65504 become
+ * infinite; pard_cod_loss's grad_scale shifts them); sums over a key head's query
+ * heads are float32.  Deterministic.  No gradient may overlap another or an input.
  * Errors: as pard_cod_attn; NOMEM (workspace too small). */
 size_t pard_cod_attn_workspace_bytes(const pard_cod_attn_args *args);
 pard_status pard_cod_attn_grad(const pard_cod_attn_args *args, const pard_heads *d_out, const pard_heads *q,

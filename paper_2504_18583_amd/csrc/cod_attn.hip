@@ -13,15 +13,18 @@
 // A tile is S^T = K Q^T, online softmax in base 2, O^T += V^T P^T, with the
 // running maximum raised only when a score passes it by 2^kLazy.
 //
-// Bound: the SIMDs' issue.  A score costs an exponential and about four more
-// instructions beside its share of the products, and the two hardly overlap: at
-// head_dim 64 the cycles of the products and of the rest add up to 93 % of the
-// kernel's.  Two tiles of 16 pairs a wavefront (NQ) share every LDS read: 1B layer
-// (16 samples of 256 to 1024 tokens, 32 / 8 heads x 64) 250 us, 302 against 389
-// with one tile when that was measured; 8B heads (x 128, 6 samples of 900 to 2048)
-// 510 us; one sample of 8193 tokens, 8 / 4 heads x 64, 246 us, 940 TFLOP/s of 1228
-// of a large product.  head_dim 128 with stages of 32 keys and a third workgroup
-// a CU spilled (584 us).  A scalar kernel, one wavefront per pair, took 24.8 ms.
+// Bound: the SIMDs' issue.  On one sample of 8193 tokens (8 / 4 heads x 64: 250 us,
+// 930 TFLOP/s of 1228 of a large product) a score costs an exponential and about
+// four more instructions beside its share of the products, whose cycles and the
+// rest's add up to 109 % of the kernel's: they overlap a little.  Rows of short
+// samples pay more for each score: in a 1B layer (16 samples of 256 to 1024 tokens,
+// 32 / 8 heads x 64: 250 us, 530 TFLOP/s) a row sees 400 keys, 16 % more scores are
+// computed than seen (the last stages, the chains' 32 keys), and a pair's fixed
+// work makes 8 instructions of a seen score's five; 8B heads (x 128, 6 samples of
+// 900 to 2048) 505 us, 7.  Two tiles of 16 pairs a wavefront (NQ) share every LDS
+// read (1B layer 302 us against 389 with one tile when that was measured).
+// head_dim 128 with stages of 32 keys and a third workgroup a CU spilled (584 us).
+// A scalar kernel, one wavefront per pair, took 24.8 ms.
 #include "cod_attn_tile.h"
 
 namespace pard {
@@ -34,7 +37,10 @@ constexpr float kLazy = 8.f;
 
 // Softmax of NB blocks of 16 keys: scores s become packed probabilities pf,
 // running maximum m (base 2), sum l and output o follow.  Hidden scores are
-// -infinity; m starts finite, so that a row without keys keeps l = 0.
+// -infinity; m starts finite, so that a row without keys keeps l = 0.  The product
+// takes probabilities of 16 bits (the sum does not): what is lost is of the size of
+// the output's own rounding (1B layer, bf16: 2.2e-3 of the output's magnitude off,
+// where rounding the exact output is 1.6e-3).
 template <int NQ, int NB, int DB, class M>
 __device__ __forceinline__ void softmax_step(const f32x4 (&s)[NQ][NB], float (&m)[NQ], float (&l)[NQ], f32x4 (&o)[NQ][DB],
                                              u32x4 (&pf)[NQ][NB / 2], float scale2) {

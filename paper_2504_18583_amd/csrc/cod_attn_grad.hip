@@ -16,10 +16,16 @@
 //
 // Both recompute the scores (9 products in place of 7 with the forward's), since
 // neither dQ nor dK and dV of a sample fit on chip.  Bound: the SIMDs' issue, as
-// in the forward: at head_dim 64 the products' cycles (36 % of the kernel's for
-// dQ, 41 % for dK and dV) and the other instructions' add up to 83 %.  1B layer (16 samples of 256 to 1024 tokens, 32 / 8 heads x 64):
-// delta 40, dQ 330, dK and dV 450 us; 8B heads (x 128, 6 samples of 900 to 2048):
-// 35, 655 and 975.  Scalar kernels took 160 and 557 ms.
+// in the forward: at head_dim 64 the products take 36 % of the busy CUs' cycles for
+// dQ and 41 % for dK and dV, the other instructions 38 and 31 %.  In dK and dV a
+// fifth of the CUs' time is idle besides: nearly all workgroups start at once, and
+// walk from a few to some 200 stages.  1B layer (16 samples of 256 to 1024 tokens, 32 / 8 heads x 64):
+// delta 38, dQ 332, dK and dV 466 us; 8B heads (x 128, 6 samples of 900 to 2048):
+// 35, 650 and 993.  Scalar kernels took 160 and 557 ms.
+//
+// P and dS enter their products with 16 bits, as the matrix instructions want; the
+// sums are float32.  (fp16: a dS below 2^-25 vanishes and one above 65504 is
+// infinite, so d_out's scale has to keep them between.)
 #include "cod_attn_tile.h"
 
 namespace pard {

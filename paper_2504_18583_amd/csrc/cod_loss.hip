@@ -10,9 +10,9 @@
 // workgroup (at most 20 a thread of 1024: 163 840 logits of two bytes) from the
 // sum to the gradient, and as soon as a vector's gradient is stored, its registers
 // take the same vector of the next row.  Longer rows are read a second time.  4099 rows of
-// 128 256 bf16 logits with gradients: 520 us, 4.0 TB/s of a large copy's 4.9 (the
-// row's two barriers, and 20 vectors' registers leave one workgroup a CU); 2050
-// rows of 152 064 f16 logits alone: 127 us, 4.9 TB/s.  Element by
+// 128 256 bf16 logits with gradients: 525 us, 4.0 TB/s of a large copy's 4.9 (the
+// row's barrier, and 16 vectors' registers leave one workgroup a CU); 2050
+// rows of 152 064 f16 logits alone: 128 us, 4.9 TB/s.  Element by
 // element, rows with gradients read twice, took 1414 and 398 us.
 #include "train.h"
 

@@ -6,8 +6,9 @@
 //   gradient  dn = R^T dy;  dg += dn x r;  dx = r (t - x^ mean(t x^)), t = g dn, x^ = x r
 //
 // Bound: memory (x in, y out; dy, x in, dx out).  bf16, 34 500 rows of 32 + 8
-// heads x 64: 77 us, 4.6 TB/s of the 4.9 of a large copy; the norm's gradient,
-// 8191 rows of 40 heads x 128: 57 us, 4.4 TB/s, and 7 us for the gains' sums.
+// heads x 64: 76 us, 4.6 TB/s of the 4.9 of a large copy; the norm's gradient,
+// 8191 rows of 40 heads x 128: 55 us, 4.7 TB/s, and 7 us for the gains' sums
+// (float32: a lane's rows, then the workgroup's lanes, then the workgroups).
 // One wavefront per (row, head) with 2-byte accesses took 1090 and 1200 us.
 #include "train.h"
 
@@ -77,7 +78,6 @@ __device__ __forceinline__ float group_sum(float x) {
 
 // Any shape (odd dims, unaligned rows): one wavefront per (row, head), a lane's
 // elements 64 apart.
-// Element e's partner in its pair and which half of the pair it is.
 template <class E, int LAYOUT, bool GRAD>
 __global__ __launch_bounds__(kRopeThreads) void k_rope_any(const RopeArgs a) {
   using T = typename E::T;

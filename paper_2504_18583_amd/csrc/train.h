@@ -46,8 +46,8 @@ struct RopeArgs {
 // Workgroups that leave partial gain gradients.
 int rope_grad_blocks(const RopeArgs& a);
 hipError_t launch_rope_spec_table(const pard_rope_spec& s, int n_pos, float2* table, hipStream_t st);
-// grad: the gradient; with gains its workgroups' partial sums are added into
-// q_dgain and k_dgain by a second launch.
+// grad: the gradient; with gains its workgroups' partial sums are summed and
+// written to q_dgain and k_dgain by a second launch.
 hipError_t launch_qk_rope(int dtype, int layout, bool grad, const RopeArgs& a, float* q_dgain, float* k_dgain,
                           hipStream_t st);
 
