@@ -19,9 +19,9 @@
 // in the forward: at head_dim 64 the products take 36 % of the busy CUs' cycles for
 // dQ and 41 % for dK and dV, the other instructions 38 and 31 %.  In dK and dV a
 // fifth of the CUs' time is idle besides: nearly all workgroups start at once, and
-// walk from a few to some 200 stages.  1B layer (16 samples of 256 to 1024 tokens, 32 / 8 heads x 64):
-// delta 38, dQ 332, dK and dV 466 us; 8B heads (x 128, 6 samples of 900 to 2048):
-// 35, 650 and 993.  Scalar kernels took 160 and 557 ms.
+// walk from a few to some 200 stages.  1B layer (16 samples of 256 to 1024 tokens,
+// 32 / 8 heads x 64): delta 38, dQ 332, dK and dV 466 us; 8B heads (x 128, 6 samples
+// of 900 to 2048): 35, 650 and 993.  Scalar kernels took 160 and 557 ms.
 //
 // P and dS enter their products with 16 bits, as the matrix instructions want; the
 // sums are float32.  (fp16: a dS below 2^-25 vanishes and one above 65504 is

@@ -286,3 +286,43 @@ def test_a_padded_batch(B):
         assert got[6].abs().max() > 0 and got[7].abs().max() > 0
         want = want or got
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_optional_outputs_and_shared_inputs(B):
+    """The C calls without lse and row_loss; inputs whose key heads, rows of
+    queries or gradients' rows are one and the same (stride 0)."""
+    section, column, offs, lens, rows = T.pack([50, 3], 4, slack=2)
+    plan = B.cod_plan(torch.from_numpy(section).cuda(), torch.from_numpy(column).cuda(), offs, torch.from_numpy(lens).cuda())
+    g = _gen(8)
+    q, v = _randn(g, rows, 4, 64, dtype=torch.bfloat16), _randn(g, rows, 2, 64, dtype=torch.bfloat16)
+    k, d_out = _randn(g, rows, 1, 64, dtype=torch.bfloat16).expand(rows, 2, 64), _randn(g, 1, 4, 64, dtype=torch.bfloat16).expand(rows, 4, 64)
+    assert k.stride(1) == d_out.stride(0) == 0
+    say("[gpu] attention of shared inputs")
+    out, lse = B.cod_attn(q, k, v, plan)
+    dq, dk, dv = B.cod_attn_grad(d_out, q, k, v, out, lse, plan)
+    want = T.attn_ref(q, k, v, section, column, offs, lens, 64 ** -0.5, d_out)
+    inside = torch.cat([torch.arange(b - a) < n for a, b, n in zip(offs, offs[1:], lens)])
+    for name, x in (("out", out), ("dq", dq), ("dk", dk), ("dv", dv)):
+        T.assert_within(x[inside.cuda()], want[name][0][inside], want[name][1][inside], name)
+    again = torch.zeros_like(out)
+    args = B.pard_cod_attn_args(B.C.pointer(plan.plan), 4, 2, 64, B.PARD_BF16, 64 ** -0.5)
+    heads = [B.pard_heads(t.data_ptr(), t.stride(0), t.stride(1)) for t in (q, k, v, again)]
+    stream = torch.cuda.current_stream().cuda_stream
+    assert B.lib.pard_cod_attn(args, *heads, None, stream) == B.PARD_OK
+    assert torch.equal(again, out)
+
+    table, pos = B.rope_table(64, 64, 1e4), torch.from_numpy(np.clip(column, 0, 63)).cuda()
+    one = _randn(g, 1, 2, 64).expand(rows, 2, 64)
+    y, _ = B.qk_rope(one, None, pos, table)
+    T.assert_within(y, *T.rope_ref(one, pos, table, "half", None, 1e-6), "rotation of one row")
+
+    logits = _randn(g, 20, 1000)
+    labels = torch.arange(20, dtype=torch.int32, device="cuda")
+    loss, parts, _, d = B.cod_loss(logits, labels, None, 1)
+    d2, loss2 = torch.empty_like(logits), torch.empty(2, device="cuda")
+    a = B.pard_cod_loss_args(20, 1000, B.PARD_F32, 1, 1.0, logits.data_ptr(), 1000, labels.data_ptr(), None, None, d2.data_ptr(), 1000,
+                             loss2.data_ptr(), None)
+    n = B.lib.pard_cod_loss_workspace_bytes(a)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    assert B.lib.pard_cod_loss(a, ws.data_ptr(), n, stream) == B.PARD_OK
+    assert torch.equal(d, d2) and torch.equal(loss2, torch.stack([loss, parts[0]]))
