@@ -545,6 +545,155 @@ size_t pard_cod_loss_workspace_bytes(const pard_cod_loss_args *args);
 pard_status pard_cod_loss(const pard_cod_loss_args *args, void *workspace, size_t workspace_bytes,
                           void *hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * Serving over a paged cache: the verification stage of Sec. 2.2 for a model of
+ * the caller's.  A step rotates its new rows (pard_qk_rope), writes their keys
+ * and values into the cache (pard_kv_write), attends to it (pard_kv_attn) in
+ * every layer, and adjusts the last rows' logits before tokens are picked
+ * (pard_logits_adjust).  Rollback is a smaller kv_len at the next step.
+ *
+ * Buffers, streams, workspaces, capture and status codes as for mask-token
+ * training above.  What lies in device memory (page tables, lengths, offsets,
+ * ids) is read by the kernels: a captured graph may be replayed after it has
+ * changed.  Entries outside their ranges never lead outside a buffer; each call
+ * says what they do.
+ * ------------------------------------------------------------------------ */
+
+/* A paged cache of one layer.  A page holds page_size (a power of two, 16 to
+ * 4096) consecutive positions of a sequence:
+ *   k, v: [n_pages][n_kv_heads][page_size][head_dim] of dtype, 16-byte aligned,
+ * head_dim 64 or 128.  dtype: PARD_BF16, PARD_F16 (elements as they are), or a
+ * type whose elements share the scale of their block of 32 elements of a head:
+ *   PARD_E4M3  a byte an element: sign, 4 bits of exponent (bias 7), 3 of
+ *              fraction; at most 448; 0x7f and 0xff are NaN
+ *   PARD_E2M1  4 bits an element (the lower half of a byte first): 0, 0.5, 1,
+ *              1.5, 2, 3, 4, 6 and their negatives
+ * k_scale, v_scale (these types only; 4-byte aligned): [n_pages][n_kv_heads]
+ * [page_size][head_dim / 32] bytes: byte b is the scale 2^(b - 127); 255 makes
+ * the block NaN.  An element's value is exact in bfloat16 and float32 (where
+ * scales are at least 2^-117), and in float16 within its range. */
+enum { PARD_E4M3 = 3, PARD_E2M1 = 4 };
+typedef struct {
+  int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;
+  void *k, *v;
+  uint8_t *k_scale, *v_scale;
+} pard_kv_cache;
+
+/* The sequences of a step, in device memory.  Rows row_start[s] ..
+ * row_start[s + 1] - 1 are sequence s's new rows (none: it takes no part), the
+ * last of its kv_len[s] positions: row r is at position kv_len[s] -
+ * row_start[s + 1] + r.  Position p lies in page page_table[s][p / page_size].
+ * row_start ascends from 0 or more to at most rows; rows before row_start[0] and from
+ * row_start[n_seqs] on belong to no sequence and are left as they are.
+ * max_seq_rows: the most rows of a sequence where the caller knows it (0: not
+ * known); it helps to choose kernels, and no result needs it to be right. */
+typedef struct {
+  int64_t rows;
+  int32_t n_seqs, max_pages, max_seq_rows;
+  const int32_t *page_table;       /* device, [n_seqs][max_pages] */
+  const int32_t *row_start;        /* device, [n_seqs + 1] */
+  const int32_t *kv_len;           /* device, [n_seqs] */
+} pard_kv_batch;
+
+/* Writes the rows' keys and values ([rows][n_kv_heads][head_dim] of dtype:
+ * PARD_F32, PARD_BF16 or PARD_F16) into their places in the cache, rounded to
+ * the nearest (ties to even) of its type.  A block of 32 elements takes the
+ * smallest scale 2^e, e >= -126, that brings it within the type's range (448 or
+ * 6: nothing saturates, and what is rounded does not depend on the elements'
+ * order); a block that holds a NaN or an infinity becomes NaN.  A row whose position
+ * is negative or has no page (past max_pages, or an entry outside [0, n_pages))
+ * is not written.  Two rows in one place: either.
+ * pard_kv_read reads the rows' places back (a row without a place: NaN): with
+ * row_start covering whole sequences, all of them.  Values are rounded to dtype.
+ * Vectorised where the rows' data and strides are multiples of 16 bytes.
+ * Errors: ARG (null pointer, sizes below 1, rows or max_seq_rows negative, page_size not a
+ * power of two in [16, 4096], misaligned cache or scales, strides negative, overlapping
+ * heads of an output), UNSUPPORTED (a dtype, head_dim not 64 or 128, 2^30 rows
+ * or more, above 65535 heads or 2^20 sequences, max_pages * page_size above
+ * 2^30), DEVICE. */
+pard_status pard_kv_write(const pard_kv_cache *cache, const pard_kv_batch *batch, int32_t dtype, const pard_heads *k,
+                          const pard_heads *v, void *hip_stream);
+pard_status pard_kv_read(const pard_kv_cache *cache, const pard_kv_batch *batch, int32_t dtype, const pard_heads *k,
+                         const pard_heads *v, void *hip_stream);
+
+/* Attention of the new rows over the cache, which holds them already.  The row
+ * at position p sees the positions j <= p, and with a window w > 0 those of
+ * them with j > p - w or j < sinks (the first tokens stay visible):
+ *   out = softmax(scale * q K^T) V,  lse = log sum exp(scale * q K^T)
+ * q, out: [rows][n_heads][head_dim] of dtype (PARD_BF16 or PARD_F16; the
+ * cache's type is the same, PARD_E4M3 or PARD_E2M1), query head h reads key
+ * head h / (n_heads / n_kv_heads); lse: [n_heads][rows], float, may be null.
+ * A row that sees nothing (a negative position) gets out = 0 and lse = -inf.  A
+ * row that would see a position without a page gets NaN.  Pages that no row of
+ * the sequence sees into are not used, their entries may hold anything, and
+ * positions that no row sees may hold anything.  (A NaN or an infinity that one row sees may
+ * reach any row of its sequence.)  Scores, softmax and sums are float32 (scores
+ * within +-1e30); cached values and probabilities are rounded to dtype for the
+ * products.  Results are deterministic; how sums are split depends on the
+ * batch.  No output may overlap an input.
+ * Errors: as pard_kv_write for the cache and the batch; ARG (null pointer,
+ * n_heads not a multiple of n_kv_heads, scale not finite, window or sinks
+ * negative, data not 16-byte aligned, strides negative, not multiples of 8
+ * elements or above 2^31 - 1, overlapping heads of an output, an output that
+ * starts where the queries do), UNSUPPORTED (dtypes, n_heads above 1024
+ * n_kv_heads, rows * n_heads / n_kv_heads of 2^30 or more), NOMEM (workspace
+ * too small), DEVICE. */
+typedef struct {
+  const pard_kv_cache *cache;
+  const pard_kv_batch *batch;
+  int32_t n_heads, dtype, window, sinks;
+  float scale;
+} pard_kv_attn_args;
+size_t pard_kv_attn_workspace_bytes(const pard_kv_attn_args *args);
+pard_status pard_kv_attn(const pard_kv_attn_args *args, const pard_heads *q, const pard_heads *out, float *lse,
+                         void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Logits before tokens are picked (Sec. 2.1 eq. 2 then takes best): row r of
+ * sequence s = row_seq[r] (row_seq null: s = r) has the history
+ * tokens[s][0 .. row_len[r]), of which the first prompt_len[s] are its prompt,
+ * so that a verify pass's rows share a history and count the candidates before
+ * them.  For every id, in float32 and in this order:
+ *   y = x; in the history: y = x > 0 ? x / repetition[s] : x * repetition[s]
+ *   y -= frequency[s] * c, c: how often it is in the history after the prompt
+ *   y -= presence[s] if c > 0
+ *   y += bias_values[i] for i in bias_start[s] .. bias_start[s + 1] - 1 with
+ *        bias_ids[i] = id (the last one, if there are several)
+ *   y = -inf where bit id % 32 of word id / 32 of row mask_row[r] of the mask
+ *       is 0 (mask_row null: row r; negative: no mask; n_masks or more: all)
+ * out = y rounded to dtype; best[r] = the lowest id of the largest y in out (NaN
+ * is passed over; -1 if none is above -inf).  Every step may be left out (null): tokens (with
+ * row_len and prompt_len), repetition, presence, frequency (these need tokens), bias_start, mask,
+ * best.  prompt_len null: 0.  Ids outside [0, vocab) count for nothing; lengths
+ * are cut to [0, tokens_stride], bias_start to [0, n_bias]; a row whose sequence
+ * is outside [0, n_seqs) has no history and no biases.  out may be logits itself
+ * (same stride), but may not overlap it otherwise.  Deterministic.
+ * Errors: ARG (null pointer, rows < 0, vocab < 1, n_seqs < 1, row_seq null with fewer sequences
+ * than rows, strides below vocab / the mask's words, counts negative, out at
+ * logits with another stride, misaligned elements), UNSUPPORTED (dtype, 2^30
+ * rows or a vocab above 2^28), NOMEM (workspace too small; only best needs one), DEVICE. */
+typedef struct {
+  int64_t rows;
+  int32_t vocab, dtype, n_seqs;
+  const void *logits;
+  int64_t logits_stride;
+  void *out;
+  int64_t out_stride;
+  const int32_t *tokens;           /* device, [n_seqs][tokens_stride] */
+  int64_t tokens_stride;
+  const int32_t *row_seq, *row_len;   /* device, [rows] */
+  const int32_t *prompt_len;       /* device, [n_seqs] */
+  const float *repetition, *presence, *frequency;   /* device, [n_seqs] */
+  const int32_t *bias_start, *bias_ids;             /* device, [n_seqs + 1], [n_bias] */
+  const float *bias_values;        /* device, [n_bias] */
+  int32_t n_bias, n_masks;
+  const uint32_t *mask;            /* device, [n_masks] rows */
+  int64_t mask_stride;             /* words */
+  const int32_t *mask_row;         /* device, [rows] */
+  int32_t *best;                   /* device, [rows] */
+} pard_logits_args;
+size_t pard_logits_workspace_bytes(const pard_logits_args *args);
+pard_status pard_logits_adjust(const pard_logits_args *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Message of the last error on this context (never NULL; "" if none). */
 const char *pard_last_error(const pard_ctx *ctx);
 

@@ -24,7 +24,7 @@ lib = C.CDLL(LIB_PATH)
 
 PARD_OK, PARD_ERR_ARG, PARD_ERR_STATE, PARD_ERR_CAPACITY = 0, -1, -2, -3
 PARD_ERR_NOMEM, PARD_ERR_DEVICE, PARD_ERR_UNSUPPORTED, PARD_ERR_RANGE = -4, -5, -6, -7
-PARD_F32, PARD_BF16, PARD_F16 = 0, 1, 2
+PARD_F32, PARD_BF16, PARD_F16, PARD_E4M3, PARD_E2M1 = range(5)
 PARD_TARGET, PARD_DRAFT = 0, 1
 PARD_MODE_PARALLEL, PARD_MODE_VANILLA = 0, 1
 PARD_ROPE_PLAIN, PARD_ROPE_LINEAR, PARD_ROPE_LLAMA3, PARD_ROPE_YARN = range(4)
@@ -81,6 +81,31 @@ class pard_cod_loss_args(C.Structure):
                 ("d_logits", C.c_void_p), ("d_stride", C.c_int64), ("loss", C.c_void_p), ("row_loss", C.c_void_p)]
 
 
+class pard_kv_cache(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class pard_kv_batch(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("max_seq_rows", C.c_int32),
+                ("page_table", C.c_void_p), ("row_start", C.c_void_p), ("kv_len", C.c_void_p)]
+
+
+class pard_kv_attn_args(C.Structure):
+    _fields_ = [("cache", C.POINTER(pard_kv_cache)), ("batch", C.POINTER(pard_kv_batch)), ("n_heads", C.c_int32),
+                ("dtype", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("scale", C.c_float)]
+
+
+class pard_logits_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int32), ("dtype", C.c_int32), ("n_seqs", C.c_int32),
+                ("logits", C.c_void_p), ("logits_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                ("tokens", C.c_void_p), ("tokens_stride", C.c_int64), ("row_seq", C.c_void_p), ("row_len", C.c_void_p),
+                ("prompt_len", C.c_void_p), ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+                ("bias_start", C.c_void_p), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p), ("n_bias", C.c_int32),
+                ("n_masks", C.c_int32), ("mask", C.c_void_p), ("mask_stride", C.c_int64), ("mask_row", C.c_void_p),
+                ("best", C.c_void_p)]
+
+
 _I32P = C.POINTER(C.c_int32)
 _HEADSP = C.POINTER(pard_heads)
 _SPECP = C.POINTER(pard_model_spec)
@@ -124,6 +149,13 @@ _sig = {
     "pard_cod_attn_workspace_bytes": (C.c_size_t, [C.POINTER(pard_cod_attn_args)]),
     "pard_cod_attn_grad": (C.c_int, [C.POINTER(pard_cod_attn_args), *[_HEADSP] * 5, C.c_void_p, *[_HEADSP] * 3,
                                      C.c_void_p, C.c_size_t, C.c_void_p]),
+    "pard_kv_write": (C.c_int, [C.POINTER(pard_kv_cache), C.POINTER(pard_kv_batch), C.c_int32, _HEADSP, _HEADSP, C.c_void_p]),
+    "pard_kv_read": (C.c_int, [C.POINTER(pard_kv_cache), C.POINTER(pard_kv_batch), C.c_int32, _HEADSP, _HEADSP, C.c_void_p]),
+    "pard_kv_attn_workspace_bytes": (C.c_size_t, [C.POINTER(pard_kv_attn_args)]),
+    "pard_kv_attn": (C.c_int, [C.POINTER(pard_kv_attn_args), _HEADSP, _HEADSP, C.c_void_p, C.c_void_p, C.c_size_t,
+                               C.c_void_p]),
+    "pard_logits_workspace_bytes": (C.c_size_t, [C.POINTER(pard_logits_args)]),
+    "pard_logits_adjust": (C.c_int, [C.POINTER(pard_logits_args), C.c_void_p, C.c_size_t, C.c_void_p]),
     "pard_cod_loss_workspace_bytes": (C.c_size_t, [C.POINTER(pard_cod_loss_args)]),
     "pard_cod_loss": (C.c_int, [C.POINTER(pard_cod_loss_args), C.c_void_p, C.c_size_t, C.c_void_p]),
     "pard_read_logits": (C.c_int, [_CTX, C.c_int32, C.c_int32, C.POINTER(C.c_float), C.c_int32,
@@ -586,6 +618,199 @@ def cod_loss(logits, labels, section, n_sections: int, weights: Optional[Sequenc
         ws = _workspace(n_ws, dev)
         _done(lib.pard_cod_loss(args, ws.data_ptr(), n_ws, on.handle), "pard_cod_loss")
     return loss[0], loss[1:], row_loss, d_logits
+
+
+# ---- serving: a paged cache, attention over it, logits before tokens are picked ----
+
+def _no_gradient(what: str, *tensors) -> None:
+    """Turns away tensors that require gradients where torch would record them."""
+    import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        _bad(f"{what} has no gradient: call it under torch.no_grad()")
+
+
+class KVCache:
+    """A paged cache of one layer (pard_kv_cache) in the caller's tensors: k, v
+    [pages, kv heads, page size, head_dim] in bfloat16 or float16; or in uint8,
+    a byte (e4m3) or half a byte (e2m1) an element, with scales [pages, kv heads,
+    page size, head_dim / 32] in uint8."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        for name, t in (("k", k), ("v", v), ("k_scale", k_scale), ("v_scale", v_scale)):
+            if t is None and name.endswith("scale"):
+                continue
+            if t.dim() != 4 or not t.is_cuda or not t.is_contiguous():
+                _bad(f"KVCache: {name}: a contiguous device tensor of 4 dimensions is wanted")
+            if t.device != k.device or t.shape[:3] != k.shape[:3]:
+                _bad(f"KVCache: {name}: {tuple(t.shape)} on {t.device}, k is {tuple(k.shape)} on {k.device}")
+        if v.dtype != k.dtype or v.shape != k.shape or (k_scale is None) != (v_scale is None):
+            _bad("KVCache: keys and values of one form are wanted")
+        hd = k.shape[3]
+        if k_scale is None:
+            if k.dtype not in (torch.bfloat16, torch.float16):
+                raise PardError(PARD_ERR_UNSUPPORTED, f"KVCache: dtype {k.dtype} without scales")
+            self.dtype = _dtype(k, "KVCache")
+        else:
+            hd = 32 * k_scale.shape[3]
+            if (k.dtype != torch.uint8 or k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8
+                    or v_scale.shape != k_scale.shape or k.shape[3] not in (hd, hd // 2)):
+                _bad("KVCache: with scales, uint8 tensors of head_dim (or half) bytes and head_dim / 32 scales a head are wanted")
+            self.dtype = PARD_E4M3 if k.shape[3] == hd else PARD_E2M1
+        self.k, self.v, self.k_scale, self.v_scale, self.device, self.head_dim = k, v, k_scale, v_scale, k.device, hd
+        self.n_kv_heads = k.shape[1]
+        self.c = pard_kv_cache(k.shape[0], k.shape[2], k.shape[1], hd, self.dtype, k.data_ptr(), v.data_ptr(),
+                               None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
+
+
+def kv_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype="e4m3", device="cuda") -> KVCache:
+    """A new cache, not initialised: torch.bfloat16, torch.float16, "e4m3" or "e2m1"."""
+    import torch
+    shape = (n_pages, n_kv_heads, page_size)
+    if dtype not in ("e4m3", "e2m1"):
+        return KVCache(*(torch.empty(*shape, head_dim, dtype=dtype, device=device) for _ in "kv"))
+    if head_dim % 32:
+        raise PardError(PARD_ERR_UNSUPPORTED, "kv_cache: head_dim must be 64 or 128")
+    new = lambda n: torch.empty(*shape, n, dtype=torch.uint8, device=device)  # noqa: E731
+    n = head_dim if dtype == "e4m3" else head_dim // 2
+    return KVCache(new(n), new(n), new(head_dim // 32), new(head_dim // 32))
+
+
+class KVBatch:
+    """The sequences of a step (pard_kv_batch), in device tensors of int32 that may
+    change between calls: page_table [sequences, pages], row_start [sequences +
+    1], kv_len [sequences].  max_seq_rows: the most rows of a sequence, where known."""
+
+    def __init__(self, page_table, row_start, kv_len, max_seq_rows: int = 0):
+        import torch
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_cuda or not page_table.is_contiguous():
+            _bad("KVBatch: page_table: a contiguous int32 [sequences, pages] device tensor is wanted")
+        n, self.device = page_table.shape[0], page_table.device
+        _vector(row_start, "row_start", n + 1, torch.int32, self.device)
+        _vector(kv_len, "kv_len", n, torch.int32, self.device)
+        self.page_table, self.row_start, self.kv_len, self.max_seq_rows = page_table, row_start, kv_len, int(max_seq_rows)
+
+    def c(self, rows: int) -> pard_kv_batch:
+        return pard_kv_batch(rows, *self.page_table.shape, self.max_seq_rows, self.page_table.data_ptr(),
+                             self.row_start.data_ptr(), self.kv_len.data_ptr())
+
+
+def _same_device(what: str, device, cache: KVCache, batch: KVBatch) -> None:
+    if cache.device != device or batch.device != device:
+        _bad(f"{what}: the cache is on {cache.device}, the batch on {batch.device}, the rows on {device}")
+
+
+def kv_write(k, v, cache: KVCache, batch: KVBatch, stream=None) -> None:
+    """Keys and values of the batch's rows [rows, kv heads, head_dim] (float32,
+    bfloat16 or float16) into their places in the cache (pard_kv_write)."""
+    _no_gradient("kv_write", k, v)
+    hk = _heads(k, "k")
+    hv = _heads(v, "v", k, (k.shape[0], cache.n_kv_heads, cache.head_dim))
+    if k.shape != v.shape:
+        _bad(f"kv_write: k: shape {tuple(k.shape)}, expected {tuple(v.shape)}")
+    _same_device("kv_write", k.device, cache, batch)
+    with _On(k.device, stream, k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.page_table, batch.row_start, batch.kv_len) as on:
+        _done(lib.pard_kv_write(cache.c, batch.c(k.shape[0]), _dtype(k, "kv_write"), hk, hv, on.handle), "pard_kv_write")
+
+
+def kv_read(cache: KVCache, batch: KVBatch, rows: int, dtype=None, k_out=None, v_out=None, stream=None):
+    """What the cache holds in the places of the batch's rows (pard_kv_read): (k,
+    v) [rows, kv heads, head_dim], new tensors of dtype (bfloat16) unless given.
+    Rows of no sequence are left as they are (given) or hold nothing (new)."""
+    import torch
+    shape = (rows, cache.n_kv_heads, cache.head_dim)
+    _same_device("kv_read", cache.device, cache, batch)
+    if k_out is not None and v_out is not None and k_out.dtype != v_out.dtype:
+        _bad("kv_read: outputs of one type are wanted")
+    for t in (k_out, v_out):
+        dtype = t.dtype if t is not None and dtype is None else dtype
+    with _On(cache.device, stream, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.page_table, batch.row_start, batch.kv_len, k_out,
+             v_out) as on:
+        new = lambda: torch.empty(shape, dtype=dtype or torch.bfloat16, device=cache.device)  # noqa: E731
+        like = new()[:0]
+        k_out, v_out = (new() if t is None else t for t in (k_out, v_out))
+        hk, hv = _heads(k_out, "k_out", like, shape), _heads(v_out, "v_out", like, shape)
+        _done(lib.pard_kv_read(cache.c, batch.c(rows), _dtype(like, "kv_read"), hk, hv, on.handle), "pard_kv_read")
+    return k_out, v_out
+
+
+def kv_attn(q, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, window: int = 0, sinks: int = 0, out=None, stream=None):
+    """Attention of the batch's rows q [rows, heads, head_dim] over the cache
+    (pard_kv_attn), causal, or within a window > 0 and to the first `sinks`
+    positions.  scale: head_dim ** -0.5 unless given.  Returns (out, lse), lse
+    [heads, rows] in float32.  Rows of no sequence are left as they are (out
+    given) or hold nothing (new)."""
+    import torch
+    _no_gradient("kv_attn", q)
+    hq = _heads(q, "q")
+    rows, n_q, hd = q.shape
+    if hd != cache.head_dim:
+        _bad(f"kv_attn: head_dim {hd}, the cache has {cache.head_dim}")
+    _same_device("kv_attn", q.device, cache, batch)
+    scale = hd ** -0.5 if scale is None else float(scale)
+    args = pard_kv_attn_args(C.pointer(cache.c), C.pointer(batch.c(rows)), n_q, _dtype(q, "kv_attn"), window, sinks, scale)
+    with _On(q.device, stream, q, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.page_table, batch.row_start, batch.kv_len, out) as on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ho = _heads(out, "out", q, q.shape)
+        lse = torch.empty(n_q, rows, dtype=torch.float32, device=q.device)
+        n_ws = lib.pard_kv_attn_workspace_bytes(args)
+        ws = _workspace(n_ws, q.device)
+        _done(lib.pard_kv_attn(args, hq, ho, lse.data_ptr(), ws.data_ptr(), n_ws, on.handle), "pard_kv_attn")
+    return out, lse
+
+
+def logits_adjust(logits, tokens=None, row_len=None, prompt_len=None, row_seq=None, repetition=None, presence=None,
+                  frequency=None, bias=None, mask=None, mask_row=None, out=None, best: bool = True, stream=None):
+    """Penalties for repeated tokens, biases and a grammar's mask on logits [rows,
+    vocab], and the token with the largest logit left (pard_logits_adjust).
+    tokens: int32 [sequences, length] histories, of which row r counts the first
+    row_len[r] of sequence row_seq[r] (None: r), prompt_len[s] of them its
+    prompt; repetition, presence, frequency: float32 [sequences]; bias: (start
+    [sequences + 1], ids, values); mask: int32 [masks, vocab / 32 rounded up] of
+    bits, mask_row[r] (None: r) the row's, negative: none.  Returns (out, best): out is
+    new unless given and may be logits itself; best None if not wanted."""
+    import torch
+    _no_gradient("logits_adjust", logits)
+    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _bad("logits_adjust: logits: a [rows, vocab] device tensor with contiguous rows is wanted")
+    rows, vocab = logits.shape
+    dev = logits.device
+    vec = lambda t, what, n, dtype=torch.int32: None if t is None else _vector(t, what, n, dtype, dev)  # noqa: E731
+    n_seqs = rows
+    if tokens is not None:
+        if tokens.dim() != 2 or tokens.dtype != torch.int32 or tokens.device != dev or not tokens.is_contiguous():
+            _bad("logits_adjust: tokens: a contiguous int32 [sequences, length] tensor on the logits' device is wanted")
+        if row_len is None:
+            _bad("logits_adjust: tokens need row_len")
+        n_seqs = tokens.shape[0]
+    elif bias is not None:
+        n_seqs = bias[0].shape[0] - 1
+    if mask is not None and (mask.dim() != 2 or mask.dtype != torch.int32 or mask.device != dev or not mask.is_contiguous()
+                             or mask.shape[1] < (vocab + 31) // 32 or (mask_row is None and mask.shape[0] < rows)):
+        _bad("logits_adjust: mask: a contiguous int32 tensor of rows of vocab bits on the logits' device is wanted")
+    start, ids, values = (None, None, None) if bias is None else bias
+    n_bias = 0 if bias is None else ids.numel()
+    pointers = [vec(row_seq, "row_seq", rows), vec(row_len, "row_len", rows), vec(prompt_len, "prompt_len", n_seqs),
+                *(vec(t, what, n_seqs, torch.float32) for t, what in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency"))),
+                vec(start, "bias start", n_seqs + 1), vec(ids, "bias ids", n_bias), vec(values, "bias values", n_bias, torch.float32)]
+    p_mask_row = vec(mask_row, "mask_row", rows)
+    with _On(dev, stream, logits, tokens, row_len, prompt_len, row_seq, repetition, presence, frequency, start, ids, values, mask, mask_row,
+             out) as on:
+        if out is None:
+            out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
+        elif out.dtype != logits.dtype or out.device != dev or out.shape != logits.shape or (vocab > 1 and out.stride(1) != 1):
+            _bad("logits_adjust: out: a tensor like logits is wanted")
+        top = torch.empty(rows, dtype=torch.int32, device=dev) if best else None
+        args = pard_logits_args(rows, vocab, _dtype(logits, "logits_adjust"), max(n_seqs, 1), logits.data_ptr(), logits.stride(0),
+                                out.data_ptr(), out.stride(0), None if tokens is None else tokens.data_ptr(),
+                                0 if tokens is None else tokens.shape[1], *pointers, n_bias, 0 if mask is None else mask.shape[0],
+                                None if mask is None else mask.data_ptr(), 0 if mask is None else mask.shape[1], p_mask_row,
+                                None if top is None else top.data_ptr())
+        n_ws = lib.pard_logits_workspace_bytes(args)
+        ws = _workspace(n_ws, dev) if n_ws else None
+        _done(lib.pard_logits_adjust(args, ws.data_ptr() if n_ws else None, n_ws, on.handle), "pard_logits_adjust")
+    return out, top
 
 
 class Engine:

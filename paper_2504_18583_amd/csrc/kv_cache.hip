@@ -1,0 +1,226 @@
+// Rows of keys and values into a paged cache and out of it.
+//
+// A lane holds 8 elements of a head (16 bytes of a 16-bit type), so a block of
+// 32, which shares a scale, is four neighbouring lanes: its largest magnitude
+// takes two exchanges within quads of lanes.  A row of the batch is one run of
+// units (head by head, keys then values); a wavefront takes one row, or several
+// where a row has fewer than 64 units.
+//
+// Bound: memory, each element read once and written once.
+#include "serve.h"
+
+#include <algorithm>
+
+namespace pard {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kSeqsInLds = 1024;
+
+struct Row8 { float v[8]; };
+
+template <class E, bool VEC>
+__device__ __forceinline__ Row8 load8(const char* row, int64_t at) {
+  const typename E::T* p = reinterpret_cast<const typename E::T*>(row) + at;
+  Row8 r;
+  if constexpr (VEC) {
+    if constexpr (sizeof(typename E::T) == 4) {
+      const u32x4 a = reinterpret_cast<const u32x4*>(p)[0], b = reinterpret_cast<const u32x4*>(p)[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.v[i] = __uint_as_float(a[i]), r.v[4 + i] = __uint_as_float(b[i]);
+    } else {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.v[i] = E::load((uint16_t)(a[i >> 1] >> (16 * (i & 1))));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = E::load(p[i]);
+  }
+  return r;
+}
+
+template <class E>
+__device__ __forceinline__ u32x4 pack8(const Row8& r) {
+  u32x4 a;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = (uint32_t)E::store(r.v[2 * i]) | (uint32_t)E::store(r.v[2 * i + 1]) << 16;
+  return a;
+}
+
+template <class E, bool VEC>
+__device__ __forceinline__ void store8(char* row, int64_t at, const Row8& r) {
+  typename E::T* p = reinterpret_cast<typename E::T*>(row) + at;
+  if constexpr (VEC) {
+    if constexpr (sizeof(typename E::T) == 4) {
+      u32x4 a, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(r.v[i]), b[i] = __float_as_uint(r.v[4 + i]);
+      reinterpret_cast<u32x4*>(p)[0] = a;
+      reinterpret_cast<u32x4*>(p)[1] = b;
+    } else {
+      *reinterpret_cast<u32x4*>(p) = pack8<E>(r);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = E::store(r.v[i]);
+  }
+}
+
+// The scale byte of a block with this largest magnitude (as bits: an order of
+// floats): the exponent field e + 127 of the smallest 2^e, e >= -126, with
+// largest <= (2 - 2^-FRACTION_GAP..) 2^(e + TOP): a fraction above the type's
+// largest one carries into the exponent.  255: the block is NaN.
+template <int DT>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
+  constexpr uint32_t kCarry = DT == PARD_E4M3 ? 0x1fffffu : 0x3fffffu;   // 448 = 1.75 2^8, 6 = 1.5 2^2
+  constexpr int kTop = DT == PARD_E4M3 ? 8 : 2;
+  if (largest >= 0x7f800000u) return 255;
+  return (uint32_t)max((int)((largest + kCarry) >> 23) - kTop, 1);
+}
+
+template <int HD, class E, int DT, bool VEC, bool WRITE>
+__global__ __launch_bounds__(256) void k_kv_copy(const KvCopyArgs a) {
+  constexpr int HU = HD / 8;                          // units of a head
+  constexpr int RB = kv_row_bytes(DT, HD), SB = kv_scale_bytes(DT, HD);
+  __shared__ int starts[kSeqsInLds + 1];
+  const KvBatchView& b = a.batch;
+  const bool in_lds = b.n_seqs <= kSeqsInLds;
+  if (in_lds) {
+    for (int i = threadIdx.x; i <= b.n_seqs; i += 256) starts[i] = b.row_start[i];
+    __syncthreads();
+  }
+  const int lane = threadIdx.x & 63, units = 2 * a.cache.n_kv * HU;
+  const int per_row = min(units, 64), per_wave = 64 / per_row;            // lanes of a row, rows of a wavefront
+  const int wave = blockIdx.x * 4 + (threadIdx.x >> 6), n_waves = gridDim.x * 4;
+  const int sub = lane / per_row, u0 = lane - sub * per_row;
+  if (sub >= per_wave) return;
+  for (int64_t r64 = (int64_t)wave * per_wave + sub; r64 < b.rows; r64 += (int64_t)n_waves * per_wave) {
+    const int row = (int)r64;
+    const int s = in_lds ? kv_seq_of(starts, b.n_seqs, row) : kv_seq_of(b.row_start, b.n_seqs, row);
+    if (s >= b.n_seqs || row < b.row_start[s]) continue;                  // (a row of no sequence)
+    const int pos = b.kv_len[s] - b.row_start[s + 1] + row;
+    const int page = pos < 0 ? -1 : kv_page(a.cache, b, s, pos);
+    if (WRITE && page < 0) continue;
+    const int place = pos & ((1 << a.cache.page_log2) - 1);
+    for (int u = u0; u < units; u += per_row) {
+      const bool is_v = u >= units / 2;
+      const int head = (is_v ? u - units / 2 : u) / HU, unit = u % HU;
+      const Heads& rows = is_v ? a.v : a.k;
+      char* const data = rows.data;
+      const int64_t at = row * rows.rs + head * rows.hs + unit * 8;
+      const int64_t slot = (((int64_t)max(page, 0) * a.cache.n_kv + head) << a.cache.page_log2) + place;
+      char* const held = (is_v ? a.cache.v : a.cache.k) + slot * RB + unit * (RB / HU);
+      uint8_t* const scale = SB ? (is_v ? a.cache.v_scale : a.cache.k_scale) + slot * SB + unit / 4 : nullptr;
+      if constexpr (WRITE) {
+        Row8 r = load8<E, VEC>(data, at);
+        if constexpr (SB) {
+          uint32_t big = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) big = max(big, __float_as_uint(r.v[i]) & 0x7fffffffu);
+          big = max(big, (uint32_t)__builtin_amdgcn_mov_dpp((int)big, 0xB1, 0xF, 0xF, false));   // quad_perm 1 0 3 2
+          big = max(big, (uint32_t)__builtin_amdgcn_mov_dpp((int)big, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
+          const uint32_t byte = scale_byte<DT>(big);
+          if (unit % 4 == 0) *scale = (uint8_t)byte;
+          const float inv = __uint_as_float((254 - min(byte, 253u)) << 23);    // 2^-e: products with it are exact
+#pragma unroll
+          for (int i = 0; i < 8; ++i) r.v[i] *= inv;
+          if constexpr (DT == PARD_E4M3) {
+            u32x2 w = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              int x = __builtin_amdgcn_cvt_pk_fp8_f32(r.v[4 * i], r.v[4 * i + 1], 0, false);
+              x = __builtin_amdgcn_cvt_pk_fp8_f32(r.v[4 * i + 2], r.v[4 * i + 3], x, true);
+              w[i] = (uint32_t)x;
+            }
+            *reinterpret_cast<u32x2*>(held) = w;
+          } else {
+            uint32_t w = 0;
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[0], r.v[1], 1.f, 0);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[2], r.v[3], 1.f, 1);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[4], r.v[5], 1.f, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[6], r.v[7], 1.f, 3);
+            *reinterpret_cast<uint32_t*>(held) = w;
+          }
+        } else if constexpr (DT == PARD_BF16) {
+          *reinterpret_cast<u32x4*>(held) = pack8<ElemBF16>(r);
+        } else {
+          *reinterpret_cast<u32x4*>(held) = pack8<ElemF16>(r);
+        }
+      } else {
+        Row8 r;
+        if (page < 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) r.v[i] = __uint_as_float(0x7fc00000u);
+        } else if constexpr (SB) {
+          const uint32_t byte = *scale;
+          const float f = __uint_as_float(byte == 0 ? 0x400000u : byte == 255 ? 0x7fc00000u : byte << 23);
+          if constexpr (DT == PARD_E4M3) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(held);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false);
+              const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+              r.v[4 * i] = lo[0] * f, r.v[4 * i + 1] = lo[1] * f, r.v[4 * i + 2] = hi[0] * f, r.v[4 * i + 3] = hi[1] * f;
+            }
+          } else {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(held);
+            const f32x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+            const f32x2 x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+            r = Row8{{x0[0] * f, x0[1] * f, x1[0] * f, x1[1] * f, x2[0] * f, x2[1] * f, x3[0] * f, x3[1] * f}};
+          }
+        } else {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(held);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint16_t h = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+            r.v[i] = DT == PARD_BF16 ? ElemBF16::load(h) : ElemF16::load(h);
+          }
+        }
+        store8<E, VEC>(data, at, r);
+      }
+    }
+  }
+}
+
+template <int HD, class E, int DT, bool VEC>
+hipError_t launch_dir(bool write, const KvCopyArgs& a, hipStream_t st) {
+  const int units = 2 * a.cache.n_kv * (HD / 8), per_wave = 64 / std::min(units, 64);
+  const int64_t waves = ((int64_t)a.batch.rows + per_wave - 1) / per_wave;
+  const unsigned grid = (unsigned)std::min<int64_t>((waves + 3) / 4, 1 << 16);
+  if (write) k_kv_copy<HD, E, DT, VEC, true><<<grid, 256, 0, st>>>(a);
+  else k_kv_copy<HD, E, DT, VEC, false><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <int HD, class E, bool VEC>
+hipError_t launch_type(bool write, int cache_dtype, const KvCopyArgs& a, hipStream_t st) {
+  switch (cache_dtype) {
+    case PARD_BF16: return launch_dir<HD, E, PARD_BF16, VEC>(write, a, st);
+    case PARD_F16: return launch_dir<HD, E, PARD_F16, VEC>(write, a, st);
+    case PARD_E4M3: return launch_dir<HD, E, PARD_E4M3, VEC>(write, a, st);
+    default: return launch_dir<HD, E, PARD_E2M1, VEC>(write, a, st);
+  }
+}
+
+template <int HD, bool VEC>
+hipError_t launch_rows(bool write, int dtype, int cache_dtype, const KvCopyArgs& a, hipStream_t st) {
+  if (dtype == PARD_F32) return launch_type<HD, ElemF32, VEC>(write, cache_dtype, a, st);
+  if (dtype == PARD_BF16) return launch_type<HD, ElemBF16, VEC>(write, cache_dtype, a, st);
+  return launch_type<HD, ElemF16, VEC>(write, cache_dtype, a, st);
+}
+
+}  // namespace
+
+hipError_t launch_kv_copy(bool write, int head_dim, int dtype, int cache_dtype, bool vec, const KvCopyArgs& a,
+                          hipStream_t st) {
+  if (head_dim == 64)
+    return vec ? launch_rows<64, true>(write, dtype, cache_dtype, a, st) : launch_rows<64, false>(write, dtype, cache_dtype, a, st);
+  return vec ? launch_rows<128, true>(write, dtype, cache_dtype, a, st) : launch_rows<128, false>(write, dtype, cache_dtype, a, st);
+}
+
+}  // namespace pard

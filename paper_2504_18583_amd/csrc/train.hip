@@ -1,6 +1,6 @@
 // C entry points of the mask-token training operators: argument checks (host
 // only, before any device work), workspaces, launches.
-#include "train.h"
+#include "tensor_args.h"
 
 #include <algorithm>
 #include <cmath>
@@ -8,39 +8,6 @@
 using namespace pard;
 
 namespace {
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-pard_status status_of(hipError_t e) { return e == hipSuccess ? PARD_OK : PARD_ERR_DEVICE; }
-
-int elem_size(int dtype) { return dtype == PARD_F32 ? 4 : dtype == PARD_BF16 || dtype == PARD_F16 ? 2 : 0; }
-
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-// A tensor of `heads` heads of `hd` elements in `rows` rows that is read, or
-// (out) written: then no two of its heads share an element.
-bool heads_ok(const pard_heads* t, int64_t rows, int heads, int hd, bool out) {
-  if (!t || t->row_stride < 0 || t->head_stride < 0) return false;
-  if (rows == 0 || heads == 0) return true;
-  if (!t->data) return false;
-  if (!out) return true;
-  // heads within a row, or rows within a head
-  const __int128 r = t->row_stride, h = t->head_stride;
-  const bool by_row = (heads == 1 || h >= hd) && (rows == 1 || r >= h * (heads - 1) + hd);
-  const bool by_head = (rows == 1 || r >= hd) && (heads == 1 || h >= r * (rows - 1) + hd);
-  return by_row || by_head;
-}
-
-// Whether an output may lie where an input does: as the input, or apart from it
-// (overlaps of tensors that start elsewhere are the caller's to avoid).
-bool apart(const pard_heads* a, const pard_heads* b) { return a->data != b->data; }
-bool same_or_apart(const pard_heads* a, const pard_heads* b, int64_t rows, int heads) {
-  return apart(a, b) || ((rows == 1 || a->row_stride == b->row_stride) && (heads == 1 || a->head_stride == b->head_stride));
-}
-
-Heads view(const pard_heads* t) {
-  return t ? Heads{static_cast<char*>(t->data), t->row_stride, t->head_stride} : Heads{nullptr, 0, 0};
-}
 
 bool rope_spec_ok(const pard_rope_spec* s, int32_t n_pos) {
   if (!s || s->rot_dim < 2 || s->rot_dim > 1024 || s->rot_dim % 2 || n_pos < 1 || n_pos > (1 << 24)) return false;
@@ -102,10 +69,6 @@ bool attn_heads_ok(const pard_heads* t, const pard_cod_attn_args* a, int heads, 
          t->head_stride % 8 == 0 && t->row_stride <= kMaxStride && t->head_stride <= kMaxStride;
 }
 
-Heads16 view16(const pard_heads* t) {
-  return Heads16{static_cast<char*>(t->data), (uint32_t)(2 * t->row_stride), (uint32_t)(2 * t->head_stride)};
-}
-
 CodAttnArgs attn_args(const pard_cod_attn_args* a) {
   CodAttnArgs r{};
   cod_plan_layout(a->plan->rows, a->plan->n_samples, const_cast<void*>(a->plan->data), &r.plan);
@@ -114,9 +77,7 @@ CodAttnArgs attn_args(const pard_cod_attn_args* a) {
   r.n_heads = a->n_heads;
   r.n_kv = a->n_kv_heads;
   r.group = a->n_heads / a->n_kv_heads;
-  r.by_group.d = r.group;
-  while ((1u << r.by_group.l) < r.by_group.d) ++r.by_group.l;
-  r.by_group.m = (uint32_t)(((1ull << (30 + r.by_group.l)) + r.by_group.d - 1) / r.by_group.d);
+  r.by_group = fast_div(r.group);
   r.rows = a->plan->rows;
   r.scale = a->scale;
   return r;
