@@ -33,53 +33,6 @@ namespace {
 using namespace cod;
 
 constexpr int kStageKeys = 64;
-constexpr float kLazy = 8.f;
-
-// Softmax of NB blocks of 16 keys: scores s become packed probabilities pf,
-// running maximum m (base 2), sum l and output o follow.  Hidden scores are
-// -infinity; m starts finite, so that a row without keys keeps l = 0.  The product
-// takes probabilities of 16 bits (the sum does not): what is lost is of the size of
-// the output's own rounding (1B layer, bf16: 2.2e-3 of the output's magnitude off,
-// where rounding the exact output is 1.6e-3).
-template <int NQ, int NB, int DB, class M>
-__device__ __forceinline__ void softmax_step(const f32x4 (&s)[NQ][NB], float (&m)[NQ], float (&l)[NQ], f32x4 (&o)[NQ][DB],
-                                             u32x4 (&pf)[NQ][NB / 2], float scale2) {
-  bool raise = false;
-  float mx[NQ];
-#pragma unroll
-  for (int t = 0; t < NQ; ++t) {
-    float v = fmaxf(s[t][0][0], s[t][0][1]);
-#pragma unroll
-    for (int i = 2; i < 4 * NB; i += 2) v = fmaxf(fmaxf(v, s[t][i / 4][i % 4]), s[t][i / 4][i % 4 + 1]);
-    mx[t] = v * scale2;
-    raise |= mx[t] > m[t] + kLazy;
-  }
-  if (__any(raise)) {                                // uniform
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      const float mr = max4g(mx[t]);
-      const float m_new = mr > m[t] + kLazy ? mr : m[t];
-      const float corr = __builtin_amdgcn_exp2f(m[t] - m_new);
-      m[t] = m_new;
-      l[t] *= corr;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[t][db] *= corr;
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < NQ; ++t)
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) {
-      float p[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][kb][i], scale2, -m[t]));
-        l[t] += p[i];
-      }
-      pf[t][kb >> 1][(kb & 1) * 2] = M::pack(p[0], p[1]);
-      pf[t][kb >> 1][(kb & 1) * 2 + 1] = M::pack(p[2], p[3]);
-    }
-}
 
 template <int HD, int NQ, class M>
 __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void k_cod_attn(const CodAttnArgs a) {

@@ -2,6 +2,7 @@
 // any device work), workspaces, launches.
 #include "serve.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "tensor_args.h"
@@ -84,8 +85,8 @@ KvAttnArgs attn_args(const pard_kv_attn_args* a) {
   r.n_heads = a->n_heads;
   r.group = a->n_heads / a->cache->n_kv_heads;
   r.by_group = fast_div(r.group);
-  r.window = a->window;
-  r.sinks = a->sinks;
+  r.window = std::min(a->window, 1 << 30);  // (positions with a page are below 2^30)
+  r.sinks = std::min(a->sinks, 1 << 30);
   r.scale = a->scale;
   return r;
 }
@@ -130,7 +131,7 @@ pard_status pard_kv_read(const pard_kv_cache* cache, const pard_kv_batch* batch,
 }
 
 size_t pard_kv_attn_workspace_bytes(const pard_kv_attn_args* args) {
-  return attn_check(args) == PARD_OK ? kv_attn_workspace(attn_args(args), args->cache->head_dim) : 0;
+  return attn_check(args) == PARD_OK ? kv_attn_workspace(attn_args(args), args->cache->head_dim, args->batch->max_seq_rows) : 0;
 }
 
 pard_status pard_kv_attn(const pard_kv_attn_args* args, const pard_heads* q, const pard_heads* out, float* lse,
@@ -141,7 +142,7 @@ pard_status pard_kv_attn(const pard_kv_attn_args* args, const pard_heads* q, con
   if (args->batch->rows == 0) return PARD_OK;
   if (!apart(q, out) || out->data == args->cache->k || out->data == args->cache->v) return PARD_ERR_ARG;
   KvAttnArgs r = attn_args(args);
-  const size_t need = kv_attn_workspace(r, args->cache->head_dim);
+  const size_t need = kv_attn_workspace(r, args->cache->head_dim, args->batch->max_seq_rows);
   if (!workspace || !aligned(workspace, 256)) return PARD_ERR_ARG;
   if (workspace_bytes < need) return PARD_ERR_NOMEM;
   r.q = view16(q);
