@@ -29,8 +29,8 @@ namespace {
 using namespace cod;
 
 constexpr int kStageKeys = 64;
-constexpr int kMinShare = 4;               // stages of a share at least
-constexpr int kShares = 512;               // shares that long contexts are cut into, about
+constexpr int kMinKeys = 256;              // keys of a share at least
+constexpr int kShares = 512;               // shares that all stages are cut into, about
 
 // ---- sharing out ------------------------------------------------------------
 
@@ -41,7 +41,7 @@ struct SeqWork {
   int stages;                              // of a tile, at most
 };
 
-template <int QP>
+template <int QP, int KEYS>
 __device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int s) {
   SeqWork w{};
   if (s >= a.batch.n_seqs) return w;
@@ -52,8 +52,8 @@ __device__ __forceinline__ SeqWork seq_work(const KvAttnArgs& a, int s) {
   w.tiles = (w.rows * a.group + QP - 1) / QP;
   int keys = min(max(w.len, 0), a.batch.cap);
   // (with a window: what a tile's rows see between them, and a partial stage)
-  if (a.window) keys = (int)min((int64_t)keys, (int64_t)a.window + min(w.rows, QP / a.group + 2) + min(a.sinks, keys) + kStageKeys);
-  w.stages = w.tiles ? max((keys + kStageKeys - 1) / kStageKeys, 1) : 0;
+  if (a.window) keys = (int)min((int64_t)keys, (int64_t)a.window + min(w.rows, QP / a.group + 2) + min(a.sinks, keys) + KEYS);
+  w.stages = w.tiles ? max((keys + KEYS - 1) / KEYS, 1) : 0;
   return w;
 }
 
@@ -72,20 +72,24 @@ __device__ __forceinline__ int scan(int x) {
 
 __device__ __forceinline__ int shares_of(const SeqWork& w, int share) { return (w.stages + share - 1) / share; }
 
-// The length of a share, such that about kShares of them hold all stages; every
-// wavefront finds the same.
-template <int QP>
+// The length of a share; every wavefront finds the same.  kShares of it hold all
+// stages, or half as many where there are so many tiles that only the longest
+// need be cut.
+template <int QP, int KEYS>
 __device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& first, int lane) {
   float total = 0.f;
+  int tiles = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {   // uniform
-    const SeqWork w = s0 ? seq_work<QP>(a, s0 + lane) : first;
+    const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
     float x = (float)w.tiles * w.stages;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
     total += x;
+    tiles = min(tiles + __builtin_amdgcn_readlane(scan(min(w.tiles, kShares)), 63), kShares);
   }
   total *= a.cache.n_kv;
-  return max(kMinShare, (int)fminf(ceilf(total / kShares), 1 << 24));
+  const float shares = tiles * a.cache.n_kv >= kShares / 2 ? kShares / 2 : kShares;
+  return max(kMinKeys / KEYS, (int)fminf(ceilf(total / shares), 1 << 24));
 }
 
 struct Item {
@@ -96,12 +100,12 @@ struct Item {
 
 // Item `left` of a key head: a tile's shares first, then tiles (the last first:
 // they see the most keys), then sequences.
-template <int QP>
+template <int QP, int KEYS>
 __device__ __forceinline__ Item find_item(const KvAttnArgs& a, const SeqWork& first, int share, int left, int kvh, int lane) {
   Item it{};
   int slots = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {
-    const SeqWork w = s0 ? seq_work<QP>(a, s0 + lane) : first;
+    const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
     const int n = shares_of(w, share), items = w.tiles * n, split = n > 1 ? items : 0;
     const int upto = scan(items), slots_upto = scan(split);
     const uint64_t past = __ballot(upto > left);
@@ -196,28 +200,44 @@ struct KvF16 : MmaF16 {
   }
 };
 
+// At most N loads still in flight.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x0f70 | (N >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+
 // Partial sums of a tile: [QP][HD] of O, [QP] maxima, [QP] sums.
 template <int HD, int QP>
 constexpr int kRecord = QP * (HD + 2);
 
-template <int HD, int NQ, class M, int DT>
-__global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_attn(const KvAttnArgs a) {
+// Wavefronts a SIMD, as LDS and registers allow.
+template <int HD, int NQ, int DT>
+constexpr int kResident = NQ == 2 ? (HD == 128 ? 2 : 3) : 4;
+
+// KH: wavefronts that share 16 NQ pairs, each with its part of a stage's keys.
+template <int HD, int NQ, int KH, class M, int DT>
+__global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(const KvAttnArgs a) {
   constexpr int QW = 16 * NQ, QP = 4 * QW;             // pairs of a wavefront, of the workgroup
+  constexpr int NB = 4 / KH;                           // blocks of 16 keys of a wavefront
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
   constexpr int RB = kv_row_bytes(DT, HD), SB = kv_scale_bytes(DT, HD);
+  constexpr int AHEAD = SB ? 2 : 1;                    // stages in flight beside the current one
   // a stage: four blocks of K, four of V; two arrays of their own (the
   // compiler's waits before an LDS read cover the loads into that array only)
   __shared__ __attribute__((aligned(16))) u32x4 b0[8 * BU], b1[8 * BU];
   __shared__ int any_bad;                              // a stage of this item has a key without a page
+  __shared__ float ml[KH == 2 ? 4 : 1][2][16];
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // its pairs (and the block of every stage that it loads), its part of the keys
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, part = __builtin_amdgcn_readfirstlane(tid >> 8);
   const KvBatchView& b = a.batch;
-  const SeqWork first = seq_work<QP>(a, lane);
-  const int share = share_length<QP>(a, first, lane);
+  const SeqWork first = seq_work<QP, kStageKeys>(a, lane);
+  const int share = share_length<QP, kStageKeys>(a, first, lane);
   // key heads fastest: with 8 of them each keeps to an XCD and its L2
   const int kvh = blockIdx.x % a.cache.n_kv;
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
-    const Item it = find_item<QP>(a, first, share, u, kvh, lane);
+    const Item it = find_item<QP, kStageKeys>(a, first, share, u, kvh, lane);
     if (it.splits == 0) return;                        // uniform: past the last item
     if (it.splits > 1 && it.slot >= a.slots) continue; // uniform (row_start does not ascend)
     __syncthreads();                                   // (the item before has read LDS)
@@ -249,37 +269,33 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
       const Block k = block_of(st);
       return table[min(k.key, k.high) >> a.cache.page_log2];
     };
-    Staged<HD, M, DT> sk, sv;
-    auto load = [&](u32x4* buf, int st, int entry) __attribute__((always_inline)) {
+    struct Parts { Staged<HD, M, DT> x[2 / KH]; };     // of K and V; with two parts, the first's wavefronts load K
+    Parts p0, p1;
+    auto load = [&](Parts& p, u32x4* buf, int st, int entry) __attribute__((always_inline)) {
       const Block k = block_of(st);
       int page = __builtin_amdgcn_readfirstlane(entry);
       if ((uint32_t)page >= (uint32_t)a.cache.n_pages) {  // uniform
         page = 0;
         if (lane == 0) any_bad = 1;
       }
-      const int r = DT == PARD_E4M3 || DT == PARD_E2M1 ? c16 : block_row(lane);
+      const int r = SB ? c16 : block_row(lane);
       const int place = max(min(k.key + r, k.high), k.low) & ((1 << a.cache.page_log2) - 1);
       const int64_t slot = (((int64_t)page * a.cache.n_kv + kvh) << a.cache.page_log2) + place;
-      if constexpr (SB) {
-        sk.load(a.cache.k + slot * RB, a.cache.k_scale + slot * SB, g4);
-        sv.load(a.cache.v + slot * RB, a.cache.v_scale + slot * SB, g4);
-      } else {
-        load_block<HD>(a.cache.k + slot * RB + block_byte(lane), buf + wave * BU);
-        load_block<HD>(a.cache.v + slot * RB + block_byte(lane), buf + (4 + wave) * BU);
+#pragma unroll
+      for (int i = 0; i < 2 / KH; ++i) {
+        const bool is_v = KH == 2 ? part : i;
+        const char* const src = (is_v ? a.cache.v : a.cache.k) + slot * RB;
+        if constexpr (SB) p.x[i].load(src, (is_v ? a.cache.v_scale : a.cache.k_scale) + slot * SB, g4);
+        else load_block<HD>(src + block_byte(lane), buf + (4 * is_v + wave) * BU);
       }
     };
-    auto widen = [&](u32x4* buf) __attribute__((always_inline)) {
+    auto widen = [&](const Parts& p, u32x4* buf) __attribute__((always_inline)) {
       if constexpr (SB) {
-        sk.store(buf + wave * BU, c16, g4);
-        sv.store(buf + (4 + wave) * BU, c16, g4);
+#pragma unroll
+        for (int i = 0; i < 2 / KH; ++i) p.x[i].store(buf + (4 * (KH == 2 ? part : i) + wave) * BU, c16, g4);
       }
     };
 
-    int entry = 0;
-    if (st0 < st1) {                                   // uniform
-      load(b0, st0, entry_of(st0));
-      if (st0 + 1 < st1) entry = entry_of(st0 + 1);
-    }
     // this lane's pairs: those past the sequence repeat its last and are not stored
     const int w_pair = pair0 + wave * QW;
     const bool idle = w_pair >= n_pairs;               // uniform: no pairs of its own
@@ -288,6 +304,13 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
     float m[NQ], l[NQ];
     f32x4 o[NQ][DB];
     int pos[NQ];
+    // table entries of the stages to be loaded next (any stage's may be read),
+    // read as many stages before their loads that these wait for nothing newer
+    int e0 = 0, e1 = 0, e2 = 0, e3 = 0;
+    if (st0 < st1) {                                   // uniform
+      e0 = entry_of(st0), e1 = entry_of(st0 + 1), e2 = entry_of(st0 + 2);
+      if constexpr (AHEAD == 2) e3 = entry_of(st0 + 3);
+    }
     const uint32_t sign = scale_sign(a.scale);
     const float scale2 = base2_scale(a.scale);
 #pragma unroll
@@ -302,6 +325,10 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    if (st0 < st1) {                                   // uniform
+      load(p0, b0, st0, e0);
+      if (AHEAD == 2 && st0 + 1 < st1) load(p1, b1, st0 + 1, e1);
+    }
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
@@ -311,19 +338,22 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
 
     auto compute = [&](int st, const u32x4* cur) __attribute__((always_inline)) {
       const bool in_a = st < n_a;
-      const int key0 = in_a ? st * kStageKeys : from + (st - n_a) * kStageKeys, end = key0 + kStageKeys - 1;
-      const int low = in_a ? 0 : lo, high = in_a ? a_last : last, gone = a.window ? w_lo - a.window : -1;   // keys up to `gone` are no row's but first tokens
-      if (idle || key0 > w_hi || (end <= gone && key0 >= a.sinks)) return;   // uniform: no row of this wavefront sees it
-      f32x4 sc[NQ][4];
+      const int key0 = (in_a ? st * kStageKeys : from + (st - n_a) * kStageKeys) + part * NB * 16, end = key0 + NB * 16 - 1;
+      const int low = in_a ? 0 : lo, high = in_a ? a_last : last;
+      const int gone = a.window ? w_lo - a.window : -1;  // keys up to it are no row's but first tokens
+      if (idle || key0 > min(w_hi, high) || (end <= gone && key0 >= a.sinks)) return;   // uniform: no row of this wavefront sees them
+      const u32x4* const kc = cur + part * NB * BU;
+      const u32x4* const vc = kc + 4 * BU;
+      f32x4 sc[NQ][NB];
 #pragma unroll
       for (int t = 0; t < NQ; ++t)
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) sc[t][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kb = 0; kb < NB; ++kb) sc[t][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
+      for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 kf = rows_frag(cur + kb * BU, ks, lane);
+          const u32x4 kf = rows_frag(kc + kb * BU, ks, lane);
 #pragma unroll
           for (int t = 0; t < NQ; ++t) sc[t][kb] = M::mma(kf, q[t][ks], sc[t][kb]);
         }
@@ -331,7 +361,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
       const bool whole = key0 >= low && end <= min(w_lo, high) && (!a.window || key0 > w_hi - a.window || end < a.sinks);
       if (bad || !whole) {                             // uniform
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
+        for (int kb = 0; kb < NB; ++kb) {
           const int k16 = key0 + kb * 16;
           const bool none = bad && (uint32_t)table[min(k16, high) >> a.cache.page_log2] >= (uint32_t)a.cache.n_pages;
 #pragma unroll
@@ -345,43 +375,80 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
             }
         }
       }
-      u32x4 pf[NQ][2];
-      softmax_step<NQ, 4, DB, M>(sc, m, l, o, pf, scale2);
+      u32x4 pf[NQ][NB / 2];
+      softmax_step<NQ, NB, DB, M>(sc, m, l, o, pf, scale2);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+      for (int tt = 0; tt < NB / 2; ++tt)
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const u32x4 vf = cols_frag<HD>(cur + (4 + 2 * tt) * BU, db, lane);
+          const u32x4 vf = cols_frag<HD>(vc + 2 * tt * BU, db, lane);
 #pragma unroll
           for (int t = 0; t < NQ; ++t) o[t][db] = M::mma(vf, pf[t][tt], o[t][db]);
         }
     };
-    auto stage = [&](int st, const u32x4* cur, u32x4* nxt) __attribute__((always_inline)) {
-      wait_and_meet();
-      const bool more = st + 1 < st1;
-      if (more) {                                      // uniform
-        const int e = entry;
-        if (st + 2 < st1) entry = entry_of(st + 2);
-        load(nxt, st + 1, e);
+    // One stage; entry: of stage st + AHEAD, loaded into nxt (16 bits) or p (then
+    // q1, the next stage, is widened into nxt).
+    auto stage = [&](int st, const u32x4* cur, u32x4* nxt, int& entry, Parts& p, const Parts& q1) __attribute__((always_inline)) {
+      // this wavefront's loads of the stage are in LDS, and its LDS accesses done;
+      // then everyone's
+      if constexpr (SB) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);            // lgkmcnt(0): newer loads stay in flight
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        wait_and_meet();
+      }
+      if (st + AHEAD < st1) {                          // uniform
+        load(p, nxt, st + AHEAD, entry);
+        entry = entry_of(st + AHEAD + 2);
       }
       __builtin_amdgcn_sched_barrier(0);
       compute(st, cur);
-      if (more) widen(nxt);
+      if (SB && st + 1 < st1) widen(q1, nxt);
     };
-    if (st0 < st1) widen(b0);
-    int st = st0;
-    for (; st + 2 <= st1; st += 2) {
-      stage(st, b0, b1);
-      stage(st + 1, b1, b0);
+    if constexpr (SB) {
+      if (st0 < st1) widen(p0, b0);
+      for (int st = st0; st < st1; st += 2) {          // uniform
+        stage(st, b0, b1, e2, p0, p1);
+        if (st + 1 < st1) stage(st + 1, b1, b0, e3, p1, p0);
+      }
+    } else {
+      for (int st = st0; st < st1; st += 2) {
+        stage(st, b0, b1, e1, p0, p0);
+        if (st + 1 < st1) stage(st + 1, b1, b0, e2, p0, p0);
+      }
     }
-    if (st < st1) stage(st, b0, b1);
+
+    // the second part's sums are added to the first's
+    float sums[NQ];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) sums[t] = sum4g(l[t]);
+    if constexpr (KH == 2) {
+      static_assert(NQ == 1, "one tile of pairs");
+      __syncthreads();                                 // (LDS is no longer read)
+      if (part == 1) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) b0[(wave * DB + db) * 64 + lane] = __builtin_bit_cast(u32x4, o[0][db]);
+        if (g4 == 0) ml[wave][0][c16] = m[0], ml[wave][1][c16] = sums[0];
+      }
+      __syncthreads();
+      if (part == 1) continue;                         // uniform by wavefront: the barriers of the next item meet again
+      const float m1 = ml[wave][0][c16], top = fmaxf(m[0], m1);
+      const float f0 = __builtin_amdgcn_exp2f(m[0] - top), f1 = __builtin_amdgcn_exp2f(m1 - top);
+      m[0] = top;
+      sums[0] = sums[0] * f0 + ml[wave][1][c16] * f1;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[0][db] = o[0][db] * f0 + __builtin_bit_cast(f32x4, b0[(wave * DB + db) * 64 + lane]) * f1;
+    }
 
     // lane (c16, g4) holds elements 16 db + 4 g4 .. + 3 of pair 16 t + c16
     const float nan = __uint_as_float(0x7fc00000u);
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       const int pair = w_pair + t * 16 + c16, in_tile = wave * QW + t * 16 + c16;
-      float sum = sum4g(l[t]);
+      float sum = sums[t];
       if (pair >= n_pairs) continue;
       if (pos[t] >= b.cap) sum = nan;                  // (past the table)
       if (it.splits > 1) {                             // uniform
@@ -405,18 +472,302 @@ __global__ __launch_bounds__(256, HD == 128 ? 2 : NQ == 2 ? 3 : 4) void k_kv_att
   }
 }
 
-// Joins the shares of split sequences: a wavefront per pair, shares in order.
-template <int HD, int QP, class M>
+// Few pairs: a workgroup owns 16 NT of them, each of its wavefronts all of these
+// against a quarter of the keys, 32 of every stage of 128, so that a token's
+// bytes pass through one wavefront only and no wavefront waits for another
+// until the end.  K goes straight into operand registers (8 and 4 bits:
+// a lane's 16 bytes are elements next to each other, and Q's are put in the same
+// order), V through the wavefront's own LDS, which transposes it; the next tile
+// is in flight during the current one.
+constexpr int kFewKeys = 128;
+
+// K of a block of 16 keys as operands: of step s, lane (c16, g4) holds key c16's
+// elements first(s, g4) .. + 7.
+template <int HD, class M, int DT>
+struct Keys {
+  u32x4 x[HD / 32];
+  static __device__ __forceinline__ int first(int s, int g) { return 32 * s + 8 * g; }
+  __device__ __forceinline__ void load(const char* row, const uint8_t*, int g) {
+#pragma unroll
+    for (int s = 0; s < HD / 32; ++s) x[s] = *reinterpret_cast<const u32x4*>(row + s * 64 + g * 16);
+  }
+  __device__ __forceinline__ u32x4 frag(int s) const { return x[s]; }
+};
+template <int HD, class M>
+struct Keys<HD, M, PARD_E4M3> {
+  u32x4 x[HD / 64];
+  uint32_t scale;
+  static __device__ __forceinline__ int first(int s, int g) { return 64 * (s / 2) + 16 * g + 8 * (s % 2); }
+  __device__ __forceinline__ void load(const char* row, const uint8_t* scales, int g) {
+#pragma unroll
+    for (int h = 0; h < HD / 64; ++h) x[h] = *reinterpret_cast<const u32x4*>(row + h * 64 + g * 16);
+    if constexpr (HD == 128) scale = *reinterpret_cast<const uint32_t*>(scales) >> (8 * (g >> 1));
+    else scale = *reinterpret_cast<const uint16_t*>(scales) >> (8 * (g >> 1));
+  }
+  __device__ __forceinline__ u32x4 frag(int s) const {
+    const float f = __uint_as_float((scale >> (16 * (s / 2)) & 255) << 23);
+    const uint32_t a = x[s / 2][2 * (s % 2)], b = x[s / 2][2 * (s % 2) + 1];
+    return u32x4{M::fp8(a, f, false), M::fp8(a, f, true), M::fp8(b, f, false), M::fp8(b, f, true)};
+  }
+};
+template <int HD, class M>
+struct Keys<HD, M, PARD_E2M1> {
+  uint32_t x[HD / 32];
+  uint32_t scale;
+  static __device__ __forceinline__ int first(int s, int g) { return HD / 4 * g + 8 * s; }
+  __device__ __forceinline__ void load(const char* row, const uint8_t* scales, int g) {
+    if constexpr (HD == 128) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(row + g * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = v[i];
+      scale = scales[g];
+    } else {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(row + g * 8);
+      x[0] = v[0], x[1] = v[1];
+      scale = scales[g >> 1];
+    }
+  }
+  __device__ __forceinline__ u32x4 frag(int s) const {
+    const float f = __uint_as_float(scale << 23);
+    return u32x4{M::template fp4<0>(x[s], f), M::template fp4<1>(x[s], f), M::template fp4<2>(x[s], f), M::template fp4<3>(x[s], f)};
+  }
+};
+
+template <int HD, int NT, class M, int DT>
+__global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
+  constexpr int QP = 16 * NT;
+  constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
+  constexpr int RB = kv_row_bytes(DT, HD), SB = kv_scale_bytes(DT, HD);
+  constexpr int NEXT = 4 * KS;                         // 16 bits: loads of a tile
+  // V of a tile by wavefront; 16 bits: of the next one too
+  __shared__ __attribute__((aligned(16))) u32x4 v0[8 * BU], v1[SB ? 1 : 8 * BU];
+  __shared__ float ml[4][2][16];
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const KvBatchView& b = a.batch;
+  const SeqWork first = seq_work<QP, kFewKeys>(a, lane);
+  const int share = share_length<QP, kFewKeys>(a, first, lane);
+  const int kvh = blockIdx.x % a.cache.n_kv;           // (as k_kv_attn)
+  for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
+    const Item it = find_item<QP, kFewKeys>(a, first, share, u, kvh, lane);
+    if (it.splits == 0) return;                        // uniform: past the last item
+    if (it.splits > 1 && it.slot >= a.slots) continue; // uniform (row_start does not ascend)
+    const int n_pairs = it.w.rows * a.group, pair0 = it.tile * QP;
+    const int pos0 = it.w.len - it.w.rows;
+    auto row_of = [&](int pair) { return quotient(min(pair, n_pairs - 1), a.by_group); };
+    const int pos_lo = pos0 + row_of(pair0), pos_hi = pos0 + row_of(pair0 + QP - 1);
+    const int last = min(pos_hi, b.cap - 1);
+    int lo = a.window ? max(pos_lo - a.window + 1, 0) : 0;
+    int a_last = min(a.sinks, lo) - 1;
+    if (a.sinks >= lo) lo = 0, a_last = -1;            // one run of keys
+    const int from = lo & ~15, n_a = (a_last + kFewKeys) / kFewKeys;
+    const int n_all = last < 0 ? 0 : n_a + (last - from) / kFewKeys + 1;
+    const int st0 = (int)((int64_t)n_all * it.split / it.splits), st1 = (int)((int64_t)n_all * (it.split + 1) / it.splits);
+
+    // this wavefront's 32 keys of a stage
+    struct Tile { int key, low, high; };
+    auto tile_of = [&](int st) __attribute__((always_inline)) {
+      const bool in_a = st < n_a;
+      const int key = (in_a ? st * kFewKeys : from + (st - n_a) * kFewKeys) + wave * 32;
+      return Tile{key, in_a ? 0 : lo, in_a ? a_last : last};
+    };
+    const int32_t* const table = b.table + (int64_t)it.seq * b.max_pages;
+    struct Entries { int e[2]; };
+    auto entries_of = [&](int st) __attribute__((always_inline)) {
+      const Tile k = tile_of(st);
+      return Entries{{table[min(k.key, k.high) >> a.cache.page_log2], table[min(k.key + 16, k.high) >> a.cache.page_log2]}};
+    };
+    struct Loaded {
+      Keys<HD, M, DT> k[2];
+      Staged<HD, M, DT> v[2];
+      bool none[2];                                    // blocks without a page
+    };
+    auto load = [&](Loaded& d, u32x4* vbuf, int st, const Entries& e) __attribute__((always_inline)) {
+      const Tile k = tile_of(st);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        int page = __builtin_amdgcn_readfirstlane(e.e[i]);
+        d.none[i] = (uint32_t)page >= (uint32_t)a.cache.n_pages;
+        page = d.none[i] ? 0 : page;
+        const int64_t base = ((int64_t)page * a.cache.n_kv + kvh) << a.cache.page_log2;
+        auto place = [&](int r) { return max(min(k.key + 16 * i + r, k.high), k.low) & ((1 << a.cache.page_log2) - 1); };
+        const int64_t slot = base + place(c16);
+        d.k[i].load(a.cache.k + slot * RB, SB ? a.cache.k_scale + slot * SB : nullptr, g4);
+        if constexpr (SB) d.v[i].load(a.cache.v + slot * RB, a.cache.v_scale + slot * SB, g4);
+      }
+      if constexpr (!SB) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int page = d.none[i] ? 0 : __builtin_amdgcn_readfirstlane(e.e[i]);
+          const int64_t base = ((int64_t)page * a.cache.n_kv + kvh) << a.cache.page_log2;
+          const int place = max(min(k.key + 16 * i + block_row(lane), k.high), k.low) & ((1 << a.cache.page_log2) - 1);
+          load_block<HD>(a.cache.v + (base + place) * RB + block_byte(lane), vbuf + (wave * 2 + i) * BU);
+        }
+      }
+    };
+
+    Loaded d0, d1;
+    Entries next{};
+    // (a run's last stage may have no keys for this wavefront: such a tile is skipped)
+    auto here = [&](int st) __attribute__((always_inline)) { const Tile k = tile_of(st); return k.key <= k.high; };
+    Entries now{};
+    if (st0 < st1) {                                   // uniform
+      now = entries_of(st0);
+      if (st0 + 1 < st1) next = entries_of(st0 + 1);
+    }
+    u32x4 q[NT][KS];
+    float m[NT], l[NT];
+    f32x4 o[NT][DB];
+    int pos[NT];
+    const uint32_t sign = scale_sign(a.scale);
+    const float scale2 = base2_scale(a.scale);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int pair = min(pair0 + t * 16 + c16, n_pairs - 1), r = quotient(pair, a.by_group);
+      pos[t] = pos0 + r;
+      const char* src = at(a.q, it.w.row0 + r, kvh * a.group + remainder(pair, r, a.by_group));
+#pragma unroll
+      for (int s = 0; s < KS; ++s) q[t][s] = *reinterpret_cast<const u32x4*>(src + 2 * Keys<HD, M, DT>::first(s, g4));
+      m[t] = -1e30f;
+      l[t] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (st0 < st1) load(d0, v0, st0, now);             // uniform
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[t][s][i] ^= sign;
+
+    auto tile = [&](int st, Loaded& d, u32x4* vbuf, Loaded& dn, u32x4* vnext) __attribute__((always_inline)) {
+      const bool more = st + 1 < st1;
+      __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0): the tile before has left LDS
+      asm volatile("" ::: "memory");
+      if (more) {                                      // uniform
+        const Entries e = next;
+        if (st + 2 < st1) next = entries_of(st + 2);
+        load(dn, vnext, st + 1, e);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (!here(st)) return;                           // uniform
+      const Tile k = tile_of(st);
+      const int end = k.key + 31;
+      f32x4 sc[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const u32x4 kf = d.k[i].frag(s);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sc[t][i] = M::mma(kf, q[t][s], sc[t][i]);
+        }
+      const bool whole = k.key >= k.low && end <= min(pos_lo, k.high) && (!a.window || k.key > pos_hi - a.window || end < a.sinks);
+      if (d.none[0] || d.none[1] || !whole) {          // uniform
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int key = k.key + i * 16 + g4 * 4 + j;
+              const bool seen = key >= k.low && key <= min(pos[t], k.high) && (!a.window || key > pos[t] - a.window || key < a.sinks);
+              if (!seen) sc[t][i][j] = -INFINITY;
+              else if (d.none[i]) sc[t][i][j] = __uint_as_float(0x7fc00000u);
+            }
+      }
+      u32x4 pf[NT][1];
+      softmax_step<NT, 2, DB, M>(sc, m, l, o, pf, scale2);
+      u32x4* const mine = vbuf + wave * 2 * BU;
+      if constexpr (SB) {
+        // (this wavefront's reads of the tile before are done: their products were waited for)
+        d.v[0].store(mine, c16, g4);
+        d.v[1].store(mine + BU, c16, g4);
+        asm volatile("" ::: "memory");
+      } else {
+        if (more) wait_loads<NEXT>();
+        else wait_loads<0>();
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x4 vf = cols_frag<HD>(mine, db, lane);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t][db] = M::mma(vf, pf[t][0], o[t][db]);
+      }
+    };
+    int st = st0;
+    for (; st + 2 <= st1; st += 2) {
+      tile(st, d0, v0, d1, SB ? v0 : v1);
+      tile(st + 1, d1, SB ? v0 : v1, d0, v0);
+    }
+    if (st < st1) tile(st, d0, v0, d1, SB ? v0 : v1);
+
+    // The wavefronts' sums, 16 pairs at a time: each adds up, in the wavefronts'
+    // order, a quarter of the elements.
+    const float nan = __uint_as_float(0x7fc00000u);
+    float* const rec = static_cast<float*>(a.work) + (int64_t)it.slot * kRecord<HD, QP>;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float sum = sum4g(l[t]);
+      __syncthreads();                                 // (LDS is no longer read)
+      if (g4 == 0) ml[wave][0][c16] = m[t], ml[wave][1][c16] = sum;
+      __syncthreads();
+      float top = m[t];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][0][c16]);
+      sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) sum += ml[w][1][c16] * __builtin_amdgcn_exp2f(ml[w][0][c16] - top);
+      const float f = __builtin_amdgcn_exp2f(m[t] - top);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) v0[(wave * DB + db) * 64 + lane] = __builtin_bit_cast(u32x4, o[t][db] * f);
+      __syncthreads();
+      const int pair = pair0 + t * 16 + c16, in_tile = t * 16 + c16;
+      if (pos[t] >= b.cap) sum = nan;                  // (past the table)
+      const int r = quotient(min(pair, n_pairs - 1), a.by_group);
+      const int head = kvh * a.group + remainder(min(pair, n_pairs - 1), r, a.by_group), row = it.w.row0 + r;
+      const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);     // (1 ulp of float32, before the rounding to 16 bits)
+      if (pair < n_pairs) {
+#pragma unroll
+        for (int j = 0; j < DB / 4; ++j) {
+          const int db = wave * (DB / 4) + j;
+          f32x4 v = __builtin_bit_cast(f32x4, v0[db * 64 + lane]);
+#pragma unroll
+          for (int w = 1; w < 4; ++w) v += __builtin_bit_cast(f32x4, v0[(w * DB + db) * 64 + lane]);
+          if (it.splits > 1) {                         // uniform
+            *reinterpret_cast<f32x4*>(rec + in_tile * HD + db * 16 + g4 * 4) = v;
+          } else {
+            v = v * inv;
+            *reinterpret_cast<u32x2*>(at(a.out, row, head) + db * 32 + g4 * 8) = u32x2{M::pack(v[0], v[1]), M::pack(v[2], v[3])};
+          }
+        }
+        if (wave == 0 && g4 == 0) {
+          if (it.splits > 1) rec[QP * HD + in_tile] = top, rec[QP * HD + QP + in_tile] = sum;
+          else if (a.lse) a.lse[(int64_t)head * b.rows + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+      }
+    }
+    __syncthreads();                                   // (the next item's loads write LDS)
+  }
+}
+
+// Joins the shares of split sequences: a wavefront per pair; 16 (32) lanes hold
+// its 64 (128) elements, and the four (two) groups of lanes take turns with the
+// shares.
+template <int HD, int QP, int KEYS, class M>
 __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
-  constexpr int PER = HD / 64;
-  const int lane = threadIdx.x & 63;
+  constexpr int W = HD / 4, TURNS = 64 / W, AT_ONCE = 8;
+  const int lane = threadIdx.x & 63, turn = lane / W, e = lane % W;
   const int n_waves = gridDim.x * 4;
-  const SeqWork first = seq_work<QP>(a, lane);
-  const int share = share_length<QP>(a, first, lane);
+  const SeqWork first = seq_work<QP, KEYS>(a, lane);
+  const int share = share_length<QP, KEYS>(a, first, lane);
   int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // pair of all split sequences, key heads fastest
   int before = 0, slots = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {                       // uniform
-    const SeqWork w = s0 ? seq_work<QP>(a, s0 + lane) : first;
+    const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
     const int n = shares_of(w, share), items = n > 1 ? w.tiles * n : 0;
     const int upto = scan(items), pairs = n > 1 ? w.rows * a.group : 0, pairs_upto = scan(pairs);
     const int all = __builtin_amdgcn_readlane(pairs_upto, 63);
@@ -429,35 +780,44 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
       if ((slot0 + splits) * a.cache.n_kv > a.slots) continue;             // (row_start does not ascend)
       const float* const rec = static_cast<const float*>(a.work) + ((int64_t)slot0 * a.cache.n_kv + kvh) * kRecord<HD, QP>;
       const int64_t step = (int64_t)a.cache.n_kv * kRecord<HD, QP>;
+      // the group's shares (maxima are finite; past the last one: nothing)
       float top = -1e30f, sum = 0.f;
-      for (int i = lane; i < splits; i += 64) {        // (maxima are finite)
-        const float m = rec[i * step + QP * HD + in_tile], s = rec[i * step + QP * HD + QP + in_tile], t = fmaxf(top, m);
-        sum = sum * __builtin_amdgcn_exp2f(top - t) + s * __builtin_amdgcn_exp2f(m - t);
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int i0 = turn; i0 < splits + turn; i0 += TURNS * AT_ONCE) {      // uniform
+        f32x4 x[AT_ONCE];
+        float m[AT_ONCE], s[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+          const int i = min(i0 + j * TURNS, splits - 1);
+          x[j] = *reinterpret_cast<const f32x4*>(rec + i * step + in_tile * HD + e * 4);
+          m[j] = rec[i * step + QP * HD + in_tile];
+          s[j] = rec[i * step + QP * HD + QP + in_tile];
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+          if (i0 + j * TURNS >= splits) continue;
+          const float t = fmaxf(top, m[j]), f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m[j] - t);
+          top = t;
+          sum = sum * f0 + s[j] * f1;
+          o = o * f0 + x[j] * f1;
+        }
+      }
+#pragma unroll
+      for (int d = W; d < 64; d *= 2) {                                    // the groups', in a tree
+        const float m2 = __shfl_xor(top, d), s2 = __shfl_xor(sum, d), t = fmaxf(top, m2);
+        const float f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m2 - t);
         top = t;
-      }
-      const float own = top;
+        sum = sum * f0 + s2 * f1;
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-      sum *= __builtin_amdgcn_exp2f(own - top);
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-      float o[PER] = {};
-#pragma unroll 8
-      for (int i = 0; i < splits; ++i) {
-        const float f = __builtin_amdgcn_exp2f(rec[i * step + QP * HD + in_tile] - top);
-#pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] += f * rec[i * step + in_tile * HD + lane * PER + e];
+        for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + __shfl_xor(o[j], d) * f1;
       }
-      const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
-      const int r = quotient(pair, a.by_group), head = kvh * a.group + remainder(pair, r, a.by_group), row = from(w.row0) + r;
-      char* const dst = at(a.out, row, head);
-      if constexpr (PER == 2) {
-        reinterpret_cast<uint32_t*>(dst)[lane] = M::pack(o[0] * inv, o[1] * inv);
-      } else {
-        reinterpret_cast<uint16_t*>(dst)[lane] = (uint16_t)M::pack(o[0] * inv, 0.f);
+      if (turn == 0) {
+        const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
+        const int r = quotient(pair, a.by_group), head = kvh * a.group + remainder(pair, r, a.by_group), row = from(w.row0) + r;
+        *reinterpret_cast<u32x2*>(at(a.out, row, head) + e * 8) = u32x2{M::pack(o[0] * inv, o[1] * inv), M::pack(o[2] * inv, o[3] * inv)};
+        if (a.lse && e == 0)
+          a.lse[(int64_t)head * a.batch.rows + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
       }
-      if (a.lse && lane == 0)
-        a.lse[(int64_t)head * a.batch.rows + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
     before += all;
     slots += __builtin_amdgcn_readlane(upto, 63);
@@ -469,12 +829,14 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
 int64_t max_tiles(const KvAttnArgs& a, int qp) {
   return std::min<int64_t>(a.batch.n_seqs, a.batch.rows) + (int64_t)a.batch.rows * a.group / qp;
 }
-bool may_split(const KvAttnArgs& a) { return a.batch.cap > kMinShare * kStageKeys; }
+bool may_split(const KvAttnArgs& a) { return a.batch.cap > kMinKeys; }
 
-// Pairs of a workgroup: 64 where sequences have few, on average.
+// Pairs of a workgroup: those of a sequence up to 64 (known, or on average),
+// else 128.
 int tile_pairs(const KvAttnArgs& a, int max_seq_rows) {
-  const int64_t most = (int64_t)max_seq_rows * a.group;
-  return (max_seq_rows > 0 && most <= 64) || (int64_t)a.batch.rows * a.group <= 64ll * a.batch.n_seqs ? 64 : 128;
+  const int64_t mean = ((int64_t)a.batch.rows * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
+  const int64_t pairs = max_seq_rows > 0 ? std::min((int64_t)max_seq_rows * a.group, mean) : mean;
+  return pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
 }
 
 // Records of partial sums: a sequence of k > 1 shares has k - 1 of them full, so
@@ -482,27 +844,35 @@ int tile_pairs(const KvAttnArgs& a, int max_seq_rows) {
 // everything.
 int64_t max_slots(const KvAttnArgs& a, int qp) {
   if (!may_split(a)) return 0;
-  const int64_t cap_stages = (a.batch.cap + kStageKeys - 1) / kStageKeys + 2;
-  return std::min<int64_t>(max_tiles(a, qp) * a.cache.n_kv * ((cap_stages + kMinShare - 1) / kMinShare), 2 * kShares + 2);
+  const int64_t shares = (a.batch.cap + kMinKeys - 1) / kMinKeys + 2;
+  return std::min<int64_t>(max_tiles(a, qp) * a.cache.n_kv * shares, 2 * kShares + 2);
 }
 
-template <int HD, int NQ, class M, int DT>
-hipError_t launch_tiles(KvAttnArgs a, hipStream_t st) {
-  constexpr int QP = 64 * NQ;
+template <int HD, int QP, class M, int DT>
+hipError_t launch_pairs(KvAttnArgs a, hipStream_t st) {
   a.slots = (int)max_slots(a, QP);
   const int64_t items = max_tiles(a, QP) + (may_split(a) ? kShares / a.cache.n_kv + 1 : 0);   // of a key head
   const int64_t most = std::max((1 << 20) / a.cache.n_kv, 1);
-  k_kv_attn<HD, NQ, M, DT><<<(unsigned)(std::min(items, most) * a.cache.n_kv), 256, 0, st>>>(a);
+  const unsigned grid = (unsigned)(std::min(items, most) * a.cache.n_kv);
+  constexpr int KEYS = QP >= 64 ? kStageKeys : kFewKeys;
+  if constexpr (QP == 128) k_kv_attn<HD, 2, 1, M, DT><<<grid, 256, 0, st>>>(a);
+  else if constexpr (QP == 64) k_kv_attn<HD, 1, 2, M, DT><<<grid, 512, 0, st>>>(a);
+  else k_kv_few<HD, QP / 16, M, DT><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !may_split(a)) return e;
   const int64_t waves = (int64_t)a.batch.rows * a.n_heads;
-  k_kv_join<HD, QP, M><<<(unsigned)std::min<int64_t>((waves + 3) / 4, 1024), 256, 0, st>>>(a);
+  k_kv_join<HD, QP, KEYS, M><<<(unsigned)std::min<int64_t>((waves + 3) / 4, 2048), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <int HD, class M, int DT>
 hipError_t launch_cache(const KvAttnArgs& a, int max_seq_rows, hipStream_t st) {
-  return tile_pairs(a, max_seq_rows) == 64 ? launch_tiles<HD, 1, M, DT>(a, st) : launch_tiles<HD, 2, M, DT>(a, st);
+  switch (tile_pairs(a, max_seq_rows)) {
+    case 16: return launch_pairs<HD, 16, M, DT>(a, st);
+    case 32: return launch_pairs<HD, 32, M, DT>(a, st);
+    case 64: return launch_pairs<HD, 64, M, DT>(a, st);
+    default: return launch_pairs<HD, 128, M, DT>(a, st);
+  }
 }
 
 template <int HD, class M, int SAME>
