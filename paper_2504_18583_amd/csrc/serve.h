@@ -88,9 +88,10 @@ struct LogitsArgs {
   const int32_t* mask_row;
   int n_masks;
   int32_t* best;
-  uint64_t* keys;                          // workspace: [rows][chunks]
+  uint64_t* keys;                          // workspace: [rows][logits_keys]
+  int row0;                                // first row of a launch
 };
-int logits_chunks(int rows, int vocab);    // workgroups that share a row
+int logits_keys(int vocab);                // candidates of a row for best
 hipError_t launch_logits_adjust(int dtype, const LogitsArgs& a, hipStream_t st);
 
 }  // namespace pard

@@ -155,7 +155,7 @@ pard_status pard_kv_attn(const pard_kv_attn_args* args, const pard_heads* q, con
 
 size_t pard_logits_workspace_bytes(const pard_logits_args* args) {
   if (logits_check(args) != PARD_OK || !args->best) return 0;
-  return align256((size_t)args->rows * logits_chunks((int)args->rows, args->vocab) * sizeof(uint64_t));
+  return align256((size_t)args->rows * logits_keys(args->vocab) * sizeof(uint64_t));
 }
 
 pard_status pard_logits_adjust(const pard_logits_args* args, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -168,7 +168,7 @@ pard_status pard_logits_adjust(const pard_logits_args* args, void* workspace, si
   const LogitsArgs r{(int)a.rows, a.vocab, a.n_seqs, static_cast<const char*>(a.logits), a.logits_stride, static_cast<char*>(a.out),
                      a.out_stride, a.tokens, a.row_seq, a.row_len, a.prompt_len, a.tokens_stride, a.repetition, a.presence,
                      a.frequency, a.bias_start, a.bias_ids, a.bias_values, a.n_bias, a.mask, a.mask_stride, a.mask_row,
-                     a.n_masks, a.best, static_cast<uint64_t*>(workspace)};
+                     a.n_masks, a.best, static_cast<uint64_t*>(workspace), 0};
   return status_of(launch_logits_adjust(a.dtype, r, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
