@@ -625,8 +625,9 @@ def cod_loss(logits, labels, section, n_sections: int, weights: Optional[Sequenc
 def _no_gradient(what: str, *tensors) -> None:
     """Turns away tensors that require gradients where torch would record them."""
     import torch
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        _bad(f"{what} has no gradient: call it under torch.no_grad()")
+    for t in tensors:
+        if t.requires_grad and torch.is_grad_enabled():
+            _bad(f"{what} has no gradient: call it under torch.no_grad()")
 
 
 class KVCache:
@@ -659,6 +660,7 @@ class KVCache:
             self.dtype = PARD_E4M3 if k.shape[3] == hd else PARD_E2M1
         self.k, self.v, self.k_scale, self.v_scale, self.device, self.head_dim = k, v, k_scale, v_scale, k.device, hd
         self.n_kv_heads = k.shape[1]
+        self.tensors = k, v, k_scale, v_scale
         self.c = pard_kv_cache(k.shape[0], k.shape[2], k.shape[1], hd, self.dtype, k.data_ptr(), v.data_ptr(),
                                None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
 
@@ -689,10 +691,11 @@ class KVBatch:
         _vector(row_start, "row_start", n + 1, torch.int32, self.device)
         _vector(kv_len, "kv_len", n, torch.int32, self.device)
         self.page_table, self.row_start, self.kv_len, self.max_seq_rows = page_table, row_start, kv_len, int(max_seq_rows)
+        self._fields = (*page_table.shape, self.max_seq_rows, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr())
+        self.tensors = page_table, row_start, kv_len
 
     def c(self, rows: int) -> pard_kv_batch:
-        return pard_kv_batch(rows, *self.page_table.shape, self.max_seq_rows, self.page_table.data_ptr(),
-                             self.row_start.data_ptr(), self.kv_len.data_ptr())
+        return pard_kv_batch(rows, *self._fields)
 
 
 def _same_device(what: str, device, cache: KVCache, batch: KVBatch) -> None:
@@ -709,7 +712,7 @@ def kv_write(k, v, cache: KVCache, batch: KVBatch, stream=None) -> None:
     if k.shape != v.shape:
         _bad(f"kv_write: k: shape {tuple(k.shape)}, expected {tuple(v.shape)}")
     _same_device("kv_write", k.device, cache, batch)
-    with _On(k.device, stream, k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.page_table, batch.row_start, batch.kv_len) as on:
+    with _On(k.device, stream, k, v, *cache.tensors, *batch.tensors) as on:
         _done(lib.pard_kv_write(cache.c, batch.c(k.shape[0]), _dtype(k, "kv_write"), hk, hv, on.handle), "pard_kv_write")
 
 
@@ -720,17 +723,17 @@ def kv_read(cache: KVCache, batch: KVBatch, rows: int, dtype=None, k_out=None, v
     import torch
     shape = (rows, cache.n_kv_heads, cache.head_dim)
     _same_device("kv_read", cache.device, cache, batch)
-    if k_out is not None and v_out is not None and k_out.dtype != v_out.dtype:
-        _bad("kv_read: outputs of one type are wanted")
-    for t in (k_out, v_out):
-        dtype = t.dtype if t is not None and dtype is None else dtype
-    with _On(cache.device, stream, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.page_table, batch.row_start, batch.kv_len, k_out,
-             v_out) as on:
-        new = lambda: torch.empty(shape, dtype=dtype or torch.bfloat16, device=cache.device)  # noqa: E731
-        like = new()[:0]
-        k_out, v_out = (new() if t is None else t for t in (k_out, v_out))
-        hk, hv = _heads(k_out, "k_out", like, shape), _heads(v_out, "v_out", like, shape)
-        _done(lib.pard_kv_read(cache.c, batch.c(rows), _dtype(like, "kv_read"), hk, hv, on.handle), "pard_kv_read")
+    if dtype is None:
+        dtype = k_out.dtype if k_out is not None else v_out.dtype if v_out is not None else torch.bfloat16
+    with _On(cache.device, stream, *cache.tensors, *batch.tensors, k_out, v_out) as on:
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dtype, device=cache.device)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=dtype, device=cache.device)
+        if k_out.dtype != dtype or v_out.dtype != dtype or k_out.device != cache.device:
+            _bad(f"kv_read: outputs of {dtype} on {cache.device} are wanted")
+        hk, hv = _heads(k_out, "k_out", v_out, shape), _heads(v_out, "v_out", k_out, shape)
+        _done(lib.pard_kv_read(cache.c, batch.c(rows), _dtype(k_out, "kv_read"), hk, hv, on.handle), "pard_kv_read")
     return k_out, v_out
 
 
@@ -749,7 +752,7 @@ def kv_attn(q, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, wi
     _same_device("kv_attn", q.device, cache, batch)
     scale = hd ** -0.5 if scale is None else float(scale)
     args = pard_kv_attn_args(C.pointer(cache.c), C.pointer(batch.c(rows)), n_q, _dtype(q, "kv_attn"), window, sinks, scale)
-    with _On(q.device, stream, q, cache.k, cache.v, cache.k_scale, cache.v_scale, batch.page_table, batch.row_start, batch.kv_len, out) as on:
+    with _On(q.device, stream, q, *cache.tensors, *batch.tensors, out) as on:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         ho = _heads(out, "out", q, q.shape)

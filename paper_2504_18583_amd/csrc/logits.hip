@@ -21,7 +21,6 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64, kPer = 16, kChunk = kThreads * kPer, kMaxRun = 32;
-constexpr int kWorkgroups = 1024;           // that the chip holds at once, about
 
 // Products and sums by themselves: what is left out changes nothing else.
 __device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
@@ -269,8 +268,11 @@ __global__ __launch_bounds__(256) void k_logits_best(const uint64_t* keys, int r
 template <class E>
 hipError_t launch_type(const LogitsArgs& a, hipStream_t st) {
   const int chunks = (a.vocab + kChunk - 1) / kChunk;
-  // rows of a run: about the workgroups that the chip holds at once are left
-  int run = (int)std::min<int64_t>(((int64_t)a.rows * chunks + kWorkgroups - 1) / kWorkgroups, kMaxRun);
+  // Rows of a run: few balance the ids that histories are full of (288 rows of
+  // 128 256 with all steps, histories to 1545: 83 us in 1024 workgroups, 77 in
+  // 4096), many scan a history less often (16 000 tokens: 84 and 105 us).
+  const int64_t wanted = a.tokens && a.tokens_stride > 2048 ? 1024 : 4096;
+  int run = (int)std::min<int64_t>(((int64_t)a.rows * chunks + wanted - 1) / wanted, kMaxRun);
   if ((a.rows + run - 1) / run > 65535) run = kMaxRun;
   const int size = sizeof(typename E::T), w = 16 / size;
   const bool vec = a.stride % w == 0 && a.out_stride % w == 0 && reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 &&
