@@ -360,6 +360,16 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
       const bool bad = any_bad;
       const bool whole = key0 >= low && end <= min(w_lo, high) && (!a.window || key0 > w_hi - a.window || end < a.sinks);
       if (bad || !whole) {                             // uniform
+        // (first tokens beside the window's keys are a run of their own or, where the
+        // two meet, the start of the one run)
+        const bool both = a.window && !in_a && a.sinks > low;
+        int span0[NQ];
+        uint32_t span[NQ];                             // keys span0 .. span0 + span - 1
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+          span0[t] = a.window && !in_a ? max(low, pos[t] - a.window + 1) : low;
+          span[t] = (uint32_t)max(min(pos[t], high) + 1 - span0[t], 0);
+        }
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
           const int k16 = key0 + kb * 16;
@@ -369,9 +379,8 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int key = k16 + g4 * 4 + i;
-              const bool seen = key >= low && key <= min(pos[t], high) && (!a.window || key > pos[t] - a.window || key < a.sinks);
-              if (!seen) sc[t][kb][i] = -INFINITY;
-              else if (none) sc[t][kb][i] = __uint_as_float(0x7fc00000u);
+              if (none) sc[t][kb][i] = __uint_as_float(0x7fc00000u);
+              if ((uint32_t)(key - span0[t]) >= span[t] && !(both && key < min(a.sinks, pos[t] + 1))) sc[t][kb][i] = -INFINITY;
             }
         }
       }
