@@ -70,6 +70,20 @@ __device__ __forceinline__ int scan(int x) {
   return x;
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus_shifted(float x) {
+  return x + __uint_as_float((uint32_t)shifted<CTRL, ROWS>((int)__float_as_uint(x)));
+}
+__device__ __forceinline__ float sum_lanes(float x) {
+  x = plus_shifted<0x111, 0xF>(x);
+  x = plus_shifted<0x112, 0xF>(x);
+  x = plus_shifted<0x114, 0xF>(x);
+  x = plus_shifted<0x118, 0xF>(x);
+  x = plus_shifted<0x142, 0xA>(x);
+  x = plus_shifted<0x143, 0xC>(x);
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+}
+
 __device__ __forceinline__ int shares_of(const SeqWork& w, int share) { return (w.stages + share - 1) / share; }
 
 // The length of a share; every wavefront finds the same.  kShares of it hold all
@@ -81,10 +95,7 @@ __device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& 
   int tiles = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {   // uniform
     const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
-    float x = (float)w.tiles * w.stages;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    total += x;
+    total += sum_lanes((float)w.tiles * w.stages);
     tiles = min(tiles + __builtin_amdgcn_readlane(scan(min(w.tiles, kShares)), 63), kShares);
   }
   total *= a.cache.n_kv;
@@ -207,13 +218,22 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// Everyone's LDS accesses are done; loads stay in flight.
+__device__ __forceinline__ void meet_with_loads() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);                  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Partial sums of a tile: [QP][HD] of O, [QP] maxima, [QP] sums.
 template <int HD, int QP>
 constexpr int kRecord = QP * (HD + 2);
 
 // Wavefronts a SIMD, as LDS and registers allow.
 template <int HD, int NQ, int DT>
-constexpr int kResident = NQ == 2 ? (HD == 128 ? 2 : 3) : 4;
+constexpr int kResident = NQ == 1 ? 4 : HD == 128 ? 2 : kv_scale_bytes(DT, HD) ? 3 : 4;
 
 // KH: wavefronts that share 16 NQ pairs, each with its part of a stage's keys.
 template <int HD, int NQ, int KH, class M, int DT>
@@ -222,7 +242,8 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
   constexpr int NB = 4 / KH;                           // blocks of 16 keys of a wavefront
   constexpr int KS = HD / 32, DB = HD / 16, BU = kBlockUnits<HD>;
   constexpr int RB = kv_row_bytes(DT, HD), SB = kv_scale_bytes(DT, HD);
-  constexpr int AHEAD = SB ? 2 : 1;                    // stages in flight beside the current one
+  // stages in flight beside the current one; loads of a stage
+  constexpr int AHEAD = SB ? 2 : 1, LOADS = 2 * KS / KH;
   // a stage: four blocks of K, four of V; two arrays of their own (the
   // compiler's waits before an LDS read cover the loads into that array only)
   __shared__ __attribute__((aligned(16))) u32x4 b0[8 * BU], b1[8 * BU];
@@ -308,8 +329,7 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
     // read as many stages before their loads that these wait for nothing newer
     int e0 = 0, e1 = 0, e2 = 0, e3 = 0;
     if (st0 < st1) {                                   // uniform
-      e0 = entry_of(st0), e1 = entry_of(st0 + 1), e2 = entry_of(st0 + 2);
-      if constexpr (AHEAD == 2) e3 = entry_of(st0 + 3);
+      e0 = entry_of(st0), e1 = entry_of(st0 + 1), e2 = entry_of(st0 + 2), e3 = entry_of(st0 + 3);
     }
     const uint32_t sign = scale_sign(a.scale);
     const float scale2 = base2_scale(a.scale);
@@ -327,7 +347,7 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
     }
     if (st0 < st1) {                                   // uniform
       load(p0, b0, st0, e0);
-      if (AHEAD == 2 && st0 + 1 < st1) load(p1, b1, st0 + 1, e1);
+      if (st0 + 1 < st1) load(p1, b1, st0 + 1, e1);
     }
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
@@ -400,15 +420,8 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
     auto stage = [&](int st, const u32x4* cur, u32x4* nxt, int& entry, Parts& p, const Parts& q1) __attribute__((always_inline)) {
       // this wavefront's loads of the stage are in LDS, and its LDS accesses done;
       // then everyone's
-      if constexpr (SB) {
-        __builtin_amdgcn_s_waitcnt(0xc07f);            // lgkmcnt(0): newer loads stay in flight
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-      } else {
-        wait_and_meet();
-      }
+      if constexpr (SB) meet_with_loads();
+      else wait_and_meet();
       if (st + AHEAD < st1) {                          // uniform
         load(p, nxt, st + AHEAD, entry);
         entry = entry_of(st + AHEAD + 2);
@@ -424,9 +437,16 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
         if (st + 1 < st1) stage(st + 1, b1, b0, e3, p1, p0);
       }
     } else {
-      for (int st = st0; st < st1; st += 2) {
-        stage(st, b0, b1, e1, p0, p0);
-        if (st + 1 < st1) stage(st + 1, b1, b0, e2, p0, p0);
+      // (the second stage's loads stay in flight during the first)
+      if (st0 < st1) {
+        if (st0 + 1 < st1) wait_loads<LOADS>();
+        else wait_loads<0>();
+        meet_with_loads();
+        compute(st0, b0);
+      }
+      for (int st = st0 + 1; st < st1; st += 2) {
+        stage(st, b1, b0, e2, p0, p0);
+        if (st + 1 < st1) stage(st + 1, b0, b1, e3, p0, p0);
       }
     }
 
