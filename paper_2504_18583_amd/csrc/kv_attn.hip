@@ -22,6 +22,7 @@
 #include <algorithm>
 
 #include "cod_attn_tile.h"
+#include "tensor_args.h"
 
 namespace pard {
 namespace {
@@ -86,11 +87,19 @@ __device__ __forceinline__ float sum_lanes(float x) {
 
 __device__ __forceinline__ int shares_of(const SeqWork& w, int share) { return (w.stages + share - 1) / share; }
 
-// The length of a share; every wavefront finds the same.  kShares of it hold all
-// stages, or half as many where there are so many tiles that only the longest
-// need be cut.
+// The length of a share from all stages and tiles: kShares of it hold all stages,
+// or half as many where there are so many tiles that only the longest need be
+// cut.  (Up to kShares tiles are counted.)
+template <int KEYS>
+__device__ __forceinline__ int share_of(const KvAttnArgs& a, float stages, int tiles) {
+  const float shares = tiles * a.cache.n_kv >= kShares / 2 ? kShares / 2 : kShares;
+  return max(kMinKeys / KEYS, (int)fminf(ceilf(stages * a.cache.n_kv / shares), 1 << 24));
+}
+
+// The same by one wavefront; every wavefront finds the same.
 template <int QP, int KEYS>
 __device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& first, int lane) {
+  if (a.plan) return a.plan[0];                        // uniform
   float total = 0.f;
   int tiles = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {   // uniform
@@ -98,15 +107,42 @@ __device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& 
     total += sum_lanes((float)w.tiles * w.stages);
     tiles = min(tiles + __builtin_amdgcn_readlane(scan(min(w.tiles, kShares)), 63), kShares);
   }
-  total *= a.cache.n_kv;
-  const float shares = tiles * a.cache.n_kv >= kShares / 2 ? kShares / 2 : kShares;
-  return max(kMinKeys / KEYS, (int)fminf(ceilf(total / shares), 1 << 24));
+  return share_of<KEYS>(a, total, tiles);
+}
+
+// The first sequence whose running number `upto` is past `left`, 64 candidates
+// at a time (n_seqs: none); its work in every lane, and the numbers up to it.
+struct Found {
+  SeqWork w;
+  int seq;
+};
+template <int QP, int KEYS>
+__device__ __forceinline__ Found search(const KvAttnArgs& a, const int* upto, int left, int lane) {
+  int lo = 0, n = a.batch.n_seqs;
+  while (n > 64) {                                     // uniform
+    const int step = (n + 63) / 64;
+    const uint64_t past = __ballot(upto[min(lo + (lane + 1) * step, lo + n) - 1] > left);
+    if (!past) return Found{SeqWork{}, a.batch.n_seqs};
+    const int l = __builtin_ctzll(past);
+    n = min(step, n - l * step);
+    lo += l * step;
+  }
+  const SeqWork w = seq_work<QP, KEYS>(a, lo + min(lane, n - 1));
+  const uint64_t past = __ballot(lane < n && upto[lo + min(lane, n - 1)] > left);
+  if (!past) return Found{SeqWork{}, a.batch.n_seqs};
+  const int l = __builtin_ctzll(past);
+  auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+  return Found{SeqWork{from(w.row0), from(w.rows), from(w.len), from(w.tiles), from(w.stages)}, lo + l};
 }
 
 struct Item {
   SeqWork w;
   int seq, tile, split, splits;            // splits 0: no such item
   int slot;                                // of its partial sums
+  // whether the numbers fit together: they do if row_start ascends
+  __device__ __forceinline__ bool valid(const KvAttnArgs& a) const {
+    return tile >= 0 && tile < w.tiles && split >= 0 && (splits == 1 || (slot >= 0 && slot < a.slots));
+  }
 };
 
 // Item `left` of a key head: a tile's shares first, then tiles (the last first:
@@ -114,6 +150,18 @@ struct Item {
 template <int QP, int KEYS>
 __device__ __forceinline__ Item find_item(const KvAttnArgs& a, const SeqWork& first, int share, int left, int kvh, int lane) {
   Item it{};
+  if (a.plan) {                                        // uniform
+    const Found f = search<QP, KEYS>(a, a.plan + 1, left, lane);
+    if (f.seq == a.batch.n_seqs) return it;
+    it.w = f.w;
+    it.seq = f.seq;
+    it.splits = shares_of(f.w, share);
+    const int mine = left - (f.seq ? a.plan[f.seq] : 0);
+    it.tile = f.w.tiles - 1 - mine / it.splits;
+    it.split = mine % it.splits;
+    it.slot = ((f.seq ? a.plan[a.batch.n_seqs + f.seq] : 0) + mine) * a.cache.n_kv + kvh;
+    return it;
+  }
   int slots = 0;
   for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {
     const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
@@ -136,6 +184,58 @@ __device__ __forceinline__ Item find_item(const KvAttnArgs& a, const SeqWork& fi
     slots += __builtin_amdgcn_readlane(slots_upto, 63);
   }
   return it;
+}
+
+// Running numbers of a large batch, by one workgroup ahead of the others: the
+// length of a share, then up to each sequence its shares, those that leave
+// partial sums, and the pairs of split sequences.  (Every wavefront adding up
+// 4096 sequences by itself took 5.4 ms for 300 keys each, 16 384 workgroups
+// twice 64 loads one after the other.)
+template <int QP, int KEYS>
+__global__ __launch_bounds__(1024) void k_kv_plan(const KvAttnArgs a) {
+  __shared__ float f_sum[16];
+  __shared__ int n_sum[16], i_sum[3][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.batch.n_seqs;
+  float total = 0.f;
+  int tiles = 0;
+  for (int s = tid; s < n; s += 1024) {
+    const SeqWork w = seq_work<QP, KEYS>(a, s);
+    total += (float)w.tiles * w.stages;
+    tiles = min(tiles + w.tiles, kShares);
+  }
+  total = sum_lanes(total);
+  tiles = __builtin_amdgcn_readlane(scan(tiles), 63);
+  if (lane == 0) f_sum[wave] = total, n_sum[wave] = tiles;
+  __syncthreads();
+  total = 0.f;
+  tiles = 0;
+  for (int w = 0; w < 16; ++w) total += f_sum[w], tiles = min(tiles + n_sum[w], kShares);
+  const int share = share_of<KEYS>(a, total, tiles);
+  if (tid == 0) a.plan[0] = share;
+  int before[3] = {};
+  for (int s0 = 0; s0 < n; s0 += 1024) {               // uniform
+    const SeqWork w = seq_work<QP, KEYS>(a, s0 + tid);
+    const int k = shares_of(w, share), items = w.tiles * k;
+    const int x[3] = {items, k > 1 ? items : 0, k > 1 ? w.rows * a.group : 0};
+    int upto[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      upto[i] = scan(x[i]);
+      if (lane == 63) i_sum[i][wave] = upto[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      int all = 0;
+      for (int v = 0; v < 16; ++v) {
+        if (v < wave) upto[i] += i_sum[i][v];
+        all += i_sum[i][v];
+      }
+      if (s0 + tid < n) a.plan[1 + i * n + s0 + tid] = before[i] + upto[i];
+      before[i] += all;
+    }
+    __syncthreads();
+  }
 }
 
 // ---- keys and values into LDS --------------------------------------------------
@@ -260,7 +360,7 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
     const Item it = find_item<QP, kStageKeys>(a, first, share, u, kvh, lane);
     if (it.splits == 0) return;                        // uniform: past the last item
-    if (it.splits > 1 && it.slot >= a.slots) continue; // uniform (row_start does not ascend)
+    if (!it.valid(a)) continue;                        // uniform (row_start does not ascend)
     __syncthreads();                                   // (the item before has read LDS)
     if (tid == 0) any_bad = 0;
     __syncthreads();
@@ -580,7 +680,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
     const Item it = find_item<QP, kFewKeys>(a, first, share, u, kvh, lane);
     if (it.splits == 0) return;                        // uniform: past the last item
-    if (it.splits > 1 && it.slot >= a.slots) continue; // uniform (row_start does not ascend)
+    if (!it.valid(a)) continue;                        // uniform (row_start does not ascend)
     const int n_pairs = it.w.rows * a.group, pair0 = it.tile * QP;
     const int pos0 = it.w.len - it.w.rows;
     auto row_of = [&](int pair) { return quotient(min(pair, n_pairs - 1), a.by_group); };
@@ -794,19 +894,44 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
   const SeqWork first = seq_work<QP, KEYS>(a, lane);
   const int share = share_length<QP, KEYS>(a, first, lane);
   int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // pair of all split sequences, key heads fastest
+  const int n_seqs = a.batch.n_seqs;
   int before = 0, slots = 0;
-  for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {                       // uniform
-    const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
-    const int n = shares_of(w, share), items = n > 1 ? w.tiles * n : 0;
-    const int upto = scan(items), pairs = n > 1 ? w.rows * a.group : 0, pairs_upto = scan(pairs);
-    const int all = __builtin_amdgcn_readlane(pairs_upto, 63);
+  for (int s0 = 0; s0 < n_seqs; s0 += a.plan ? n_seqs : 64) {             // uniform
+    SeqWork w = first;
+    int n = 0, upto = 0, items = 0, pairs = 0, pairs_upto = 0, all;
+    if (a.plan) {
+      all = a.plan[3 * n_seqs];                        // (the last sequence's running number)
+    } else {
+      if (s0) w = seq_work<QP, KEYS>(a, s0 + lane);
+      n = shares_of(w, share);
+      items = n > 1 ? w.tiles * n : 0;
+      upto = scan(items);
+      pairs = n > 1 ? w.rows * a.group : 0;
+      pairs_upto = scan(pairs);
+      all = __builtin_amdgcn_readlane(pairs_upto, 63);
+    }
     for (; unit < (before + all) * a.cache.n_kv; unit += n_waves) {
       const int kvh = unit % a.cache.n_kv, left = unit / a.cache.n_kv - before;
-      const int l = __builtin_ctzll(__ballot(pairs_upto > left));
-      auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-      const int pair = left - (from(pairs_upto) - from(pairs)), splits = from(n), in_tile = pair % QP;
-      const int slot0 = slots + from(upto) - from(items) + (from(w.tiles) - 1 - pair / QP) * splits;
-      if ((slot0 + splits) * a.cache.n_kv > a.slots) continue;             // (row_start does not ascend)
+      int pair, splits, slot0, row0;
+      if (a.plan) {
+        const Found f = search<QP, KEYS>(a, a.plan + 1 + 2 * n_seqs, left, lane);
+        if (f.seq == n_seqs) continue;                 // uniform
+        // (numbers that do not fit together: row_start does not ascend)
+        pair = left - (f.seq ? a.plan[2 * n_seqs + f.seq] : 0);
+        splits = shares_of(f.w, share);
+        slot0 = (f.seq ? a.plan[n_seqs + f.seq] : 0) + (f.w.tiles - 1 - pair / QP) * splits;
+        row0 = f.w.row0;
+        if (pair < 0 || pair >= f.w.rows * a.group || splits < 2) continue;
+      } else {
+        const int l = __builtin_ctzll(__ballot(pairs_upto > left));
+        auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+        pair = left - (from(pairs_upto) - from(pairs));
+        splits = from(n);
+        slot0 = slots + from(upto) - from(items) + (from(w.tiles) - 1 - pair / QP) * splits;
+        row0 = from(w.row0);
+      }
+      const int in_tile = pair % QP;
+      if (slot0 < 0 || (slot0 + splits) * a.cache.n_kv > a.slots) continue;   // (row_start does not ascend)
       const float* const rec = static_cast<const float*>(a.work) + ((int64_t)slot0 * a.cache.n_kv + kvh) * kRecord<HD, QP>;
       const int64_t step = (int64_t)a.cache.n_kv * kRecord<HD, QP>;
       // the group's shares (maxima are finite; past the last one: nothing)
@@ -842,7 +967,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
       }
       if (turn == 0) {
         const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
-        const int r = quotient(pair, a.by_group), head = kvh * a.group + remainder(pair, r, a.by_group), row = from(w.row0) + r;
+        const int r = quotient(pair, a.by_group), head = kvh * a.group + remainder(pair, r, a.by_group), row = row0 + r;
         *reinterpret_cast<u32x2*>(at(a.out, row, head) + e * 8) = u32x2{M::pack(o[0] * inv, o[1] * inv), M::pack(o[2] * inv, o[3] * inv)};
         if (a.lse && e == 0)
           a.lse[(int64_t)head * a.batch.rows + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -852,6 +977,10 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
     slots += __builtin_amdgcn_readlane(upto, 63);
   }
 }
+
+// Sequences that every wavefront adds up by itself (four steps of 64; 256
+// sequences of 300 keys run at the rate of 64); more have a plan.
+constexpr int kMaxAlone = 256;
 
 // Tiles of QP pairs that the rows can make, and whether a sequence can have
 // more than one share.
@@ -880,10 +1009,18 @@ int64_t max_slots(const KvAttnArgs& a, int qp) {
 template <int HD, int QP, class M, int DT>
 hipError_t launch_pairs(KvAttnArgs a, hipStream_t st) {
   a.slots = (int)max_slots(a, QP);
+  a.plan = nullptr;
+  if (a.batch.n_seqs > kMaxAlone)
+    a.plan = reinterpret_cast<int*>(static_cast<char*>(a.work) + align256((size_t)a.slots * kRecord<HD, QP> * sizeof(float)));
   const int64_t items = max_tiles(a, QP) + (may_split(a) ? kShares / a.cache.n_kv + 1 : 0);   // of a key head
   const int64_t most = std::max((1 << 20) / a.cache.n_kv, 1);
   const unsigned grid = (unsigned)(std::min(items, most) * a.cache.n_kv);
   constexpr int KEYS = QP >= 64 ? kStageKeys : kFewKeys;
+  if (a.plan) {
+    k_kv_plan<QP, KEYS><<<1, 1024, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if constexpr (QP == 128) k_kv_attn<HD, 2, 1, M, DT><<<grid, 256, 0, st>>>(a);
   else if constexpr (QP == 64) k_kv_attn<HD, 1, 2, M, DT><<<grid, 512, 0, st>>>(a);
   else k_kv_few<HD, QP / 16, M, DT><<<grid, 256, 0, st>>>(a);
@@ -915,7 +1052,8 @@ hipError_t launch_hd(int cache_dtype, const KvAttnArgs& a, int max_seq_rows, hip
 
 size_t kv_attn_workspace(const KvAttnArgs& a, int head_dim, int max_seq_rows) {
   const int qp = tile_pairs(a, max_seq_rows);
-  return std::max<size_t>((size_t)max_slots(a, qp) * qp * (head_dim + 2) * sizeof(float), 256);
+  const size_t plan = a.batch.n_seqs > kMaxAlone ? (1 + 3 * (size_t)a.batch.n_seqs) * sizeof(int) : 0;
+  return std::max<size_t>(align256((size_t)max_slots(a, qp) * qp * (head_dim + 2) * sizeof(float)) + plan, 256);
 }
 
 hipError_t launch_kv_attn(int head_dim, int dtype, int cache_dtype, const KvAttnArgs& a, int max_seq_rows, hipStream_t st) {

@@ -67,6 +67,7 @@ struct KvAttnArgs {
   float* lse;                              // [n_heads][rows], may be null
   void* work;
   int slots;                               // records of partial sums in it
+  int* plan;                               // running numbers of large batches in it, or null
 };
 size_t kv_attn_workspace(const KvAttnArgs& a, int head_dim, int max_seq_rows);
 hipError_t launch_kv_attn(int head_dim, int dtype, int cache_dtype, const KvAttnArgs& a, int max_seq_rows, hipStream_t st);
