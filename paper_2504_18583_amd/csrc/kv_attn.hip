@@ -96,18 +96,16 @@ __device__ __forceinline__ int share_of(const KvAttnArgs& a, float stages, int t
   return max(kMinKeys / KEYS, (int)fminf(ceilf(stages * a.cache.n_kv / shares), 1 << 24));
 }
 
-// The same by one wavefront; every wavefront finds the same.
-template <int QP, int KEYS>
-__device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& first, int lane) {
+// Sequences that every wavefront adds up by itself, one to a lane; more have a
+// plan (decode of 300 keys each, 8 key heads x 128, by steps of 64 and with a
+// plan: 256 sequences 86 and 73 us, 4096 5358 and 957).
+constexpr int kMaxAlone = 64;
+
+template <int KEYS>
+__device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& mine) {
   if (a.plan) return a.plan[0];                        // uniform
-  float total = 0.f;
-  int tiles = 0;
-  for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {   // uniform
-    const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
-    total += sum_lanes((float)w.tiles * w.stages);
-    tiles = min(tiles + __builtin_amdgcn_readlane(scan(min(w.tiles, kShares)), 63), kShares);
-  }
-  return share_of<KEYS>(a, total, tiles);
+  const int tiles = __builtin_amdgcn_readlane(scan(min(mine.tiles, kShares)), 63);
+  return share_of<KEYS>(a, sum_lanes((float)mine.tiles * mine.stages), min(tiles, kShares));
 }
 
 // The first sequence whose running number `upto` is past `left`, 64 candidates
@@ -148,7 +146,7 @@ struct Item {
 // Item `left` of a key head: a tile's shares first, then tiles (the last first:
 // they see the most keys), then sequences.
 template <int QP, int KEYS>
-__device__ __forceinline__ Item find_item(const KvAttnArgs& a, const SeqWork& first, int share, int left, int kvh, int lane) {
+__device__ __forceinline__ Item find_item(const KvAttnArgs& a, const SeqWork& own, int share, int left, int kvh, int lane) {
   Item it{};
   if (a.plan) {                                        // uniform
     const Found f = search<QP, KEYS>(a, a.plan + 1, left, lane);
@@ -162,35 +160,25 @@ __device__ __forceinline__ Item find_item(const KvAttnArgs& a, const SeqWork& fi
     it.slot = ((f.seq ? a.plan[a.batch.n_seqs + f.seq] : 0) + mine) * a.cache.n_kv + kvh;
     return it;
   }
-  int slots = 0;
-  for (int s0 = 0; s0 < a.batch.n_seqs; s0 += 64) {
-    const SeqWork w = s0 ? seq_work<QP, KEYS>(a, s0 + lane) : first;
-    const int n = shares_of(w, share), items = w.tiles * n, split = n > 1 ? items : 0;
-    const int upto = scan(items), slots_upto = scan(split);
-    const uint64_t past = __ballot(upto > left);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-      it.w = SeqWork{from(w.row0), from(w.rows), from(w.len), from(w.tiles), from(w.stages)};
-      const int mine = left - (from(upto) - from(items));
-      it.seq = s0 + l;
-      it.splits = from(n);
-      it.tile = it.w.tiles - 1 - mine / it.splits;
-      it.split = mine % it.splits;
-      it.slot = (slots + from(slots_upto) - from(split) + mine) * a.cache.n_kv + kvh;
-      return it;
-    }
-    left -= __builtin_amdgcn_readlane(upto, 63);
-    slots += __builtin_amdgcn_readlane(slots_upto, 63);
-  }
+  const int n = shares_of(own, share), items = own.tiles * n, split = n > 1 ? items : 0;
+  const int upto = scan(items), slots_upto = scan(split);
+  const uint64_t past = __ballot(upto > left);
+  if (!past) return it;
+  const int l = __builtin_ctzll(past);
+  auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+  it.w = SeqWork{from(own.row0), from(own.rows), from(own.len), from(own.tiles), from(own.stages)};
+  const int mine = left - (from(upto) - from(items));
+  it.seq = l;
+  it.splits = from(n);
+  it.tile = it.w.tiles - 1 - mine / it.splits;
+  it.split = mine % it.splits;
+  it.slot = (from(slots_upto) - from(split) + mine) * a.cache.n_kv + kvh;
   return it;
 }
 
 // Running numbers of a large batch, by one workgroup ahead of the others: the
 // length of a share, then up to each sequence its shares, those that leave
-// partial sums, and the pairs of split sequences.  (Every wavefront adding up
-// 4096 sequences by itself took 5.4 ms for 300 keys each, 16 384 workgroups
-// twice 64 loads one after the other.)
+// partial sums, and the pairs of split sequences.
 template <int QP, int KEYS>
 __global__ __launch_bounds__(1024) void k_kv_plan(const KvAttnArgs a) {
   __shared__ float f_sum[16];
@@ -353,12 +341,12 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
   // its pairs (and the block of every stage that it loads), its part of the keys
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, part = __builtin_amdgcn_readfirstlane(tid >> 8);
   const KvBatchView& b = a.batch;
-  const SeqWork first = seq_work<QP, kStageKeys>(a, lane);
-  const int share = share_length<QP, kStageKeys>(a, first, lane);
+  const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, kStageKeys>(a, lane);   // of sequence `lane`
+  const int share = share_length<kStageKeys>(a, own);
   // key heads fastest: with 8 of them each keeps to an XCD and its L2
   const int kvh = blockIdx.x % a.cache.n_kv;
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
-    const Item it = find_item<QP, kStageKeys>(a, first, share, u, kvh, lane);
+    const Item it = find_item<QP, kStageKeys>(a, own, share, u, kvh, lane);
     if (it.splits == 0) return;                        // uniform: past the last item
     if (!it.valid(a)) continue;                        // uniform (row_start does not ascend)
     __syncthreads();                                   // (the item before has read LDS)
@@ -674,11 +662,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, c16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const KvBatchView& b = a.batch;
-  const SeqWork first = seq_work<QP, kFewKeys>(a, lane);
-  const int share = share_length<QP, kFewKeys>(a, first, lane);
+  const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, kFewKeys>(a, lane);     // of sequence `lane`
+  const int share = share_length<kFewKeys>(a, own);
   const int kvh = blockIdx.x % a.cache.n_kv;           // (as k_kv_attn)
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
-    const Item it = find_item<QP, kFewKeys>(a, first, share, u, kvh, lane);
+    const Item it = find_item<QP, kFewKeys>(a, own, share, u, kvh, lane);
     if (it.splits == 0) return;                        // uniform: past the last item
     if (!it.valid(a)) continue;                        // uniform (row_start does not ascend)
     const int n_pairs = it.w.rows * a.group, pair0 = it.tile * QP;
@@ -891,96 +879,77 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
   constexpr int W = HD / 4, TURNS = 64 / W, AT_ONCE = 8;
   const int lane = threadIdx.x & 63, turn = lane / W, e = lane % W;
   const int n_waves = gridDim.x * 4;
-  const SeqWork first = seq_work<QP, KEYS>(a, lane);
-  const int share = share_length<QP, KEYS>(a, first, lane);
+  const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, KEYS>(a, lane);
+  const int share = share_length<KEYS>(a, own);
   int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // pair of all split sequences, key heads fastest
   const int n_seqs = a.batch.n_seqs;
-  int before = 0, slots = 0;
-  for (int s0 = 0; s0 < n_seqs; s0 += a.plan ? n_seqs : 64) {             // uniform
-    SeqWork w = first;
-    int n = 0, upto = 0, items = 0, pairs = 0, pairs_upto = 0, all;
+  const int own_n = shares_of(own, share), items = own_n > 1 ? own.tiles * own_n : 0, upto = scan(items);
+  const int pairs = own_n > 1 ? own.rows * a.group : 0, pairs_upto = scan(pairs);
+  const int all = a.plan ? a.plan[3 * n_seqs] : __builtin_amdgcn_readlane(pairs_upto, 63);   // (of the last sequence)
+  for (; unit < all * a.cache.n_kv; unit += n_waves) { // uniform
+    const int kvh = unit % a.cache.n_kv, left = unit / a.cache.n_kv;
+    int pair, splits, slot0, row0;
     if (a.plan) {
-      all = a.plan[3 * n_seqs];                        // (the last sequence's running number)
+      const Found f = search<QP, KEYS>(a, a.plan + 1 + 2 * n_seqs, left, lane);
+      if (f.seq == n_seqs) continue;
+      pair = left - (f.seq ? a.plan[2 * n_seqs + f.seq] : 0);
+      splits = shares_of(f.w, share);
+      slot0 = (f.seq ? a.plan[n_seqs + f.seq] : 0) + (f.w.tiles - 1 - pair / QP) * splits;
+      row0 = f.w.row0;
+      // (numbers that do not fit together: row_start does not ascend)
+      if (pair < 0 || pair >= f.w.rows * a.group || splits < 2) continue;
     } else {
-      if (s0) w = seq_work<QP, KEYS>(a, s0 + lane);
-      n = shares_of(w, share);
-      items = n > 1 ? w.tiles * n : 0;
-      upto = scan(items);
-      pairs = n > 1 ? w.rows * a.group : 0;
-      pairs_upto = scan(pairs);
-      all = __builtin_amdgcn_readlane(pairs_upto, 63);
+      const int l = __builtin_ctzll(__ballot(pairs_upto > left));
+      auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+      pair = left - (from(pairs_upto) - from(pairs));
+      splits = from(own_n);
+      slot0 = from(upto) - from(items) + (from(own.tiles) - 1 - pair / QP) * splits;
+      row0 = from(own.row0);
     }
-    for (; unit < (before + all) * a.cache.n_kv; unit += n_waves) {
-      const int kvh = unit % a.cache.n_kv, left = unit / a.cache.n_kv - before;
-      int pair, splits, slot0, row0;
-      if (a.plan) {
-        const Found f = search<QP, KEYS>(a, a.plan + 1 + 2 * n_seqs, left, lane);
-        if (f.seq == n_seqs) continue;                 // uniform
-        // (numbers that do not fit together: row_start does not ascend)
-        pair = left - (f.seq ? a.plan[2 * n_seqs + f.seq] : 0);
-        splits = shares_of(f.w, share);
-        slot0 = (f.seq ? a.plan[n_seqs + f.seq] : 0) + (f.w.tiles - 1 - pair / QP) * splits;
-        row0 = f.w.row0;
-        if (pair < 0 || pair >= f.w.rows * a.group || splits < 2) continue;
-      } else {
-        const int l = __builtin_ctzll(__ballot(pairs_upto > left));
-        auto from = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-        pair = left - (from(pairs_upto) - from(pairs));
-        splits = from(n);
-        slot0 = slots + from(upto) - from(items) + (from(w.tiles) - 1 - pair / QP) * splits;
-        row0 = from(w.row0);
-      }
-      const int in_tile = pair % QP;
-      if (slot0 < 0 || (slot0 + splits) * a.cache.n_kv > a.slots) continue;   // (row_start does not ascend)
-      const float* const rec = static_cast<const float*>(a.work) + ((int64_t)slot0 * a.cache.n_kv + kvh) * kRecord<HD, QP>;
-      const int64_t step = (int64_t)a.cache.n_kv * kRecord<HD, QP>;
-      // the group's shares (maxima are finite; past the last one: nothing)
-      float top = -1e30f, sum = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int i0 = turn; i0 < splits + turn; i0 += TURNS * AT_ONCE) {      // uniform
-        f32x4 x[AT_ONCE];
-        float m[AT_ONCE], s[AT_ONCE];
+    const int in_tile = pair % QP;
+    if (slot0 < 0 || (int64_t)(slot0 + splits) * a.cache.n_kv > a.slots) continue;   // (row_start does not ascend)
+    const float* const rec = static_cast<const float*>(a.work) + ((int64_t)slot0 * a.cache.n_kv + kvh) * kRecord<HD, QP>;
+    const int64_t step = (int64_t)a.cache.n_kv * kRecord<HD, QP>;
+    // the group's shares (maxima are finite; past the last one: nothing)
+    float top = -1e30f, sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = turn; i0 < splits + turn; i0 += TURNS * AT_ONCE) {      // uniform
+      f32x4 x[AT_ONCE];
+      float m[AT_ONCE], s[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-          const int i = min(i0 + j * TURNS, splits - 1);
-          x[j] = *reinterpret_cast<const f32x4*>(rec + i * step + in_tile * HD + e * 4);
-          m[j] = rec[i * step + QP * HD + in_tile];
-          s[j] = rec[i * step + QP * HD + QP + in_tile];
-        }
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-          if (i0 + j * TURNS >= splits) continue;
-          const float t = fmaxf(top, m[j]), f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m[j] - t);
-          top = t;
-          sum = sum * f0 + s[j] * f1;
-          o = o * f0 + x[j] * f1;
-        }
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const int i = min(i0 + j * TURNS, splits - 1);
+        x[j] = *reinterpret_cast<const f32x4*>(rec + i * step + in_tile * HD + e * 4);
+        m[j] = rec[i * step + QP * HD + in_tile];
+        s[j] = rec[i * step + QP * HD + QP + in_tile];
       }
 #pragma unroll
-      for (int d = W; d < 64; d *= 2) {                                    // the groups', in a tree
-        const float m2 = __shfl_xor(top, d), s2 = __shfl_xor(sum, d), t = fmaxf(top, m2);
-        const float f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m2 - t);
+      for (int j = 0; j < AT_ONCE; ++j) {
+        if (i0 + j * TURNS >= splits) continue;
+        const float t = fmaxf(top, m[j]), f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m[j] - t);
         top = t;
-        sum = sum * f0 + s2 * f1;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + __shfl_xor(o[j], d) * f1;
-      }
-      if (turn == 0) {
-        const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
-        const int r = quotient(pair, a.by_group), head = kvh * a.group + remainder(pair, r, a.by_group), row = row0 + r;
-        *reinterpret_cast<u32x2*>(at(a.out, row, head) + e * 8) = u32x2{M::pack(o[0] * inv, o[1] * inv), M::pack(o[2] * inv, o[3] * inv)};
-        if (a.lse && e == 0)
-          a.lse[(int64_t)head * a.batch.rows + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        sum = sum * f0 + s[j] * f1;
+        o = o * f0 + x[j] * f1;
       }
     }
-    before += all;
-    slots += __builtin_amdgcn_readlane(upto, 63);
+#pragma unroll
+    for (int d = W; d < 64; d *= 2) {                                    // the groups', in a tree
+      const float m2 = __shfl_xor(top, d), s2 = __shfl_xor(sum, d), t = fmaxf(top, m2);
+      const float f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m2 - t);
+      top = t;
+      sum = sum * f0 + s2 * f1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + __shfl_xor(o[j], d) * f1;
+    }
+    if (turn == 0) {
+      const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
+      const int r = quotient(pair, a.by_group), head = kvh * a.group + remainder(pair, r, a.by_group), row = row0 + r;
+      *reinterpret_cast<u32x2*>(at(a.out, row, head) + e * 8) = u32x2{M::pack(o[0] * inv, o[1] * inv), M::pack(o[2] * inv, o[3] * inv)};
+      if (a.lse && e == 0)
+        a.lse[(int64_t)head * a.batch.rows + row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
   }
 }
-
-// Sequences that every wavefront adds up by itself (four steps of 64; 256
-// sequences of 300 keys run at the rate of 64); more have a plan.
-constexpr int kMaxAlone = 256;
 
 // Tiles of QP pairs that the rows can make, and whether a sequence can have
 // more than one share.
@@ -989,12 +958,25 @@ int64_t max_tiles(const KvAttnArgs& a, int qp) {
 }
 bool may_split(const KvAttnArgs& a) { return a.batch.cap > kMinKeys; }
 
-// Pairs of a workgroup: those of a sequence up to 64 (known, or on average),
-// else 128.
+// Pairs of a workgroup, by those that a sequence has on average (8 key heads x
+// 128, us for 16, 32, 64 and 128 pairs a workgroup):
+//   up to 16 or 32: as few as that (16 sequences of 20 000 keys in e4m3, 4 pairs:
+//     169 with 16, 206 with 64)
+//   up to 64: 64 (32 sequences of 1000 keys, 36 pairs: 42, 35, 28, 40), but 32 for
+//     8 and 4 bits, where each half of a stage's wavefronts widens all of it (of
+//     8000 keys in e4m3: 233, 158, 179, 220)
+//   more: 128 (68 pairs: 137, 98, 75, 57), but 64 where 128 leave much empty (132
+//     pairs: 219, 140, 95, 124)
+// A long chunk beside single tokens counts, where it is known: 1000 single
+// tokens and 2000 rows of one sequence 896, 575, 444, 437; 63 and 1000 405, 254,
+// 185, 222.
 int tile_pairs(const KvAttnArgs& a, int max_seq_rows) {
   const int64_t mean = ((int64_t)a.batch.rows * a.group + a.batch.n_seqs - 1) / a.batch.n_seqs;
-  const int64_t pairs = max_seq_rows > 0 ? std::min((int64_t)max_seq_rows * a.group, mean) : mean;
-  return pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
+  const int64_t most = (int64_t)max_seq_rows * a.group;
+  const int64_t pairs = max_seq_rows > 0 ? std::min(most, mean) : mean;
+  const bool chunk = most >= 4 * mean && most > 64 && 4ll * max_seq_rows >= a.batch.rows;
+  if (pairs <= 64) return chunk ? 64 : pairs <= 16 ? 16 : pairs <= 32 || a.cache.k_scale ? 32 : 64;
+  return pairs <= 192 && (pairs > 128 || chunk) ? 64 : 128;
 }
 
 // Records of partial sums: a sequence of k > 1 shares has k - 1 of them full, so

@@ -19,7 +19,7 @@ __host__ __device__ constexpr int kv_scale_bytes(int dtype, int hd) {
 
 struct KvCacheView {
   char *k, *v;
-  uint8_t *k_scale, *v_scale;
+  uint8_t *k_scale, *v_scale;              // null: elements as they are
   int n_pages, n_kv, page_log2;
 };
 struct KvBatchView {

@@ -34,7 +34,9 @@ pard_status batch_check(const pard_kv_batch* b, const pard_kv_cache* c) {
 }
 
 KvCacheView cache_view(const pard_kv_cache* c) {
-  KvCacheView v{static_cast<char*>(c->k), static_cast<char*>(c->v), c->k_scale, c->v_scale, c->n_pages, c->n_kv_heads, 0};
+  const bool scales = blocked(c->dtype);
+  KvCacheView v{static_cast<char*>(c->k), static_cast<char*>(c->v), scales ? c->k_scale : nullptr, scales ? c->v_scale : nullptr,
+                c->n_pages, c->n_kv_heads, 0};
   while ((1 << v.page_log2) < c->page_size) ++v.page_log2;
   return v;
 }

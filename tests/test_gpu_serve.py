@@ -236,6 +236,19 @@ def test_attention_of_ragged_batches(B, kind, known):
     _check_attn(B, [70], [8000], 16, 4, 2, 64, "bf16", kind, known=known)
 
 
+@pytest.mark.parametrize("rows", [1, 7, 12, 40])
+def test_attention_of_many_sequences_with_long_ones_among_them(B, rows):
+    """More sequences than a wavefront has lanes (their running numbers come from a
+    launch ahead), some of them split: every size of tile."""
+    n = 200
+    long = {3: 9000, 64: 4000, 150: 2500, 199: 7000}
+    for kind in ("bf16", "e4m3"):
+        _check_attn(B, [rows if i % 5 else 0 for i in range(n - 1)] + [rows], [long.get(i, i % 29) for i in range(n)], 16, 8, 2, 64, "bf16", kind,
+                    known=kind == "bf16", lead=3, trail=2)
+    _check_attn(B, [1] * 90 + [rows * 9], [i % 50 for i in range(90)] + [5000], 32, 8, 2, 128, "bf16", "bf16", known=True)
+    _check_attn(B, [rows] * 70, [i % 90 + 3 * 600 * (i == 66) for i in range(70)], 16, 4, 1, 64, "f16", "e2m1", 300, 20)
+
+
 def test_a_wrong_hint_changes_no_result(B):
     """max_seq_rows below and above the truth."""
     g = _gen(1)
