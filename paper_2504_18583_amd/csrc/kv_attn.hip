@@ -31,7 +31,13 @@ using namespace cod;
 
 constexpr int kStageKeys = 64;
 constexpr int kMinKeys = 256;              // keys of a share at least
-constexpr int kShares = 512;               // shares that all stages are cut into, about
+// Shares that all stages are cut into, about: what the chip holds at once, or
+// twice that for the smallest tiles, up to 64 a tile (single tokens of 16 contexts of
+// 20 000 keys, 512 and 1024 shares: e4m3 168 and 154 us, 64 dims in bf16 146 and
+// 128; of one of 131 000 102 and 109; tiles of 32 pairs, 32 sequences of 8000
+// keys in e4m3 192 and 229).
+template <int QP>
+constexpr int kShares = QP == 16 ? 1024 : 512;
 
 // ---- sharing out ------------------------------------------------------------
 
@@ -90,9 +96,10 @@ __device__ __forceinline__ int shares_of(const SeqWork& w, int share) { return (
 // The length of a share from all stages and tiles: kShares of it hold all stages,
 // or half as many where there are so many tiles that only the longest need be
 // cut.  (Up to kShares tiles are counted.)
-template <int KEYS>
+template <int QP, int KEYS>
 __device__ __forceinline__ int share_of(const KvAttnArgs& a, float stages, int tiles) {
-  const float shares = tiles * a.cache.n_kv >= kShares / 2 ? kShares / 2 : kShares;
+  const int all = min(max(64 * min(tiles * a.cache.n_kv, 1024), 512), kShares<QP>);
+  const float shares = tiles * a.cache.n_kv >= all / 2 ? all / 2 : all;
   return max(kMinKeys / KEYS, (int)fminf(ceilf(stages * a.cache.n_kv / shares), 1 << 24));
 }
 
@@ -101,11 +108,11 @@ __device__ __forceinline__ int share_of(const KvAttnArgs& a, float stages, int t
 // plan: 256 sequences 86 and 73 us, 4096 5358 and 957).
 constexpr int kMaxAlone = 64;
 
-template <int KEYS>
+template <int QP, int KEYS>
 __device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& mine) {
   if (a.plan) return a.plan[0];                        // uniform
-  const int tiles = __builtin_amdgcn_readlane(scan(min(mine.tiles, kShares)), 63);
-  return share_of<KEYS>(a, sum_lanes((float)mine.tiles * mine.stages), min(tiles, kShares));
+  const int tiles = __builtin_amdgcn_readlane(scan(min(mine.tiles, kShares<QP>)), 63);
+  return share_of<QP, KEYS>(a, sum_lanes((float)mine.tiles * mine.stages), min(tiles, kShares<QP>));
 }
 
 // The first sequence whose running number `upto` is past `left`, 64 candidates
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(1024) void k_kv_plan(const KvAttnArgs a) {
   for (int s = tid; s < n; s += 1024) {
     const SeqWork w = seq_work<QP, KEYS>(a, s);
     total += (float)w.tiles * w.stages;
-    tiles = min(tiles + w.tiles, kShares);
+    tiles = min(tiles + w.tiles, kShares<QP>);
   }
   total = sum_lanes(total);
   tiles = __builtin_amdgcn_readlane(scan(tiles), 63);
@@ -197,8 +204,8 @@ __global__ __launch_bounds__(1024) void k_kv_plan(const KvAttnArgs a) {
   __syncthreads();
   total = 0.f;
   tiles = 0;
-  for (int w = 0; w < 16; ++w) total += f_sum[w], tiles = min(tiles + n_sum[w], kShares);
-  const int share = share_of<KEYS>(a, total, tiles);
+  for (int w = 0; w < 16; ++w) total += f_sum[w], tiles = min(tiles + n_sum[w], kShares<QP>);
+  const int share = share_of<QP, KEYS>(a, total, tiles);
   if (tid == 0) a.plan[0] = share;
   int before[3] = {};
   for (int s0 = 0; s0 < n; s0 += 1024) {               // uniform
@@ -342,7 +349,7 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, part = __builtin_amdgcn_readfirstlane(tid >> 8);
   const KvBatchView& b = a.batch;
   const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, kStageKeys>(a, lane);   // of sequence `lane`
-  const int share = share_length<kStageKeys>(a, own);
+  const int share = share_length<QP, kStageKeys>(a, own);
   // key heads fastest: with 8 of them each keeps to an XCD and its L2
   const int kvh = blockIdx.x % a.cache.n_kv;
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
@@ -663,7 +670,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const KvBatchView& b = a.batch;
   const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, kFewKeys>(a, lane);     // of sequence `lane`
-  const int share = share_length<kFewKeys>(a, own);
+  const int share = share_length<QP, kFewKeys>(a, own);
   const int kvh = blockIdx.x % a.cache.n_kv;           // (as k_kv_attn)
   for (int u = blockIdx.x / a.cache.n_kv;; u += gridDim.x / a.cache.n_kv) {
     const Item it = find_item<QP, kFewKeys>(a, own, share, u, kvh, lane);
@@ -880,7 +887,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
   const int lane = threadIdx.x & 63, turn = lane / W, e = lane % W;
   const int n_waves = gridDim.x * 4;
   const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, KEYS>(a, lane);
-  const int share = share_length<KEYS>(a, own);
+  const int share = share_length<QP, KEYS>(a, own);
   int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // pair of all split sequences, key heads fastest
   const int n_seqs = a.batch.n_seqs;
   const int own_n = shares_of(own, share), items = own_n > 1 ? own.tiles * own_n : 0, upto = scan(items);
@@ -960,8 +967,8 @@ bool may_split(const KvAttnArgs& a) { return a.batch.cap > kMinKeys; }
 
 // Pairs of a workgroup, by those that a sequence has on average (8 key heads x
 // 128, us for 16, 32, 64 and 128 pairs a workgroup):
-//   up to 16 or 32: as few as that (16 sequences of 20 000 keys in e4m3, 4 pairs:
-//     169 with 16, 206 with 64)
+//   up to 16 or 32: as few as that (16 sequences of 20 000 keys in e2m1, 4 pairs:
+//     81, 121, 157, 208)
 //   up to 64: 64 (32 sequences of 1000 keys, 36 pairs: 42, 35, 28, 40), but 32 for
 //     8 and 4 bits, where each half of a stage's wavefronts widens all of it (of
 //     8000 keys in e4m3: 233, 158, 179, 220)
@@ -985,7 +992,7 @@ int tile_pairs(const KvAttnArgs& a, int max_seq_rows) {
 int64_t max_slots(const KvAttnArgs& a, int qp) {
   if (!may_split(a)) return 0;
   const int64_t shares = (a.batch.cap + kMinKeys - 1) / kMinKeys + 2;
-  return std::min<int64_t>(max_tiles(a, qp) * a.cache.n_kv * shares, 2 * kShares + 2);
+  return std::min<int64_t>(max_tiles(a, qp) * a.cache.n_kv * shares, 2 * (qp == 16 ? kShares<16> : kShares<64>) + 2);
 }
 
 template <int HD, int QP, class M, int DT>
@@ -994,7 +1001,7 @@ hipError_t launch_pairs(KvAttnArgs a, hipStream_t st) {
   a.plan = nullptr;
   if (a.batch.n_seqs > kMaxAlone)
     a.plan = reinterpret_cast<int*>(static_cast<char*>(a.work) + align256((size_t)a.slots * kRecord<HD, QP> * sizeof(float)));
-  const int64_t items = max_tiles(a, QP) + (may_split(a) ? kShares / a.cache.n_kv + 1 : 0);   // of a key head
+  const int64_t items = max_tiles(a, QP) + (may_split(a) ? kShares<QP> / a.cache.n_kv + 1 : 0);   // of a key head
   const int64_t most = std::max((1 << 20) / a.cache.n_kv, 1);
   const unsigned grid = (unsigned)(std::min(items, most) * a.cache.n_kv);
   constexpr int KEYS = QP >= 64 ? kStageKeys : kFewKeys;
