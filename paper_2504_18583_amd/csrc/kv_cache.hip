@@ -2,11 +2,14 @@
 //
 // A lane holds 8 elements of a head (16 bytes of a 16-bit type), so a block of
 // 32, which shares a scale, is four neighbouring lanes: its largest magnitude
-// takes two exchanges within quads of lanes.  A row of the batch is one run of
-// units (head by head, keys then values); a wavefront takes one row, or several
-// where a row has fewer than 64 units.
+// takes two exchanges within quads of lanes.  A wavefront takes one row, or
+// several where a row's keys have fewer than 64 such units; keys and values of
+// a head go together.
 //
-// Bound: memory, each element read once and written once.
+// Bound: memory, each element read once and written once (30 778 rows of 8 heads x
+// 128: into e2m1 34 us, back to bf16 30, 4.7 and 5.3 TB/s; 66 246 rows out of e4m3
+// 83 us, 4.9).  With an address of its own for every unit, not a step from head to
+// head, it was issue: 40, 34 and 98 us, the VALU busy 93, 100 and 69 % of the time.
 #include "serve.h"
 
 #include <algorithm>
@@ -71,16 +74,83 @@ __device__ __forceinline__ void store8(char* row, int64_t at, const Row8& r) {
   }
 }
 
-// The scale byte of a block with this largest magnitude (as bits: an order of
-// floats): the exponent field e + 127 of the smallest 2^e, e >= -126, with
-// largest <= (2 - 2^-FRACTION_GAP..) 2^(e + TOP): a fraction above the type's
-// largest one carries into the exponent.  255: the block is NaN.
+// The scale byte of a block with this largest magnitude (as bits, which are in
+// the order of the floats): e + 127 of the smallest 2^e, e >= -126, that brings
+// it within the type's range, 1.75 2^8 or 1.5 2^2.  A fraction above .75 or .5
+// carries into the exponent.  255: the block is NaN.
 template <int DT>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
-  constexpr uint32_t kCarry = DT == PARD_E4M3 ? 0x1fffffu : 0x3fffffu;   // 448 = 1.75 2^8, 6 = 1.5 2^2
+  constexpr uint32_t kCarry = DT == PARD_E4M3 ? 0x1fffffu : 0x3fffffu;
   constexpr int kTop = DT == PARD_E4M3 ? 8 : 2;
   if (largest >= 0x7f800000u) return 255;
   return (uint32_t)max((int)((largest + kCarry) >> 23) - kTop, 1);
+}
+
+// 8 elements into the cache; the four lanes of a block hold it together.
+template <int DT>
+__device__ __forceinline__ void put(Row8 r, char* held, uint8_t* scale, bool first) {
+  if constexpr (DT == PARD_BF16) {
+    *reinterpret_cast<u32x4*>(held) = pack8<ElemBF16>(r);
+  } else if constexpr (DT == PARD_F16) {
+    *reinterpret_cast<u32x4*>(held) = pack8<ElemF16>(r);
+  } else {
+    uint32_t big = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) big = max(big, __float_as_uint(r.v[i]) & 0x7fffffffu);
+    big = max(big, (uint32_t)__builtin_amdgcn_mov_dpp((int)big, 0xB1, 0xF, 0xF, false));   // quad_perm 1 0 3 2
+    big = max(big, (uint32_t)__builtin_amdgcn_mov_dpp((int)big, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
+    const uint32_t byte = scale_byte<DT>(big);
+    if (first) *scale = (uint8_t)byte;
+    if constexpr (DT == PARD_E4M3) {
+      const float inv = __uint_as_float((254 - min(byte, 253u)) << 23);    // 2^-e: products with it are exact
+      u32x2 w = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        int x = __builtin_amdgcn_cvt_pk_fp8_f32(r.v[4 * i] * inv, r.v[4 * i + 1] * inv, 0, false);
+        x = __builtin_amdgcn_cvt_pk_fp8_f32(r.v[4 * i + 2] * inv, r.v[4 * i + 3] * inv, x, true);
+        w[i] = (uint32_t)x;
+      }
+      *reinterpret_cast<u32x2*>(held) = w;
+    } else {
+      const float f = __uint_as_float(byte << 23);                         // (the conversion divides by it)
+      uint32_t w = 0;
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[0], r.v[1], f, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[2], r.v[3], f, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[4], r.v[5], f, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[6], r.v[7], f, 3);
+      *reinterpret_cast<uint32_t*>(held) = w;
+    }
+  }
+}
+
+// 8 elements of the cache as floats (a scale byte of 0 is 2^-127, 255 NaN: the
+// conversions know both).
+template <int DT>
+__device__ __forceinline__ Row8 get(const char* held, const uint8_t* scale) {
+  Row8 r;
+  if constexpr (DT == PARD_E4M3) {
+    const u32x2 w = *reinterpret_cast<const u32x2*>(held);
+    const float f = __uint_as_float((uint32_t)*scale << 23);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], f, true);
+      r.v[4 * i] = lo[0], r.v[4 * i + 1] = lo[1], r.v[4 * i + 2] = hi[0], r.v[4 * i + 3] = hi[1];
+    }
+  } else if constexpr (DT == PARD_E2M1) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(held);
+    const float f = __uint_as_float((uint32_t)*scale << 23);
+    const f32x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 1);
+    const f32x2 x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 3);
+    r = Row8{{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]}};
+  } else {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(held);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint16_t h = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+      r.v[i] = DT == PARD_BF16 ? ElemBF16::load(h) : ElemF16::load(h);
+    }
+  }
+  return r;
 }
 
 template <int HD, class E, int DT, bool VEC, bool WRITE>
@@ -94,102 +164,57 @@ __global__ __launch_bounds__(256) void k_kv_copy(const KvCopyArgs a) {
     for (int i = threadIdx.x; i <= b.n_seqs; i += 256) starts[i] = b.row_start[i];
     __syncthreads();
   }
-  const int lane = threadIdx.x & 63, units = 2 * a.cache.n_kv * HU;
-  const int per_row = min(units, 64), per_wave = 64 / per_row;            // lanes of a row, rows of a wavefront
+  // lanes of a row (of whole heads), rows of a wavefront; a lane keeps to its
+  // place in a head, and goes from head to head
+  const int lane = threadIdx.x & 63, units = a.cache.n_kv * HU;
+  const int per_row = min(units, 64), per_wave = 64 / per_row;
   const int wave = blockIdx.x * 4 + (threadIdx.x >> 6), n_waves = gridDim.x * 4;
   const int sub = lane / per_row, u0 = lane - sub * per_row;
   if (sub >= per_wave) return;
+  const int unit = u0 % HU, head0 = u0 / HU, heads = per_row / HU;
+  const int64_t next = (int64_t)heads << a.cache.page_log2;               // slots
   for (int64_t r64 = (int64_t)wave * per_wave + sub; r64 < b.rows; r64 += (int64_t)n_waves * per_wave) {
     const int row = (int)r64;
     const int s = in_lds ? kv_seq_of(starts, b.n_seqs, row) : kv_seq_of(b.row_start, b.n_seqs, row);
-    if (s >= b.n_seqs || row < b.row_start[s]) continue;                  // (a row of no sequence)
-    const int pos = b.kv_len[s] - b.row_start[s + 1] + row;
+    if (s >= b.n_seqs) continue;                      // (a row of no sequence)
+    const int first = in_lds ? starts[s] : b.row_start[s], end = in_lds ? starts[s + 1] : b.row_start[s + 1];
+    if (row < first) continue;
+    const int pos = b.kv_len[s] - end + row;
     const int page = pos < 0 ? -1 : kv_page(a.cache, b, s, pos);
     if (WRITE && page < 0) continue;
-    const int place = pos & ((1 << a.cache.page_log2) - 1);
+    const int64_t slot = (((int64_t)max(page, 0) * a.cache.n_kv + head0) << a.cache.page_log2) + (pos & ((1 << a.cache.page_log2) - 1));
+    char *kh = a.cache.k + slot * RB + unit * (RB / HU), *vh = a.cache.v + slot * RB + unit * (RB / HU);
+    uint8_t *ks = SB ? a.cache.k_scale + slot * SB + unit / 4 : nullptr, *vs = SB ? a.cache.v_scale + slot * SB + unit / 4 : nullptr;
+    int64_t ka = row * a.k.rs + head0 * a.k.hs + unit * 8, va = row * a.v.rs + head0 * a.v.hs + unit * 8;
     for (int u = u0; u < units; u += per_row) {
-      const bool is_v = u >= units / 2;
-      const int head = (is_v ? u - units / 2 : u) / HU, unit = u % HU;
-      const Heads& rows = is_v ? a.v : a.k;
-      char* const data = rows.data;
-      const int64_t at = row * rows.rs + head * rows.hs + unit * 8;
-      const int64_t slot = (((int64_t)max(page, 0) * a.cache.n_kv + head) << a.cache.page_log2) + place;
-      char* const held = (is_v ? a.cache.v : a.cache.k) + slot * RB + unit * (RB / HU);
-      uint8_t* const scale = SB ? (is_v ? a.cache.v_scale : a.cache.k_scale) + slot * SB + unit / 4 : nullptr;
       if constexpr (WRITE) {
-        Row8 r = load8<E, VEC>(data, at);
-        if constexpr (SB) {
-          uint32_t big = 0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) big = max(big, __float_as_uint(r.v[i]) & 0x7fffffffu);
-          big = max(big, (uint32_t)__builtin_amdgcn_mov_dpp((int)big, 0xB1, 0xF, 0xF, false));   // quad_perm 1 0 3 2
-          big = max(big, (uint32_t)__builtin_amdgcn_mov_dpp((int)big, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
-          const uint32_t byte = scale_byte<DT>(big);
-          if (unit % 4 == 0) *scale = (uint8_t)byte;
-          const float inv = __uint_as_float((254 - min(byte, 253u)) << 23);    // 2^-e: products with it are exact
-#pragma unroll
-          for (int i = 0; i < 8; ++i) r.v[i] *= inv;
-          if constexpr (DT == PARD_E4M3) {
-            u32x2 w = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              int x = __builtin_amdgcn_cvt_pk_fp8_f32(r.v[4 * i], r.v[4 * i + 1], 0, false);
-              x = __builtin_amdgcn_cvt_pk_fp8_f32(r.v[4 * i + 2], r.v[4 * i + 3], x, true);
-              w[i] = (uint32_t)x;
-            }
-            *reinterpret_cast<u32x2*>(held) = w;
-          } else {
-            uint32_t w = 0;
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[0], r.v[1], 1.f, 0);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[2], r.v[3], 1.f, 1);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[4], r.v[5], 1.f, 2);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, r.v[6], r.v[7], 1.f, 3);
-            *reinterpret_cast<uint32_t*>(held) = w;
-          }
-        } else if constexpr (DT == PARD_BF16) {
-          *reinterpret_cast<u32x4*>(held) = pack8<ElemBF16>(r);
-        } else {
-          *reinterpret_cast<u32x4*>(held) = pack8<ElemF16>(r);
-        }
+        const Row8 k = load8<E, VEC>(a.k.data, ka), v = load8<E, VEC>(a.v.data, va);
+        put<DT>(k, kh, ks, unit % 4 == 0);
+        put<DT>(v, vh, vs, unit % 4 == 0);
       } else {
-        Row8 r;
-        if (page < 0) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) r.v[i] = __uint_as_float(0x7fc00000u);
-        } else if constexpr (SB) {
-          const uint32_t byte = *scale;
-          const float f = __uint_as_float(byte == 0 ? 0x400000u : byte == 255 ? 0x7fc00000u : byte << 23);
-          if constexpr (DT == PARD_E4M3) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(held);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false);
-              const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-              r.v[4 * i] = lo[0] * f, r.v[4 * i + 1] = lo[1] * f, r.v[4 * i + 2] = hi[0] * f, r.v[4 * i + 3] = hi[1] * f;
-            }
-          } else {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(held);
-            const f32x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
-            const f32x2 x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
-            r = Row8{{x0[0] * f, x0[1] * f, x1[0] * f, x1[1] * f, x2[0] * f, x2[1] * f, x3[0] * f, x3[1] * f}};
-          }
+        Row8 k, v;
+        if (page >= 0) {
+          k = get<DT>(kh, ks);
+          v = get<DT>(vh, vs);
         } else {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(held);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint16_t h = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-            r.v[i] = DT == PARD_BF16 ? ElemBF16::load(h) : ElemF16::load(h);
-          }
+          for (int i = 0; i < 8; ++i) k.v[i] = v.v[i] = __uint_as_float(0x7fc00000u);
         }
-        store8<E, VEC>(data, at, r);
+        store8<E, VEC>(a.k.data, ka, k);
+        store8<E, VEC>(a.v.data, va, v);
       }
+      kh += next * RB;
+      vh += next * RB;
+      if (SB) ks += next * SB, vs += next * SB;
+      ka += heads * a.k.hs;
+      va += heads * a.v.hs;
     }
   }
 }
 
 template <int HD, class E, int DT, bool VEC>
 hipError_t launch_dir(bool write, const KvCopyArgs& a, hipStream_t st) {
-  const int units = 2 * a.cache.n_kv * (HD / 8), per_wave = 64 / std::min(units, 64);
+  const int units = a.cache.n_kv * (HD / 8), per_wave = 64 / std::min(units, 64);
   const int64_t waves = ((int64_t)a.batch.rows + per_wave - 1) / per_wave;
   const unsigned grid = (unsigned)std::min<int64_t>((waves + 3) / 4, 1 << 16);
   if (write) k_kv_copy<HD, E, DT, VEC, true><<<grid, 256, 0, st>>>(a);
