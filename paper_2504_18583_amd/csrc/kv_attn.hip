@@ -1,22 +1,31 @@
 // Attention of a batch's new rows over a paged cache, on gfx950 MFMA.
 //
 // A sequence's rows and query heads of one key head are its pairs (row by row).
-// A workgroup of four wavefronts owns 64 NQ of them, a wavefront 16 NQ, and
-// walks the keys that its rows see in stages of 64 through two LDS buffers, the
-// next stage in flight during the current one.  With a window the stages cover
-// the first tokens, then the keys from the first row's window on; only stages
-// that some row does not see whole compare keys with rows.  A tile is S^T = K
-// Q^T, online softmax in base 2, O^T += V^T P^T (softmax_step).
-//   * 16 bits: LDS-DMA, 16 keys to a wavefront; pages have 16 keys or more, so
-//     such a block lies in one page, whose table entry is read a stage ahead.
-//   * 8 and 4 bits: bytes and scales into registers, widened into LDS at the end
-//     of the stage (v_cvt_scalef32_*: exact in bfloat16), so that everything
-//     behind is the same.
+// A workgroup owns a tile of them and one share of the keys that its rows see;
+// with a window these are the first tokens, then the keys from the first row's
+// window on.  Only steps that some row does not see whole compare keys with rows.
+// A tile of the products is S^T = K Q^T, online softmax in base 2, O^T += V^T P^T
+// (softmax_step).  Which of two kernels runs, and how many pairs a tile has,
+// follows from the pairs of a sequence (tile_pairs):
+//   k_kv_few   16 or 32 pairs: every wavefront has all of them and a quarter of
+//              the keys
+//   k_kv_attn  64 or 128 pairs: the wavefronts share stages of 64 keys in LDS
 // Work is shared out on the device, from lengths that only the device knows:
-// every wavefront adds up the batch's stages (64 sequences at a step), finds
-// the length of a share, and from the running number of shares the one that is
-// its workgroup's (plan()).  Sequences of more than one share leave partial
-// sums, which a second launch joins in the order of the keys.
+// from all sequences' stages follows the length of a share, and from the running
+// number of shares the one that is a workgroup's.  Sequences of more than one
+// share leave partial sums, which a last launch joins in the order of the keys.
+//
+// Bound.  Single tokens: memory (16 contexts of 8000 to 32 000 keys, 32 / 8 heads x
+// 128: 255 us in bf16, 5.4 TB/s; 155 in e4m3, 4.6; 88 in e2m1, 4.1).  Verify
+// passes: memory behind a chain of dependent reads (lengths, table, keys: 5 us of
+// a workgroup's life) and the join (32 sequences of 512 to 1536 keys, 9 rows: 32
+// us for 136 MB and 5 for the join).  Chunks: the SIMDs' issue (4096 rows at 4096,
+// 32 / 8 heads x 128: 425 us, 970 TFLOP/s in bf16 and e4m3; x 64: 260 and 267 us in e2m1,
+// 790; two chunks of 3641 and 2606 rows 860 us: products 43 % of the SIMDs'
+// cycles, other instructions 45 %).  Within a window of 1024 a tile sees 18 stages,
+// of which four compare, and a row of 150 makes 4.7 tiles: products 24 %, others 58.
+// A wavefront per row and head, key by key, took 23.9 ms for the contexts in e4m3
+// and 139 for the chunks.
 #include "serve.h"
 
 #include <algorithm>
@@ -313,6 +322,14 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// Zeros in the place of 16 keys without a page.
+template <int HD>
+__device__ __forceinline__ void clear_block(u32x4* block, int lane) {
+#pragma unroll
+  for (int i = 0; i < kBlockUnits<HD>; i += 64) block[i + lane] = u32x4{0, 0, 0, 0};
+  asm volatile("" ::: "memory");
+}
+
 // Everyone's LDS accesses are done; loads stay in flight.
 __device__ __forceinline__ void meet_with_loads() {
   __builtin_amdgcn_s_waitcnt(0xc07f);                  // lgkmcnt(0)
@@ -330,7 +347,18 @@ constexpr int kRecord = QP * (HD + 2);
 template <int HD, int NQ, int DT>
 constexpr int kResident = NQ == 1 ? 4 : HD == 128 ? 2 : kv_scale_bytes(DT, HD) ? 3 : 4;
 
-// KH: wavefronts that share 16 NQ pairs, each with its part of a stage's keys.
+// Many pairs: 64 NQ to a workgroup.  A stage of 64 keys lies in one of two LDS
+// buffers, the next one in flight during the current one.
+//   * 16 bits: LDS-DMA, 16 keys to a wavefront; pages have 16 keys or more, so
+//     such a block lies in one page, whose table entry is read two stages ahead.
+//   * 8 and 4 bits: bytes and scales into registers, two stages ahead, widened into
+//     LDS at the end of a stage (v_cvt_scalef32_*), so that everything behind is
+//     the same.
+// KH wavefronts share 16 NQ pairs, each with its part of a stage's keys: with one
+// tile of pairs (NQ 1) a stage's dependent steps, not its bytes, were the time, and
+// two half as long ones run beside each other (verify pass of 32 sequences 40 and 33 us,
+// before the join).  Three stages ahead in one workgroup a CU (four buffers) took
+// 39, and two workgroups with two buffers 33.
 template <int HD, int NQ, int KH, class M, int DT>
 __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(const KvAttnArgs a) {
   constexpr int QW = 16 * NQ, QP = 4 * QW;             // pairs of a wavefront, of the workgroup
@@ -390,7 +418,8 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
     auto load = [&](Parts& p, u32x4* buf, int st, int entry) __attribute__((always_inline)) {
       const Block k = block_of(st);
       int page = __builtin_amdgcn_readfirstlane(entry);
-      if ((uint32_t)page >= (uint32_t)a.cache.n_pages) {  // uniform
+      const bool none = (uint32_t)page >= (uint32_t)a.cache.n_pages;         // uniform
+      if (none) {
         page = 0;
         if (lane == 0) any_bad = 1;
       }
@@ -403,6 +432,15 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
         const char* const src = (is_v ? a.cache.v : a.cache.k) + slot * RB;
         if constexpr (SB) p.x[i].load(src, (is_v ? a.cache.v_scale : a.cache.k_scale) + slot * SB, g4);
         else load_block<HD>(src + block_byte(lane), buf + (4 * is_v + wave) * BU);
+      }
+      if (none) {                                      // (what page 0 holds reaches nobody)
+        if constexpr (SB) {
+          p = Parts{};
+        } else {
+          wait_loads<0>();
+#pragma unroll
+          for (int i = 0; i < 2 / KH; ++i) clear_block<HD>(buf + (4 * (KH == 2 ? part : i) + wave) * BU, lane);
+        }
       }
     };
     auto widen = [&](const Parts& p, u32x4* buf) __attribute__((always_inline)) {
@@ -602,7 +640,9 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
 // until the end.  K goes straight into operand registers (8 and 4 bits:
 // a lane's 16 bytes are elements next to each other, and Q's are put in the same
 // order), V through the wavefront's own LDS, which transposes it; the next tile
-// is in flight during the current one.
+// is in flight during the current one.  (16 contexts in e4m3 with the wavefronts
+// around shared stages: 206 us against 169 then.)  Four tiles of 16 pairs (NT 4)
+// need 500 registers and took 76 us for the 32 sequences' verify pass.
 constexpr int kFewKeys = 128;
 
 // K of a block of 16 keys as operands: of step s, lane (c16, g4) holds key c16's
@@ -726,6 +766,15 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
           const int64_t base = ((int64_t)page * a.cache.n_kv + kvh) << a.cache.page_log2;
           const int place = max(min(k.key + 16 * i + block_row(lane), k.high), k.low) & ((1 << a.cache.page_log2) - 1);
           load_block<HD>(a.cache.v + (base + place) * RB + block_byte(lane), vbuf + (wave * 2 + i) * BU);
+        }
+      }
+      if (d.none[0] || d.none[1]) {                    // uniform (what page 0 holds reaches nobody)
+        if constexpr (!SB) wait_loads<0>();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (!d.none[i]) continue;
+          if constexpr (SB) d.v[i] = Staged<HD, M, DT>{};
+          else clear_block<HD>(vbuf + (wave * 2 + i) * BU, lane);
         }
       }
     };

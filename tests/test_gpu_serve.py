@@ -297,6 +297,33 @@ def test_rows_that_see_nothing_and_positions_without_a_page(B, kind, rows):
     assert out.cpu()[bad].isnan().all() and out.cpu()[~bad].isfinite().all()
 
 
+@pytest.mark.parametrize("rows", [1, 5, 9, 40])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_what_a_missing_page_is_replaced_by_reaches_nobody(B, hd, kind, rows):
+    """Pages that are no sequence's hold NaN; a row before the missing page, or
+    behind it with a window, is what it is with the page there."""
+    g = _gen(rows + hd)
+    hq, hk, page = 8, 2, 16
+    c = _cache(B, 20, page, hk, hd, kind)            # all NaN
+    table = torch.arange(1, 20, dtype=torch.int32)[None].contiguous().cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    x = _randn(g, 200, hk, hd, dtype=torch.bfloat16)
+    B.kv_write(x, x, c, B.KVBatch(table, i32(0, 200), i32(200)))
+    broken = table.clone()
+    broken[0, 5] = 77                                # positions 80 .. 95
+    say(f"[gpu] a missing page {kind} {hd} {rows}")
+    for last in (78 + rows, 83, 95, 100, 119, 160):
+        q = _randn(g, rows, hq, hd, dtype=torch.bfloat16)
+        pos = last - rows + torch.arange(rows)
+        for window, sinks in ((0, 0), (20, 4), (20, 83)):
+            want = B.kv_attn(q, c, B.KVBatch(table, i32(0, rows), i32(last)), window=window, sinks=sinks)
+            got = B.kv_attn(q, c, B.KVBatch(broken, i32(0, rows), i32(last)), window=window, sinks=sinks)
+            bad = (pos >= 80) & ((pos < 95 + window) | (window == 0) | (sinks > 80))
+            assert want[0].isfinite().all() and got[0][bad].isnan().all() and got[1][:, bad].isnan().all()
+            assert torch.equal(got[0][~bad], want[0][~bad]) and torch.equal(got[1][:, ~bad], want[1][:, ~bad]), (last, window, sinks)
+
+
 def test_attention_strides_and_optional_outputs(B):
     g = _gen(8)
     batch = S.Batch([1, 20], [40, 3], 16, lead=1, trail=1)
