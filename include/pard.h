@@ -570,8 +570,8 @@ pard_status pard_cod_loss(const pard_cod_loss_args *args, void *workspace, size_
  *              1.5, 2, 3, 4, 6 and their negatives
  * k_scale, v_scale (these types only; 4-byte aligned): [n_pages][n_kv_heads]
  * [page_size][head_dim / 32] bytes: byte b is the scale 2^(b - 127); 255 makes
- * the block NaN.  An element's value is exact in bfloat16 and float32 (where
- * scales are at least 2^-117), and in float16 within its range. */
+ * the block NaN.  Values are exact in float32 and bfloat16 down to its smallest
+ * subnormal, and in float16 within its range. */
 enum { PARD_E4M3 = 3, PARD_E2M1 = 4 };
 typedef struct {
   int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;
@@ -583,8 +583,8 @@ typedef struct {
  * row_start[s + 1] - 1 are sequence s's new rows (none: it takes no part), the
  * last of its kv_len[s] positions: row r is at position kv_len[s] -
  * row_start[s + 1] + r.  Position p lies in page page_table[s][p / page_size].
- * row_start ascends from 0 or more to at most rows; rows before row_start[0] and from
- * row_start[n_seqs] on belong to no sequence and are left as they are.
+ * row_start ascends from 0 or more to at most rows; rows before row_start[0] and
+ * from row_start[n_seqs] on belong to no sequence and are left as they are.
  * max_seq_rows: the most rows of a sequence where the caller knows it (0: not
  * known); it helps to choose kernels, and no result needs it to be right. */
 typedef struct {
@@ -599,18 +599,18 @@ typedef struct {
  * PARD_F32, PARD_BF16 or PARD_F16) into their places in the cache, rounded to
  * the nearest (ties to even) of its type.  A block of 32 elements takes the
  * smallest scale 2^e, e >= -126, that brings it within the type's range (448 or
- * 6: nothing saturates, and what is rounded does not depend on the elements'
- * order); a block that holds a NaN or an infinity becomes NaN.  A row whose position
- * is negative or has no page (past max_pages, or an entry outside [0, n_pages))
- * is not written.  Two rows in one place: either.
+ * 6: nothing saturates); a block that holds a NaN or an infinity becomes NaN.  A
+ * row whose position is negative or has no page (past max_pages, or an entry
+ * outside [0, n_pages)) is not written.  Two rows in one place: either.
  * pard_kv_read reads the rows' places back (a row without a place: NaN): with
  * row_start covering whole sequences, all of them.  Values are rounded to dtype.
  * Vectorised where the rows' data and strides are multiples of 16 bytes.
- * Errors: ARG (null pointer, sizes below 1, rows or max_seq_rows negative, page_size not a
- * power of two in [16, 4096], misaligned cache or scales, strides negative, overlapping
- * heads of an output), UNSUPPORTED (a dtype, head_dim not 64 or 128, 2^30 rows
- * or more, above 65535 heads or 2^20 sequences, max_pages * page_size above
- * 2^30), DEVICE. */
+ * Errors: ARG (null pointer, sizes below 1, rows or max_seq_rows negative,
+ * page_size not a power of two in [16, 4096], misaligned cache or scales, strides
+ * negative, overlapping heads of an output, an output that starts where the other
+ * or the cache does), UNSUPPORTED (a dtype, head_dim not 64 or 128, 2^30 rows or
+ * more, above 65535 heads or 2^20 sequences, max_pages * page_size above 2^30),
+ * DEVICE. */
 pard_status pard_kv_write(const pard_kv_cache *cache, const pard_kv_batch *batch, int32_t dtype, const pard_heads *k,
                           const pard_heads *v, void *hip_stream);
 pard_status pard_kv_read(const pard_kv_cache *cache, const pard_kv_batch *batch, int32_t dtype, const pard_heads *k,
@@ -626,10 +626,10 @@ pard_status pard_kv_read(const pard_kv_cache *cache, const pard_kv_batch *batch,
  * A row that sees nothing (a negative position) gets out = 0 and lse = -inf.  A
  * row that would see a position without a page gets NaN.  Pages that no row of
  * the sequence sees into are not used, their entries may hold anything, and
- * positions that no row sees may hold anything.  (A NaN or an infinity that one row sees may
- * reach any row of its sequence.)  Scores, softmax and sums are float32 (scores
- * within +-1e30); cached values and probabilities are rounded to dtype for the
- * products.  Results are deterministic; how sums are split depends on the
+ * positions that no row sees may hold anything.  (A NaN or an infinity that one
+ * row sees may reach any row of its sequence.)  Scores, softmax and sums are
+ * float32 (scores within +-1e30); cached values and probabilities are rounded to
+ * dtype for the products.  Results are deterministic; how sums are split depends on the
  * batch.  No output may overlap an input.
  * Errors: as pard_kv_write for the cache and the batch; ARG (null pointer,
  * n_heads not a multiple of n_kv_heads, scale not finite, window or sinks
@@ -659,18 +659,20 @@ pard_status pard_kv_attn(const pard_kv_attn_args *args, const pard_heads *q, con
  *   y += bias_values[i] for i in bias_start[s] .. bias_start[s + 1] - 1 with
  *        bias_ids[i] = id (the last one, if there are several)
  *   y = -inf where bit id % 32 of word id / 32 of row mask_row[r] of the mask
- *       is 0 (mask_row null: row r; negative: no mask; n_masks or more: all)
+ *       is 0 (mask_row null: row r; negative: no mask; n_masks or more: no
+ *       id is allowed)
  * out = y rounded to dtype; best[r] = the lowest id of the largest y in out (NaN
- * is passed over; -1 if none is above -inf).  Every step may be left out (null): tokens (with
- * row_len and prompt_len), repetition, presence, frequency (these need tokens), bias_start, mask,
- * best.  prompt_len null: 0.  Ids outside [0, vocab) count for nothing; lengths
+ * is passed over; -1 if none is above -inf).  Every step may be left out (null):
+ * tokens (with row_len), repetition, presence, frequency (these need tokens),
+ * bias_start, mask, best.  prompt_len null: 0.  Ids outside [0, vocab) count for nothing; lengths
  * are cut to [0, tokens_stride], bias_start to [0, n_bias]; a row whose sequence
  * is outside [0, n_seqs) has no history and no biases.  out may be logits itself
  * (same stride), but may not overlap it otherwise.  Deterministic.
- * Errors: ARG (null pointer, rows < 0, vocab < 1, n_seqs < 1, row_seq null with fewer sequences
- * than rows, strides below vocab / the mask's words, counts negative, out at
- * logits with another stride, misaligned elements), UNSUPPORTED (dtype, 2^30
- * rows or a vocab above 2^28), NOMEM (workspace too small; only best needs one), DEVICE. */
+ * Errors: ARG (null pointer, rows < 0, vocab < 1, n_seqs < 1, row_seq null with
+ * fewer sequences than rows, strides below vocab / the mask's words, counts
+ * negative, out at logits with another stride, misaligned elements), UNSUPPORTED
+ * (dtype, 2^30 rows or more, a vocab above 2^28), NOMEM (workspace too small; only
+ * best needs one), DEVICE. */
 typedef struct {
   int64_t rows;
   int32_t vocab, dtype, n_seqs;

@@ -330,7 +330,7 @@ def _heads(t, what: str, like=None, shape=None) -> pard_heads:
 
 
 def _vector(t, what: str, n: int, dtype, device) -> int:
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != (n,) or not t.is_contiguous():
+    if t.dtype != dtype or t.device != device or t.shape != (n,) or not t.is_contiguous():
         _bad(f"{what}: a contiguous {dtype} tensor of {n} on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
