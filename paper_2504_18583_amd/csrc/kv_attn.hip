@@ -927,22 +927,25 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
   }
 }
 
-// Joins the shares of split sequences: a wavefront per pair; 16 (32) lanes hold
-// its 64 (128) elements, and the four (two) groups of lanes take turns with the
-// shares.
-template <int HD, int QP, int KEYS, class M>
+// Joins the shares of split sequences: NW wavefronts per pair; 16 (32) lanes hold
+// its 64 (128) elements, and a wavefront's four (two) groups of lanes take turns
+// with the shares.
+template <int HD, int QP, int KEYS, int NW, class M>
 __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
-  constexpr int W = HD / 4, TURNS = 64 / W, AT_ONCE = 8;
-  const int lane = threadIdx.x & 63, turn = lane / W, e = lane % W;
-  const int n_waves = gridDim.x * 4;
+  constexpr int W = HD / 4, GROUPS = 64 / W, TURNS = GROUPS * NW, AT_ONCE = NW == 1 ? 8 : 4;
+  __shared__ f32x4 o_s[NW][W];
+  __shared__ float m_s[NW], l_s[NW];
+  const int lane = threadIdx.x & 63, e = lane % W, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int turn = (NW == 1 ? 0 : wave * GROUPS) + lane / W;
+  const int n_units = gridDim.x * (4 / NW);            // at once
   const SeqWork own = a.plan ? SeqWork{} : seq_work<QP, KEYS>(a, lane);
   const int share = share_length<QP, KEYS>(a, own);
-  int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // pair of all split sequences, key heads fastest
+  int unit = blockIdx.x * (4 / NW) + (NW == 1 ? wave : 0);               // pair of all split sequences, key heads fastest
   const int n_seqs = a.batch.n_seqs;
   const int own_n = shares_of(own, share), items = own_n > 1 ? own.tiles * own_n : 0, upto = scan(items);
   const int pairs = own_n > 1 ? own.rows * a.group : 0, pairs_upto = scan(pairs);
   const int all = a.plan ? a.plan[3 * n_seqs] : __builtin_amdgcn_readlane(pairs_upto, 63);   // (of the last sequence)
-  for (; unit < all * a.cache.n_kv; unit += n_waves) { // uniform
+  for (; unit < all * a.cache.n_kv; unit += n_units) { // uniform
     const int kvh = unit % a.cache.n_kv, left = unit / a.cache.n_kv;
     int pair, splits, slot0, row0;
     if (a.plan) {
@@ -969,7 +972,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
     // the group's shares (maxima are finite; past the last one: nothing)
     float top = -1e30f, sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = turn; i0 < splits + turn; i0 += TURNS * AT_ONCE) {      // uniform
+    for (int i0 = turn; i0 < splits + turn; i0 += TURNS * AT_ONCE) {      // uniform by wavefront
       f32x4 x[AT_ONCE];
       float m[AT_ONCE], s[AT_ONCE];
 #pragma unroll
@@ -996,6 +999,24 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvAttnArgs a) {
       sum = sum * f0 + s2 * f1;
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + __shfl_xor(o[j], d) * f1;
+    }
+    if constexpr (NW > 1) {                            // the wavefronts', in order
+      if (lane < W) {
+        o_s[wave][e] = o;
+        if (e == 0) m_s[wave] = top, l_s[wave] = sum;
+      }
+      __syncthreads();
+      for (int w = 0; w < NW; ++w) {
+        if (w == 0) {
+          top = m_s[0], sum = l_s[0], o = o_s[0][e];
+        } else {
+          const float t = fmaxf(top, m_s[w]), f0 = __builtin_amdgcn_exp2f(top - t), f1 = __builtin_amdgcn_exp2f(m_s[w] - t);
+          top = t;
+          sum = sum * f0 + l_s[w] * f1;
+          o = o * f0 + o_s[w][e] * f1;
+        }
+      }
+      __syncthreads();
     }
     if (turn == 0) {
       const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
@@ -1064,8 +1085,11 @@ hipError_t launch_pairs(KvAttnArgs a, hipStream_t st) {
   else k_kv_few<HD, QP / 16, M, DT><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !may_split(a)) return e;
-  const int64_t waves = (int64_t)a.batch.rows * a.n_heads;
-  k_kv_join<HD, QP, KEYS, M><<<(unsigned)std::min<int64_t>((waves + 3) / 4, 2048), 256, 0, st>>>(a);
+  // few pairs: a workgroup each (9 rows of 32 heads over 16 384 keys, 52 shares: 7.5 us by
+  // wavefronts, 4.7 by workgroups)
+  const int64_t pairs = (int64_t)a.batch.rows * a.n_heads;
+  if (pairs <= 1024) k_kv_join<HD, QP, KEYS, 4, M><<<(unsigned)pairs, 256, 0, st>>>(a);
+  else k_kv_join<HD, QP, KEYS, 1, M><<<(unsigned)std::min<int64_t>((pairs + 3) / 4, 2048), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
