@@ -1040,8 +1040,8 @@ bool may_split(const KvAttnArgs& a) { return a.batch.cap > kMinKeys; }
 //   up to 16 or 32: as few as that (16 sequences of 20 000 keys in e2m1, 4 pairs:
 //     81, 121, 157, 208)
 //   up to 64: 64 (32 sequences of 1000 keys, 36 pairs: 42, 35, 28, 40), but 32 for
-//     8 and 4 bits, where each half of a stage's wavefronts widens all of it (of
-//     8000 keys in e4m3: 233, 158, 179, 220)
+//     8 and 4 bits, where a wavefront of k_kv_few widens its own keys and waits for
+//     nobody's (of 8000 keys in e4m3: 233, 158, 179, 220)
 //   more: 128 (68 pairs: 137, 98, 75, 57), but 64 where 128 leave much empty (132
 //     pairs: 219, 140, 95, 124)
 // A long chunk beside single tokens counts, where it is known: 1000 single
