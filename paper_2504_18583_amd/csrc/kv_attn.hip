@@ -1041,7 +1041,8 @@ bool may_split(const KvAttnArgs& a) { return a.batch.cap > kMinKeys; }
 //     81, 121, 157, 208)
 //   up to 64: 64 (32 sequences of 1000 keys, 36 pairs: 42, 35, 28, 40), but 32 for
 //     8 and 4 bits, where a wavefront of k_kv_few widens its own keys and waits for
-//     nobody's (of 8000 keys in e4m3: 233, 158, 179, 220)
+//     nobody's (of 8000 keys in e4m3: 233, 158, 179, 220; with 2 key heads x 64 and
+//     pages of 16 in any order 39 with 32 and 51 with 64, in a row 40 and 36)
 //   more: 128 (68 pairs: 137, 98, 75, 57), but 64 where 128 leave much empty (132
 //     pairs: 219, 140, 95, 124)
 // A long chunk beside single tokens counts, where it is known: 1000 single
