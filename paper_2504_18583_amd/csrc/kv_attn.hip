@@ -125,7 +125,7 @@ __device__ __forceinline__ int share_length(const KvAttnArgs& a, const SeqWork& 
 }
 
 // The first sequence whose running number `upto` is past `left`, 64 candidates
-// at a time (n_seqs: none); its work in every lane, and the numbers up to it.
+// at a time (n_seqs: none), and its work.
 struct Found {
   SeqWork w;
   int seq;
