@@ -31,6 +31,7 @@
 #include <algorithm>
 
 #include "cod_attn_tile.h"
+#include "kv_span.h"
 #include "tensor_args.h"
 
 namespace pard {
@@ -391,32 +392,24 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
     const int pos0 = it.w.len - it.w.rows;             // of the sequence's first row
     auto row_of = [&](int pair) { return quotient(min(pair, n_pairs - 1), a.by_group); };
 
-    // what the tile's rows see: keys 0 .. a_last, then lo .. last
+    // what the tile's rows see
     const int pos_lo = pos0 + row_of(pair0), pos_hi = pos0 + row_of(pair0 + QP - 1);
-    const int last = min(pos_hi, b.cap - 1);
-    int lo = a.window ? max(pos_lo - a.window + 1, 0) : 0;
-    int a_last = min(a.sinks, lo) - 1;
-    if (a.sinks >= lo) lo = 0, a_last = -1;            // one run of keys
-    const int from = lo & ~15, n_a = (a_last + kStageKeys) / kStageKeys;
-    const int n_all = last < 0 ? 0 : n_a + (last - from) / kStageKeys + 1;
+    const KvSpan sp = kv_span(pos_lo, pos_hi, b.cap, a.window, a.sinks);
+    const int lo = sp.lo, last = sp.last, a_last = sp.a_last;
+    const int from = kv_from(sp), n_a = kv_first_stages(sp, kStageKeys), n_all = kv_stages(sp, kStageKeys);
     const int st0 = (int)((int64_t)n_all * it.split / it.splits), st1 = (int)((int64_t)n_all * (it.split + 1) / it.splits);
 
     // this wavefront's 16 keys of a stage: blocks past a run repeat its last key
-    struct Block { int key, low, high; };
-    auto block_of = [&](int st) __attribute__((always_inline)) {
-      const bool in_a = st < n_a;
-      const int key = (in_a ? st * kStageKeys : from + (st - n_a) * kStageKeys) + wave * 16, high = in_a ? a_last : last;
-      return Block{key, in_a ? 0 : lo, high};
-    };
+    auto block_of = [&](int st) __attribute__((always_inline)) { return kv_run(sp, kStageKeys, st, wave * 16); };
     const int32_t* const table = b.table + (int64_t)it.seq * b.max_pages;
     auto entry_of = [&](int st) __attribute__((always_inline)) {
-      const Block k = block_of(st);
+      const KvRun k = block_of(st);
       return table[min(k.key, k.high) >> a.cache.page_log2];
     };
     struct Parts { Staged<HD, M, DT> x[2 / KH]; };     // of K and V; with two parts, the first's wavefronts load K
     Parts p0, p1;
     auto load = [&](Parts& p, u32x4* buf, int st, int entry) __attribute__((always_inline)) {
-      const Block k = block_of(st);
+      const KvRun k = block_of(st);
       int page = __builtin_amdgcn_readfirstlane(entry);
       const bool none = (uint32_t)page >= (uint32_t)a.cache.n_pages;         // uniform
       if (none) {
@@ -490,6 +483,7 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
         for (int i = 0; i < 4; ++i) q[t][ks][i] ^= sign;
 
     auto compute = [&](int st, const u32x4* cur) __attribute__((always_inline)) {
+      // (kv_run, spelled out: called here it costs the compiler 170 scalar spills)
       const bool in_a = st < n_a;
       const int key0 = (in_a ? st * kStageKeys : from + (st - n_a) * kStageKeys) + part * NB * 16, end = key0 + NB * 16 - 1;
       const int low = in_a ? 0 : lo, high = in_a ? a_last : last;
@@ -720,25 +714,16 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
     const int pos0 = it.w.len - it.w.rows;
     auto row_of = [&](int pair) { return quotient(min(pair, n_pairs - 1), a.by_group); };
     const int pos_lo = pos0 + row_of(pair0), pos_hi = pos0 + row_of(pair0 + QP - 1);
-    const int last = min(pos_hi, b.cap - 1);
-    int lo = a.window ? max(pos_lo - a.window + 1, 0) : 0;
-    int a_last = min(a.sinks, lo) - 1;
-    if (a.sinks >= lo) lo = 0, a_last = -1;            // one run of keys
-    const int from = lo & ~15, n_a = (a_last + kFewKeys) / kFewKeys;
-    const int n_all = last < 0 ? 0 : n_a + (last - from) / kFewKeys + 1;
+    const KvSpan sp = kv_span(pos_lo, pos_hi, b.cap, a.window, a.sinks);
+    const int n_all = kv_stages(sp, kFewKeys);
     const int st0 = (int)((int64_t)n_all * it.split / it.splits), st1 = (int)((int64_t)n_all * (it.split + 1) / it.splits);
 
     // this wavefront's 32 keys of a stage
-    struct Tile { int key, low, high; };
-    auto tile_of = [&](int st) __attribute__((always_inline)) {
-      const bool in_a = st < n_a;
-      const int key = (in_a ? st * kFewKeys : from + (st - n_a) * kFewKeys) + wave * 32;
-      return Tile{key, in_a ? 0 : lo, in_a ? a_last : last};
-    };
+    auto tile_of = [&](int st) __attribute__((always_inline)) { return kv_run(sp, kFewKeys, st, wave * 32); };
     const int32_t* const table = b.table + (int64_t)it.seq * b.max_pages;
     struct Entries { int e[2]; };
     auto entries_of = [&](int st) __attribute__((always_inline)) {
-      const Tile k = tile_of(st);
+      const KvRun k = tile_of(st);
       return Entries{{table[min(k.key, k.high) >> a.cache.page_log2], table[min(k.key + 16, k.high) >> a.cache.page_log2]}};
     };
     struct Loaded {
@@ -747,7 +732,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
       bool none[2];                                    // blocks without a page
     };
     auto load = [&](Loaded& d, u32x4* vbuf, int st, const Entries& e) __attribute__((always_inline)) {
-      const Tile k = tile_of(st);
+      const KvRun k = tile_of(st);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         int page = __builtin_amdgcn_readfirstlane(e.e[i]);
@@ -782,7 +767,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
     Loaded d0, d1;
     Entries next{};
     // (a run's last stage may have no keys for this wavefront: such a tile is skipped)
-    auto here = [&](int st) __attribute__((always_inline)) { const Tile k = tile_of(st); return k.key <= k.high; };
+    auto here = [&](int st) __attribute__((always_inline)) { const KvRun k = tile_of(st); return k.key <= k.high; };
     Entries now{};
     if (st0 < st1) {                                   // uniform
       now = entries_of(st0);
@@ -825,7 +810,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
       }
       __builtin_amdgcn_sched_barrier(0);
       if (!here(st)) return;                           // uniform
-      const Tile k = tile_of(st);
+      const KvRun k = tile_of(st);
       const int end = k.key + 31;
       f32x4 sc[NT][2];
 #pragma unroll

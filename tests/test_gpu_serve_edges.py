@@ -1,0 +1,42 @@
+"""GPU checks of the serving operators at the ends of what their documentation allows:
+lengths past the page table beside windows and first tokens."""
+import pytest
+import torch
+
+import test_gpu_serve as G
+import train_common as T
+from gpu_common import say
+from test_gpu_serve import B, _gen, _randn  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _i32(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+# --------------------------------------------------------------------------
+# lengths past the table
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows", [1, 5, 9, 40, 150])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "e2m1"])
+def test_a_window_past_the_table_beside_more_first_tokens_than_it_names(B, kind, rows):  # noqa: F811
+    """The last sequence's rows past its table are NaN; the others are what they are
+    by themselves."""
+    g = _gen(rows)
+    hq, hk, hd, page, pages = 8, 2, 64, 16, 64
+    c = G._cache(B, 2 * pages, page, hk, hd, kind)
+    table = torch.arange(2 * pages, dtype=torch.int32, device="cuda").view(2, pages)
+    x = _randn(g, 2 * pages * page, hk, hd, dtype=torch.bfloat16)
+    B.kv_write(x, x, c, B.KVBatch(table, _i32(0, 1024, 2048), _i32(1024, 1024)))
+    q = _randn(g, 2 * rows, hq, hd, dtype=torch.bfloat16)
+    for window, sinks in ((100, 2048), (100, 1025), (1, 1 << 30), (100, 4), (1024, 2048)):
+        for past in (2200, 1023 + rows, 1024 + rows + 100, 1024 + rows // 2):
+            say(f"[gpu] past the table {kind} {rows} {window} {sinks} {past}")
+            out, lse = B.kv_attn(q, c, B.KVBatch(table, _i32(0, rows, 2 * rows), _i32(900, past)), window=window, sinks=sinks)
+            one, one_lse = B.kv_attn(q[:rows], c, B.KVBatch(table[:1].contiguous(), _i32(0, rows), _i32(900)), window=window, sinks=sinks)
+            T.assert_within(out[:rows], one.double().cpu(), 2.0 ** -6 * one.double().cpu().abs() + 2.0 ** -6, "the other sequence")
+            bad = torch.cat([torch.zeros(rows, dtype=torch.bool), past - rows + torch.arange(rows) >= 1024])
+            assert out.cpu()[bad].isnan().all() and lse.cpu()[:, bad].isnan().all()
+            assert out.cpu()[~bad].isfinite().all() and lse.cpu()[:, ~bad].isfinite().all()
