@@ -797,6 +797,8 @@ def logits_adjust(logits, tokens=None, row_len=None, prompt_len=None, row_seq=No
     pointers = [vec(row_seq, "row_seq", rows), vec(row_len, "row_len", rows), vec(prompt_len, "prompt_len", n_seqs),
                 *(vec(t, what, n_seqs, torch.float32) for t, what in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency"))),
                 vec(start, "bias start", n_seqs + 1), vec(ids, "bias ids", n_bias), vec(values, "bias values", n_bias, torch.float32)]
+    if n_seqs < 1:                                     # (the library wants one sequence: it has no history and no biases)
+        pointers[-3] = None
     p_mask_row = vec(mask_row, "mask_row", rows)
     with _On(dev, stream, logits, tokens, row_len, prompt_len, row_seq, repetition, presence, frequency, start, ids, values, mask, mask_row,
              out) as on:

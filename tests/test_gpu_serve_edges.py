@@ -1,8 +1,10 @@
 """GPU checks of the serving operators at the ends of what their documentation allows:
-lengths past the page table beside windows and first tokens."""
+lengths past the page table beside windows and first tokens, empty histories, masks and
+biases."""
 import pytest
 import torch
 
+import serve_common as S
 import test_gpu_serve as G
 import train_common as T
 from gpu_common import say
@@ -40,3 +42,16 @@ def test_a_window_past_the_table_beside_more_first_tokens_than_it_names(B, kind,
             bad = torch.cat([torch.zeros(rows, dtype=torch.bool), past - rows + torch.arange(rows) >= 1024])
             assert out.cpu()[bad].isnan().all() and lse.cpu()[:, bad].isnan().all()
             assert out.cpu()[~bad].isfinite().all() and lse.cpu()[:, ~bad].isfinite().all()
+
+
+# --------------------------------------------------------------------------
+# logits
+# --------------------------------------------------------------------------
+
+def test_biases_of_no_sequences(B):  # noqa: F811
+    """bias starts of one entry are those of no sequence: nothing behind it is read."""
+    x = _randn(_gen(3), 1, 70)
+    say("[gpu] biases of no sequences")
+    start = torch.tensor([0, 1], dtype=torch.int32, device="cuda")[:1]
+    out, best = B.logits_adjust(x, bias=(start, _i32(5), torch.full((1,), 100.0, device="cuda")), row_seq=_i32(0))
+    assert torch.equal(out, x) and best.tolist() == S.best_of(x)
