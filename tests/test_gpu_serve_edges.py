@@ -8,7 +8,7 @@ import serve_common as S
 import test_gpu_serve as G
 import train_common as T
 from gpu_common import say
-from test_gpu_serve import B, _gen, _randn  # noqa: F401
+from test_gpu_serve import B, INF, _gen, _randn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -47,6 +47,16 @@ def test_a_window_past_the_table_beside_more_first_tokens_than_it_names(B, kind,
 # --------------------------------------------------------------------------
 # logits
 # --------------------------------------------------------------------------
+
+def test_masks_of_no_rows(B):  # noqa: F811
+    """A row's mask that is not there allows nothing, also where none is."""
+    x = _randn(_gen(2), 4, 70)
+    mask = torch.empty(0, 3, dtype=torch.int32, device="cuda")
+    say("[gpu] masks of no rows")
+    out, best = B.logits_adjust(x, mask=mask, mask_row=_i32(0, -1, 7, -5))
+    assert bool((out[[0, 2]] == -INF).all()) and torch.equal(out[[1, 3]], x[[1, 3]])
+    assert best.tolist() == [-1, int(x[1].argmax()), -1, int(x[3].argmax())]
+
 
 def test_biases_of_no_sequences(B):  # noqa: F811
     """bias starts of one entry are those of no sequence: nothing behind it is read."""
