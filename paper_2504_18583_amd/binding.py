@@ -800,7 +800,8 @@ def logits_adjust(logits, tokens=None, row_len=None, prompt_len=None, row_seq=No
     if n_seqs < 1:                                     # (the library wants one sequence: it has no history and no biases)
         pointers[-3] = None
     p_mask_row = vec(mask_row, "mask_row", rows)
-    # (of no rows: a mask all the same, of which no word is read)
+    # (histories of no tokens, a mask of no rows: there all the same, and no word of them is read)
+    p_tokens = None if tokens is None or n_seqs < 1 else tokens.data_ptr() or pointers[1]
     p_mask = None if mask is None else mask.data_ptr() or p_mask_row
     with _On(dev, stream, logits, tokens, row_len, prompt_len, row_seq, repetition, presence, frequency, start, ids, values, mask, mask_row,
              out) as on:
@@ -810,7 +811,7 @@ def logits_adjust(logits, tokens=None, row_len=None, prompt_len=None, row_seq=No
             _bad("logits_adjust: out: a tensor like logits is wanted")
         top = torch.empty(rows, dtype=torch.int32, device=dev) if best else None
         args = pard_logits_args(rows, vocab, _dtype(logits, "logits_adjust"), max(n_seqs, 1), logits.data_ptr(), logits.stride(0),
-                                out.data_ptr(), out.stride(0), None if tokens is None else tokens.data_ptr(),
+                                out.data_ptr(), out.stride(0), p_tokens,
                                 0 if tokens is None else tokens.shape[1], *pointers, n_bias, 0 if mask is None else mask.shape[0],
                                 p_mask, 0 if mask is None else mask.shape[1], p_mask_row,
                                 None if top is None else top.data_ptr())

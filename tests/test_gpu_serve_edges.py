@@ -48,6 +48,16 @@ def test_a_window_past_the_table_beside_more_first_tokens_than_it_names(B, kind,
 # logits
 # --------------------------------------------------------------------------
 
+def test_empty_histories(B):  # noqa: F811
+    """Sequences without a token yet: penalties change nothing."""
+    x = _randn(_gen(1), 3, 700)
+    none, lens, one = torch.empty(3, 0, dtype=torch.int32, device="cuda"), _i32(0, 5, -1), torch.full((3,), 1.5, device="cuda")
+    say("[gpu] empty histories")
+    for kw in (dict(repetition=one), dict(presence=one), dict(frequency=one), dict(repetition=one, presence=one, frequency=one), {}):
+        out, best = B.logits_adjust(x, none, lens, **kw)
+        assert torch.equal(out, x) and best.tolist() == S.best_of(x)
+
+
 def test_masks_of_no_rows(B):  # noqa: F811
     """A row's mask that is not there allows nothing, also where none is."""
     x = _randn(_gen(2), 4, 70)
