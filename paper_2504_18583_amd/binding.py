@@ -630,6 +630,12 @@ def _no_gradient(what: str, *tensors) -> None:
             _bad(f"{what} has no gradient: call it under torch.no_grad()")
 
 
+def _int32(n: int) -> int:
+    """A count for a 32-bit field, which would keep its low bits only: the largest
+    stands for all above (positions are below 2^30), -1 for what is refused."""
+    return min(max(n, -1), 2 ** 31 - 1)
+
+
 class KVCache:
     """A paged cache of one layer (pard_kv_cache) in the caller's tensors: k, v
     [pages, kv heads, page size, head_dim] in bfloat16 or float16; or in uint8,
@@ -690,7 +696,7 @@ class KVBatch:
         n, self.device = page_table.shape[0], page_table.device
         _vector(row_start, "row_start", n + 1, torch.int32, self.device)
         _vector(kv_len, "kv_len", n, torch.int32, self.device)
-        self.page_table, self.row_start, self.kv_len, self.max_seq_rows = page_table, row_start, kv_len, int(max_seq_rows)
+        self.page_table, self.row_start, self.kv_len, self.max_seq_rows = page_table, row_start, kv_len, _int32(int(max_seq_rows))
         self._fields = (*page_table.shape, self.max_seq_rows, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr())
         self.tensors = page_table, row_start, kv_len
 
@@ -751,7 +757,8 @@ def kv_attn(q, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, wi
         _bad(f"kv_attn: head_dim {hd}, the cache has {cache.head_dim}")
     _same_device("kv_attn", q.device, cache, batch)
     scale = hd ** -0.5 if scale is None else float(scale)
-    args = pard_kv_attn_args(C.pointer(cache.c), C.pointer(batch.c(rows)), n_q, _dtype(q, "kv_attn"), window, sinks, scale)
+    args = pard_kv_attn_args(C.pointer(cache.c), C.pointer(batch.c(rows)), n_q, _dtype(q, "kv_attn"), _int32(window), _int32(sinks),
+                             scale)
     with _On(q.device, stream, q, *cache.tensors, *batch.tensors, out) as on:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

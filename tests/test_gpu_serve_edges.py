@@ -1,6 +1,6 @@
 """GPU checks of the serving operators at the ends of what their documentation allows:
 lengths past the page table beside windows and first tokens, empty histories, masks and
-biases."""
+biases, windows past 32 bits."""
 import pytest
 import torch
 
@@ -42,6 +42,33 @@ def test_a_window_past_the_table_beside_more_first_tokens_than_it_names(B, kind,
             bad = torch.cat([torch.zeros(rows, dtype=torch.bool), past - rows + torch.arange(rows) >= 1024])
             assert out.cpu()[bad].isnan().all() and lse.cpu()[:, bad].isnan().all()
             assert out.cpu()[~bad].isfinite().all() and lse.cpu()[:, ~bad].isfinite().all()
+
+
+# --------------------------------------------------------------------------
+# windows and hints past 32 bits
+# --------------------------------------------------------------------------
+
+def test_sizes_past_32_bits(B):  # noqa: F811
+    """A window, first tokens or a hint of 2^32 and a few are large, not a few."""
+    g = _gen(3)
+    batch = S.Batch([1, 20], [300, 90], 16)
+    c = B.KVCache(*(_randn(g, batch.n_pages, 2, 16, 64, dtype=torch.bfloat16) for _ in "kv"))
+    q, on = _randn(g, batch.n, 4, 64, dtype=torch.bfloat16), batch.device(B)
+    say("[gpu] windows past 32 bits")
+    want, want_lse = B.kv_attn(q, c, on)
+    for size in (2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63, 2 ** 70):
+        for kw in (dict(window=size), dict(window=7, sinks=size)):
+            out, lse = B.kv_attn(q, c, on, **kw)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse), (size, kw)
+        far = batch.device(B, size)
+        assert far.max_seq_rows > 0
+        out, _ = B.kv_attn(q, c, far)
+        T.assert_within(out, want.double().cpu(), 2.0 ** -6 * want.double().cpu().abs() + 2.0 ** -7, "hint")
+    for kw in (dict(window=-1), dict(window=-2 ** 32), dict(window=-2 ** 40 + 3), dict(window=7, sinks=-2 ** 32 + 1)):
+        with pytest.raises(B.PardError, match="pard_kv_attn"):
+            B.kv_attn(q, c, on, **kw)
+    with pytest.raises(B.PardError, match="pard_kv_attn"):
+        B.kv_attn(q, c, batch.device(B, -2 ** 32 + 1))
 
 
 # --------------------------------------------------------------------------
