@@ -25,9 +25,21 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64, kPer = 16, kChunk = kThreads * kPer, kMaxRun = 32;
 
-// Products and sums by themselves: what is left out changes nothing else.
-__device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
-__device__ __forceinline__ float sub(float a, float b) { return __fsub_rn(a, b); }
+// Products and sums by themselves, each rounded: by default the compiler makes one
+// operation of both (v - f c as one fused multiply-add), also of __fmul_rn and
+// __fsub_rn, which are plain operators here.
+__device__ __forceinline__ float mul(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+__device__ __forceinline__ float sub(float a, float b) {
+#pragma clang fp contract(off)
+  return a - b;
+}
+__device__ __forceinline__ float plus(float a, float b) {
+#pragma clang fp contract(off)
+  return a + b;
+}
 
 template <class E>
 __device__ __forceinline__ typename E::T minus_inf() { return E::store(-INFINITY); }
@@ -216,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_logits(const LogitsArgs a, int run
               if (c && a.frequency) v = sub(v, mul(freq, (float)c));
               if (c && a.presence) v = sub(v, pres);
             }
-            if (b[j]) v = __fadd_rn(v, a.bias_values[b[j] - 1]);
+            if (b[j]) v = plus(v, a.bias_values[b[j] - 1]);
             x[j] = E::store(v);
           }
         }

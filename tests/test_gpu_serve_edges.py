@@ -1,6 +1,7 @@
 """GPU checks of the serving operators at the ends of what their documentation allows:
-lengths past the page table beside windows and first tokens, empty histories, masks and
-biases, windows past 32 bits."""
+lengths past the page table beside windows and first tokens, the documented order of the
+logits' operations, empty histories, masks and biases, windows past 32 bits."""
+import numpy as np
 import pytest
 import torch
 
@@ -74,6 +75,48 @@ def test_sizes_past_32_bits(B):  # noqa: F811
 # --------------------------------------------------------------------------
 # logits
 # --------------------------------------------------------------------------
+
+def _in_order(x, tokens, row_len, prompt_len, row_seq, repetition, presence, frequency, bias):
+    """The documented steps as single float32 operations, one after the other."""
+    y, vocab = x.float().cpu().numpy().copy(), x.shape[1]
+    f32 = np.float32
+    for r in range(len(y)):
+        s = int(row_seq[r])
+        h = tokens[s, :int(row_len[r])].numpy()
+        had = np.bincount(h, minlength=vocab)[:vocab] > 0
+        c = np.bincount(h[int(prompt_len[s]):], minlength=vocab)[:vocab]
+        rep, pre, fre = (f32(t[s]) for t in (repetition, presence, frequency))
+        y[r] = np.where(had, np.where(y[r] > 0, y[r] / rep, y[r] * rep), y[r])
+        step = fre * c.astype(f32)
+        y[r] = np.where(c > 0, y[r] - step, y[r])
+        y[r] = np.where(c > 0, y[r] - pre, y[r])
+        lo, hi = int(bias[0][s]), int(bias[0][s + 1])
+        for t, b in {int(t): f32(b) for t, b in zip(bias[1][lo:hi], bias[2][lo:hi])}.items():
+            y[r, t] = y[r, t] + b
+    return torch.from_numpy(y).to(x.dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [70, 4096, 9001])
+def test_logits_are_the_documented_operations(B, dtype, vocab):  # noqa: F811
+    """Bit by bit: no product and sum become one operation."""
+    g = _gen(vocab)
+    rows, seqs, history = 24, 4, 3000
+    logits = _randn(g, rows, vocab, dtype=T.DTYPES[dtype], std=4.0)
+    tokens = torch.randint(0, vocab, (seqs, history), generator=g, device="cuda", dtype=torch.int32)
+    rand = lambda n: torch.rand(n, generator=g, device="cuda")  # noqa: E731
+    row_seq = torch.arange(rows, dtype=torch.int32, device="cuda") * seqs // rows
+    row_len = history - rows + torch.arange(rows, dtype=torch.int32, device="cuda")
+    args = dict(tokens=tokens, row_len=row_len, prompt_len=_i32(0, 700, 10, 2999), row_seq=row_seq, repetition=1 + rand(seqs),
+                presence=rand(seqs) - 0.3, frequency=rand(seqs) / 3,
+                bias=(_i32(0, 40, 40, 60, 60), torch.randint(0, vocab, (60,), generator=g, device="cuda", dtype=torch.int32), _randn(g, 60)))
+    say(f"[gpu] logits in order {dtype} {vocab}")
+    out, best = B.logits_adjust(logits, **args)
+    want = _in_order(logits, **{k: tuple(t.cpu() for t in v) if isinstance(v, tuple) else v.cpu() for k, v in args.items()})
+    off = out.cpu() != want
+    assert not bool(off.any()), f"{int(off.sum())} of {off.numel()} differ, first {out.cpu()[off][:3].tolist()} for {want[off][:3].tolist()}"
+    assert best.tolist() == S.best_of(want)
+
 
 def test_empty_histories(B):  # noqa: F811
     """Sequences without a token yet: penalties change nothing."""
