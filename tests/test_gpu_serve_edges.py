@@ -1,10 +1,12 @@
 """GPU checks of the serving operators at the ends of what their documentation allows:
-lengths past the page table beside windows and first tokens, the documented order of the
-logits' operations, empty histories, masks and biases, windows past 32 bits."""
+lengths past the page table beside windows and first tokens, float16 over long contexts,
+the documented order of the logits' operations, empty histories, masks and biases,
+windows past 32 bits."""
 import numpy as np
 import pytest
 import torch
 
+import serve_bounds as SB
 import serve_common as S
 import test_gpu_serve as G
 import train_common as T
@@ -43,6 +45,37 @@ def test_a_window_past_the_table_beside_more_first_tokens_than_it_names(B, kind,
             bad = torch.cat([torch.zeros(rows, dtype=torch.bool), past - rows + torch.arange(rows) >= 1024])
             assert out.cpu()[bad].isnan().all() and lse.cpu()[:, bad].isnan().all()
             assert out.cpu()[~bad].isfinite().all() and lse.cpu()[:, ~bad].isfinite().all()
+
+
+# --------------------------------------------------------------------------
+# float16
+# --------------------------------------------------------------------------
+
+LONG = [([1], [4000], 4096, 4, 1, 128), ([13, 2], [900, 1500], 128, 28, 4, 128), ([9], [9000], 16, 16, 4, 64), ([1], [20000], 64, 8, 1, 128),
+        ([70], [8000], 16, 4, 2, 64), ([2, 5], [12000, 30], 32, 16, 2, 64), ([9, 9], [9000, 200], 16, 8, 2, 128)]
+
+
+@pytest.mark.parametrize("kind", ["f16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: f"{s[0]}-{s[1]}-{s[2:]}")
+def test_float16_over_long_contexts(B, monkeypatch, shape, kind):  # noqa: F811
+    monkeypatch.setattr(S, "attn_ref", SB.sharp_attn_ref)
+    G._check_attn(B, *shape, "f16", kind, lead=1, trail=2)
+
+
+@pytest.mark.parametrize("shape", G.ATTN, ids=lambda s: f"{s[0][:3]}-{s[1][:3]}-{s[2:]}")
+def test_float16(B, monkeypatch, shape):  # noqa: F811
+    monkeypatch.setattr(S, "attn_ref", SB.sharp_attn_ref)
+    for kind in ("f16", "e4m3", "e2m1"):
+        G._check_attn(B, *shape, "f16", kind)
+
+
+@pytest.mark.parametrize("kind", ["f16", "e4m3", "e2m1"])
+def test_float16_peaked_and_within_windows(B, monkeypatch, kind):  # noqa: F811
+    """Probabilities far below the largest, which float16 holds as subnormals."""
+    monkeypatch.setattr(S, "attn_ref", SB.sharp_attn_ref)
+    for window, sinks, std in ((0, 0, 3.0), (0, 0, 8.0), (500, 4, 3.0), (100, 300, 2.0)):
+        G._check_attn(B, [1, 9, 2], [3000, 600, 40], 16, 8, 2, 64, "f16", kind, window, sinks, std=std)
+        G._check_attn(B, [5, 150], [1200, 70], 32, 8, 2, 128, "f16", kind, window, sinks, std=std)
 
 
 # --------------------------------------------------------------------------
