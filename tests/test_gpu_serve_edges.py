@@ -1,7 +1,7 @@
 """GPU checks of the serving operators at the ends of what their documentation allows:
-lengths past the page table beside windows and first tokens, float16 over long contexts,
-the documented order of the logits' operations, empty histories, masks and biases,
-windows past 32 bits."""
+lengths past the page table beside windows and first tokens, every scale byte of a
+cache, float16 over long contexts, the documented order of the logits' operations, empty
+histories, masks and biases, windows past 32 bits."""
 import numpy as np
 import pytest
 import torch
@@ -76,6 +76,80 @@ def test_float16_peaked_and_within_windows(B, monkeypatch, kind):  # noqa: F811
     for window, sinks, std in ((0, 0, 3.0), (0, 0, 8.0), (500, 4, 3.0), (100, 300, 2.0)):
         G._check_attn(B, [1, 9, 2], [3000, 600, 40], 16, 8, 2, 64, "f16", kind, window, sinks, std=std)
         G._check_attn(B, [5, 150], [1200, 70], 32, 8, 2, 128, "f16", kind, window, sinks, std=std)
+
+
+# --------------------------------------------------------------------------
+# every scale byte
+# --------------------------------------------------------------------------
+
+def _bytes(g, *shape):
+    return torch.randint(0, 256, shape, generator=g, device="cuda", dtype=torch.uint8)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "e2m1"])
+def test_reading_every_scale_byte(B, kind):  # noqa: F811
+    """All codes under the scales 2^-127 to 2^127 and NaN, rounded once to each type."""
+    for hd in (64, 128):
+        g = _gen(hd)
+        c = G._cache(B, 64, 16, 1, hd, kind)
+        for t in (c.k, c.v):
+            t.copy_(_bytes(g, *t.shape))
+        n = 64 * 16
+        c.k_scale.copy_((torch.arange(n * hd // 32, device="cuda") % 256).to(torch.uint8).view(c.k_scale.shape))
+        c.v_scale.copy_(_bytes(g, *c.v_scale.shape))
+        on = B.KVBatch(torch.arange(64, dtype=torch.int32, device="cuda")[None].contiguous(), _i32(0, n), _i32(n))
+        for dtype in ("f32", "bf16", "f16"):
+            say(f"[gpu] scale bytes {kind} {hd} {dtype}")
+            for got, t, s in zip(B.kv_read(c, on, n, T.DTYPES[dtype]), (c.k, c.v), (c.k_scale, c.v_scale)):
+                # (a value has 4 bits at most: float32 holds all within its range, and loses what is below)
+                want = S.decoded(t, s, kind).view(n, 1, hd).float().to(T.DTYPES[dtype])
+                nan = want.isnan()
+                assert torch.equal(got.cpu().isnan(), nan)
+                off = (got.cpu() != want) & ~nan
+                assert not bool(off.any()), (int(off.sum()), got.cpu()[off][:4], want[off][:4], s.view(n, -1).cpu()[off.nonzero()[:4, 0]])
+
+
+@pytest.mark.parametrize("rows", [1, 5, 9, 40, 150])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("kind", ["e4m3", "e2m1"])
+def test_attention_over_every_scale(B, kind, dtype, rows):  # noqa: F811
+    """Keys and values whose blocks have scales from 2^-127 on; and, in a sequence of
+    their own, blocks of NaN."""
+    dt = T.DTYPES[dtype]
+    for hd in (64, 128):
+        g = _gen(rows + hd)
+        hq, hk, page, n = 8, 2, 16, 320
+        c = G._cache(B, 41, page, hk, hd, kind)
+        for t in (c.k, c.v):
+            # (no codes of NaN)
+            t.copy_(_bytes(g, *t.shape) & 0xf7 if kind == "e4m3" else _bytes(g, *t.shape))
+        small = torch.tensor([0, 1, 2, 60, 110, 112, 114, 119, 120, 121], dtype=torch.uint8, device="cuda")
+        for t in (c.k_scale, c.v_scale):
+            t.copy_(small[torch.randint(0, len(small), t.shape, generator=g, device="cuda")])
+        q = _randn(g, 2 * rows, hq, hd, dtype=dt, std=0.25)
+        table = torch.arange(40, dtype=torch.int32, device="cuda").view(2, 20)
+        on = B.KVBatch(table, _i32(0, rows, 2 * rows), _i32(n, n))
+        say(f"[gpu] attention over every scale {kind} {dtype} {hd} {rows}")
+        batch = S.Batch([rows, rows], [n - rows] * 2, page)
+
+        def of(t, s):
+            v = S.decoded(t, s, kind)[:40].transpose(1, 2).reshape(2, n, hk, hd).to(torch.float32).to(dt).double()
+            return lambda seq, j: v[seq, torch.as_tensor(j)]
+        ref = SB.sharp_attn_ref(q, of(c.k, c.k_scale), of(c.v, c.v_scale), batch, hd ** -0.5)
+        out, lse = B.kv_attn(q, c, on)
+        # (2^-118: what products of the smallest values lose below float32's normal range)
+        T.assert_within(out, ref["out"][0], ref["out"][1] + 2.0 ** -118, "out")
+        T.assert_within(lse, *ref["lse"], "lse")
+        # one key, then one value, of the second sequence NaN: key head 1, position 3
+        for t in (c.k_scale, c.v_scale):
+            old = t[20, 1, 3, 0].clone()
+            t[20, 1, 3, 0] = 255
+            got, got_lse = B.kv_attn(q, c, on)
+            assert torch.equal(got[:rows], out[:rows]) and torch.equal(got_lse[:, :rows], lse[:, :rows])
+            assert torch.equal(got[rows:, :4], out[rows:, :4])           # heads of key head 0
+            bad = got[rows:, 4:] if t is c.k_scale else got[rows:, 4:, :32]
+            assert bad.isnan().all()
+            t[20, 1, 3, 0] = old
 
 
 # --------------------------------------------------------------------------
