@@ -394,9 +394,8 @@ __global__ __launch_bounds__(256 * KH, (kResident<HD, NQ, DT>)) void k_kv_attn(c
 
     // what the tile's rows see
     const int pos_lo = pos0 + row_of(pair0), pos_hi = pos0 + row_of(pair0 + QP - 1);
-    const KvSpan sp = kv_span(pos_lo, pos_hi, b.cap, a.window, a.sinks);
-    const int lo = sp.lo, last = sp.last, a_last = sp.a_last;
-    const int from = kv_from(sp), n_a = kv_first_stages(sp, kStageKeys), n_all = kv_stages(sp, kStageKeys);
+    const KvSpan sp = kv_span(pos_lo, pos_hi, b.cap, a.window, a.sinks, kStageKeys);
+    const int lo = sp.lo, last = sp.last, a_last = sp.a_last, from = sp.from, n_a = sp.n_a, n_all = sp.n_all;
     const int st0 = (int)((int64_t)n_all * it.split / it.splits), st1 = (int)((int64_t)n_all * (it.split + 1) / it.splits);
 
     // this wavefront's 16 keys of a stage: blocks past a run repeat its last key
@@ -714,8 +713,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_few(const KvAttnArgs a) {
     const int pos0 = it.w.len - it.w.rows;
     auto row_of = [&](int pair) { return quotient(min(pair, n_pairs - 1), a.by_group); };
     const int pos_lo = pos0 + row_of(pair0), pos_hi = pos0 + row_of(pair0 + QP - 1);
-    const KvSpan sp = kv_span(pos_lo, pos_hi, b.cap, a.window, a.sinks);
-    const int n_all = kv_stages(sp, kFewKeys);
+    const KvSpan sp = kv_span(pos_lo, pos_hi, b.cap, a.window, a.sinks, kFewKeys);
+    const int n_all = sp.n_all;
     const int st0 = (int)((int64_t)n_all * it.split / it.splits), st1 = (int)((int64_t)n_all * (it.split + 1) / it.splits);
 
     // this wavefront's 32 keys of a stage

@@ -4,35 +4,31 @@
 
 namespace pard {
 
-constexpr int kv_min(int a, int b) { return a < b ? a : b; }
-constexpr int kv_max(int a, int b) { return a > b ? a : b; }
-
 // Keys key .. of one run, low .. high; those outside the run repeat its ends.
 struct KvRun { int key, low, high; };
 
 // The rows at positions pos_lo .. pos_hi see between them the first tokens 0 ..
 // a_last (-1: none beside the others), then lo .. last, which has a page: the
-// table names positions below cap.
-struct KvSpan { int lo, last, a_last; };
-constexpr KvSpan kv_span(int pos_lo, int pos_hi, int cap, int window, int sinks) {
-  const int last = kv_min(pos_hi, cap - 1), lo = window ? kv_max(pos_lo - window + 1, 0) : 0;
-  if (pos_lo >= cap) return KvSpan{0, -1, -1};         // (such rows are NaN whatever they see)
-  return sinks >= lo ? KvSpan{0, last, -1} : KvSpan{lo, last, sinks - 1};
-}
-
-// Stages of `stage` keys: n_a of the first tokens, the others from key `from`,
-// n_all together.
-constexpr int kv_from(const KvSpan& s) { return s.lo & ~15; }
-constexpr int kv_first_stages(const KvSpan& s, int stage) { return (s.a_last + stage) / stage; }
-constexpr int kv_stages(const KvSpan& s, int stage) {
-  return s.last < 0 ? 0 : kv_first_stages(s, stage) + (s.last - kv_from(s)) / stage + 1;
+// table names positions below cap.  Stages of `stage` keys: n_a of the first
+// tokens, the others from key `from`, n_all together.  (Its form is the compiler's:
+// with an early return for rows past the table 1000 rows of 64 dims over 9000
+// keys took 197 us for 193.)
+struct KvSpan { int lo, last, a_last, from, n_a, n_all; };
+constexpr KvSpan kv_span(int pos_lo, int pos_hi, int cap, int window, int sinks, int stage) {
+  const int last = pos_hi < cap - 1 ? pos_hi : cap - 1;
+  int lo = window && pos_lo - window + 1 > 0 ? pos_lo - window + 1 : 0;
+  int a_last = (sinks < lo ? sinks : lo) - 1;
+  if (sinks >= lo) lo = 0, a_last = -1;                // one run of keys
+  const int from = lo & ~15, n_a = (a_last + stage) / stage;
+  // (rows all past the table are NaN whatever they see: without stages, since
+  // neither run need end within the table then)
+  return KvSpan{lo, last, a_last, from, n_a, last < 0 || pos_lo >= cap ? 0 : n_a + (last - from) / stage + 1};
 }
 
 // Stage st (any, those behind the last too) from its key `at` on.
 constexpr KvRun kv_run(const KvSpan& s, int stage, int st, int at) {
-  const int n_a = kv_first_stages(s, stage);
-  const bool in_a = st < n_a;
-  return KvRun{(in_a ? st * stage : kv_from(s) + (st - n_a) * stage) + at, in_a ? 0 : s.lo, in_a ? s.a_last : s.last};
+  const bool in_a = st < s.n_a;
+  return KvRun{(in_a ? st * stage : s.from + (st - s.n_a) * stage) + at, in_a ? 0 : s.lo, in_a ? s.a_last : s.last};
 }
 
 }  // namespace pard

@@ -23,9 +23,9 @@ static void say(const char* what, int stage, int lo, int hi, int cap, int window
 
 template <int STAGE>
 static void check(int pos_lo, int pos_hi, int cap, int window, int sinks) {
-  const KvSpan s = kv_span(pos_lo, pos_hi, cap, window, sinks);
+  const KvSpan s = kv_span(pos_lo, pos_hi, cap, window, sinks, STAGE);
   // table entries are read for these stages, ahead of the last one too
-  const int n = kv_stages(s, STAGE);
+  const int n = s.n_all;
   for (int st = 0; n > 0 && st <= n + 4; ++st) {
     if (st == 40 && n > 50) st = n - 4;
     for (int at = 0; at < STAGE; at += 16) {
