@@ -601,7 +601,8 @@ typedef struct {
  * smallest scale 2^e, e >= -126, that brings it within the type's range (448 or
  * 6: nothing saturates); a block that holds a NaN or an infinity becomes NaN.  A
  * row whose position is negative or has no page (past max_pages, or an entry
- * outside [0, n_pages)) is not written.  Two rows in one place: either.
+ * outside [0, n_pages)) is not written.  Two rows in one place: parts of both, also
+ * a block's scale of one beside elements of the other.
  * pard_kv_read reads the rows' places back (a row without a place: NaN): with
  * row_start covering whole sequences, all of them.  Values are rounded to dtype.
  * Vectorised where the rows' data and strides are multiples of 16 bytes.

@@ -20,10 +20,11 @@
 // passes: memory behind a chain of dependent reads (lengths, table, keys: 5 us of
 // a workgroup's life) and the join (32 sequences of 512 to 1536 keys, 9 rows: 32
 // us for 136 MB and 5 for the join).  Chunks: the SIMDs' issue (4096 rows at 4096,
-// 32 / 8 heads x 128: 425 us, 970 TFLOP/s in bf16 and e4m3; x 64: 260 and 267 us in e2m1,
-// 790; two chunks of 3641 and 2606 rows 860 us: products 43 % of the SIMDs'
-// cycles, other instructions 45 %).  Within a window of 1024 a tile sees 18 stages,
-// of which four compare, and a row of 150 makes 4.7 tiles: products 24 %, others 58.
+// 32 / 8 heads x 128: 425 us, 970 TFLOP/s in bf16 and e4m3; x 64: 255 us in bf16, 267 in
+// e2m1, 809 and 772: products 42 % of the SIMDs' cycles, other instructions 75 %, as
+// the softmax of a score is the same for half the products; two chunks of 3641 and
+// 2606 rows x 128 860 us: 43 and 45 %).  Within a window of 1024 a tile sees 18 stages,
+// of which four compare, and a row of 150 makes 4.7 tiles: products 23 %, others 57.
 // A wavefront per row and head, key by key, took 23.9 ms for the contexts in e4m3
 // and 139 for the chunks.
 #include "serve.h"
@@ -54,7 +55,7 @@ constexpr int kShares = QP == 16 ? 1024 : 512;
 // One sequence's work.
 struct SeqWork {
   int row0, rows, len;                     // first row, rows, positions
-  int tiles;                               // of 64 NQ pairs
+  int tiles;                               // of QP pairs
   int stages;                              // of a tile, at most
 };
 
@@ -344,7 +345,10 @@ __device__ __forceinline__ void meet_with_loads() {
 template <int HD, int QP>
 constexpr int kRecord = QP * (HD + 2);
 
-// Wavefronts a SIMD, as LDS and registers allow.
+// Wavefronts a SIMD, as LDS and registers allow.  (Two tiles of pairs x 64 dims in 16
+// bits: four keep 12 registers in memory, and chunks of 4096 rows at 4096 took 255 us
+// for 276 with three, of 1000 at 9000 193 for 189.  In 8 and 4 bits four spill more:
+// 101 us for 83 in the window.)
 template <int HD, int NQ, int DT>
 constexpr int kResident = NQ == 1 ? 4 : HD == 128 ? 2 : kv_scale_bytes(DT, HD) ? 3 : 4;
 

@@ -8,8 +8,8 @@
 //
 // Bound: memory, each element read once and written once (30 778 rows of 8 heads x
 // 128: into e2m1 34 us, back to bf16 30, 4.7 and 5.3 TB/s; 66 246 rows out of e4m3
-// 83 us, 4.9).  With an address of its own for every unit, not a step from head to
-// head, it was issue: 40, 34 and 98 us, the VALU busy 93, 100 and 69 % of the time.
+// 83 us, 4.9; the VALU busy 58, 58 and 36 % of the time).  With an address of its own
+// for every unit, not a step from head to head, it was issue: 40, 34 and 98 us.
 #include "serve.h"
 
 #include <algorithm>

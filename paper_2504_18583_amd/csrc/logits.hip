@@ -11,7 +11,7 @@
 // a row is worked on; vectors without a word set only pass the mask.
 //
 // Bound: memory, a logit read and written once (288 rows of 128 256 floats, histories
-// to 1545: 73 us, 4.1 TB/s, the VALU busy 42 % of the time).  Eight ids a thread,
+// to 1545: 74 us, 4.0 TB/s, the VALU busy 42 % of the time).  Eight ids a thread,
 // barriers a row for its token and its pick, and nothing in flight ahead took 119;
 // without non-temporal accesses it was 77.
 #include "serve.h"
